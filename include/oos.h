@@ -70,9 +70,11 @@ extern "C" {
                                   must be destroyed and created again */
 #define OOS_EUNSUPPORTED (-6)  /* shape outside what the kernels handle (see oos_model_create) */
 #define OOS_EWORKSPACE (-7)    /* workspace NULL, misaligned (256 B) or smaller than oos_workspace_bytes */
+#define OOS_EBATCH (-8)        /* batch operators: offsets, a length or a page the device found out of range */
 
 #define OOS_DTYPE_F32 0
 #define OOS_DTYPE_BF16 1
+#define OOS_DTYPE_F16 2        /* batch operators only: a model's binary16 cache is oos_model_config.kv_f16 */
 
 /* Model shape.  Supported: dtype BF16 with head_dim 128, hidden, q_dim and
  * intermediate multiples of 128 (tcgen05 path); dtype F32 with head_dim <= 128
@@ -370,6 +372,127 @@ int oos_lm_head_argmax_static(int32_t dtype, int32_t vocab, int32_t hidden_dim, 
  * counterpart).  Applies to work enqueued on `stream` after the call;
  * synchronises `stream`. */
 int oos_set_wait_limit(oos_model* m, uint64_t limit_ns, void* stream);
+
+/* ---- Batch operators: many requests behind one shared prompt ------------
+ * The requests of a tool-calling service begin alike (system prompt and tool
+ * schemas); the paper verifies one request at a time and has no counterpart.
+ * The shared prompt is prefilled once into an oos_kv_cache (oos_prefill); what
+ * each request adds lives in pages of its own.  One step of a layer is: project
+ * q, k, v (the caller's product), oos_qk_norm_rope on q, oos_paged_append of k
+ * and v, oos_shared_prefix_attention.  All three are stream-ordered, allocate
+ * nothing, keep nothing between calls and may be captured into a CUDA graph;
+ * calls may overlap on the GPU as long as no call writes what another uses.
+ *
+ * Element types are OOS_DTYPE_F32, _BF16 and _F16; head_dim is even, 2..128
+ * (OOS_EUNSUPPORTED otherwise).  Rows of q, k, v and out are tokens: the heads
+ * of a token are contiguous ([heads][head_dim]), consecutive tokens `stride`
+ * elements apart (>= heads * head_dim), so that q, k and v may be slices of one
+ * projection's rows.  Any address that is a multiple of the element size works;
+ * 16-byte-aligned rows take the wide loads. */
+
+/* Rotation rates theta^(-2m/d) of the pairs (m, m + d/2); factor > 1 rescales
+ * them as the fields of the same meaning in oos_model_config do. */
+typedef struct {
+    float theta;
+    float factor;
+    float low_freq_factor;
+    float high_freq_factor;
+    int32_t orig_max_pos;
+} oos_rope_config;
+
+/* One layer's pages: K and V of page p, position s of it, in
+ * [n_pages][page_size][n_kv_heads][head_dim], the cache layout cut into pages. */
+typedef struct {
+    int32_t dtype;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page_size;   /* positions per page, >= 1 */
+    int32_t n_pages;
+    void* k;             /* DEVICE */
+    void* v;             /* DEVICE */
+} oos_paged_cache;
+
+/* The tokens of one step.  Sequence b owns rows [q_start[b], q_start[b+1]) of
+ * q, k, v and out, its n_b = q_start[b+1] - q_start[b] newest positions; none is
+ * allowed.  Positions behind the shared prefix are counted from 0: the sequence
+ * holds seq_len[b] of them after this step, row j of its rows being position
+ * seq_len[b] - n_b + j, and position s lies in page block_table[b][s / page_size],
+ * entry s % page_size.  Rows at or past q_start[n_seqs] are padding: never read
+ * into a result, never written. */
+typedef struct {
+    int32_t n_seqs;
+    int32_t n_tokens;             /* rows of q, k, v and out, >= q_start[n_seqs] */
+    int32_t max_pages;            /* columns of block_table */
+    const int32_t* q_start;       /* DEVICE [n_seqs + 1], q_start[0] = 0, not decreasing */
+    const int32_t* seq_len;       /* DEVICE [n_seqs] */
+    const int32_t* block_table;   /* DEVICE [n_seqs][max_pages] */
+} oos_batch;
+
+/* RMSNorm over each head of q and k, then the rotation, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * gain        (gain NULL: y = x)
+ *   (y_m, y_{m+d/2}) turned by positions[t] * rate_m   (rope NULL: not turned)
+ *   dtype          of q, k, the gains and the outputs
+ *   q, k           DEVICE rows of n tokens; NULL with 0 heads
+ *   q_norm, k_norm DEVICE [head_dim] or NULL
+ *   positions      DEVICE int32[n], any values (not read when rope is NULL)
+ *   q_out, k_out   DEVICE rows; either may be its input (same address and
+ *                  stride), and must not overlap an input otherwise
+ * Sums, angles and products are fp32 (the angle is reduced exactly, whatever the
+ * position); the result is rounded once.  Returns OOS_EINVAL on a NULL or
+ * out-of-range argument, OOS_EUNSUPPORTED on the head size or a type. */
+int oos_qk_norm_rope(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* q,
+                     int64_t q_stride, const void* k, int64_t k_stride, const void* q_norm, const void* k_norm,
+                     float eps, const oos_rope_config* rope, const int32_t* positions, void* q_out,
+                     int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+
+/* Append a step's K and V to the pages: K with the norm and rotation of
+ * oos_qk_norm_rope on the way (k_norm, rope NULL: without), V as it is, both
+ * rounded (nearest even) to the pages' type.
+ *   dtype          of k, v and k_norm
+ *   k, v           DEVICE rows of batch->n_tokens tokens
+ *   positions      DEVICE int32[n_tokens], what the rotation turns by (a tree's
+ *                  nodes turn by their depth, not by their place in the pages)
+ *   out_status     DEVICE int32[1], the caller's to clear: OOS_EBATCH is written
+ *                  when a row's sequence, position or page is out of range; the
+ *                  row is then left out and the others are appended.
+ * Two sequences whose tables name the same page must not append to the same
+ * position of it.  Returns OOS_EINVAL, OOS_EUNSUPPORTED, OOS_ECUDA. */
+int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32_t dtype, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, const void* k_norm, float eps,
+                     const oos_rope_config* rope, const int32_t* positions, int32_t* out_status, void* stream);
+
+/* Attention of a step's rows over the shared prefix and their own pages:
+ * out = softmax(scale * q k) v over
+ *   - the prefix: slots [0, prefix_len) of prefix_k / prefix_v, one layer's
+ *     buffers of an oos_kv_cache (DEVICE [capacity][n_kv_heads][head_dim], the
+ *     pages' type), read once for all rows; prefix_len 0 takes NULL;
+ *   - the sequence's positions up to the row's own, appended before; or, with
+ *     tree_parent (DEVICE int32[n_tokens]), its positions before this step and
+ *     the row's ancestors among the step's rows, itself included:
+ *     tree_parent[i] is the parent's place among the sequence's rows, below its
+ *     own, or -1 for a root.  At most 128 rows per sequence then.
+ * A row that sees no key gives zeros.  What lies in slots no row sees does not
+ * matter (NaN included).
+ *   dtype      of q and out.  With pages of OOS_DTYPE_F32: F32; BF16: BF16; F16:
+ *              BF16 or F16 (OOS_EUNSUPPORTED otherwise).
+ *   q, out     DEVICE rows of n_q_heads heads (a multiple of n_kv_heads)
+ *   workspace  DEVICE, >= oos_shared_prefix_attention_workspace_bytes of the same
+ *              sizes, 256-byte aligned; caller-owned scratch for the call
+ *   out_status DEVICE int32[1], the caller's to clear: OOS_EBATCH when a
+ *              sequence's offsets, length or page is out of range (positions
+ *              without a page are then not seen), OOS_ETREE when a parent is,
+ *              OOS_ETIMEOUT when a pipeline wait exceeded 2 s (out is not valid).
+ * Sums and softmax statistics are fp32.  scale > 0.  Pages and prefix of 16-bit
+ * types start on 16-byte boundaries, and n_tokens * n_q_heads + n_seqs is below
+ * 2^26 (OOS_EINVAL otherwise).  With OOS_EBATCH for a sequence's offsets, or
+ * OOS_ETREE for more than 128 of its rows, its rows of out are not valid. */
+size_t oos_shared_prefix_attention_workspace_bytes(int32_t n_q_heads, int32_t prefix_len, const oos_paged_cache* cache,
+                                                   const oos_batch* batch);
+int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q, int64_t q_stride,
+                                const void* prefix_k, const void* prefix_v, int32_t prefix_len,
+                                const oos_paged_cache* cache, const oos_batch* batch, const int32_t* tree_parent,
+                                float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                                int32_t* out_status, void* stream);
 
 /* Synchronise `stream` and return the device status of the last verify or
  * prefill (all of its prompt) on this handle: OOS_OK, OOS_ETREE or

@@ -22,12 +22,15 @@ OOS_ETREE = -4
 OOS_ETIMEOUT = -5
 OOS_EUNSUPPORTED = -6
 OOS_EWORKSPACE = -7
+OOS_EBATCH = -8
 OOS_DTYPE_F32 = 0
 OOS_DTYPE_BF16 = 1
+OOS_DTYPE_F16 = 2
 
 MAX_T = 128
 
 c_i32 = ctypes.c_int32
+c_i64 = ctypes.c_int64
 c_vp = ctypes.c_void_p
 
 
@@ -56,6 +59,22 @@ class OosWeights(ctypes.Structure):
 class OosKvCache(ctypes.Structure):
     _fields_ = [("n_layers", c_i32), ("capacity", c_i32), ("k", ctypes.POINTER(c_vp)),
                 ("v", ctypes.POINTER(c_vp))]
+
+
+class OosRopeConfig(ctypes.Structure):
+    """Rotation rates: OosRopeConfig(theta) or, rescaled, with the four other fields."""
+    _fields_ = [("theta", ctypes.c_float), ("factor", ctypes.c_float), ("low_freq_factor", ctypes.c_float),
+                ("high_freq_factor", ctypes.c_float), ("orig_max_pos", c_i32)]
+
+
+class OosPagedCache(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("n_kv_heads", c_i32), ("head_dim", c_i32), ("page_size", c_i32),
+                ("n_pages", c_i32), ("k", c_vp), ("v", c_vp)]
+
+
+class OosBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", c_i32), ("n_tokens", c_i32), ("max_pages", c_i32), ("q_start", c_vp), ("seq_len", c_vp),
+                ("block_table", c_vp)]
 
 
 _lib = None
@@ -98,6 +117,18 @@ def lib():
         L.oos_launch_attention.restype = ctypes.c_int
         L.oos_lm_head_argmax_static.argtypes = [c_i32, c_i32, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp]
         L.oos_lm_head_argmax_static.restype = ctypes.c_int
+        L.oos_qk_norm_rope.argtypes = [c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp,
+                                       ctypes.c_float, P(OosRopeConfig), c_vp, c_vp, c_i64, c_vp, c_i64, c_vp]
+        L.oos_qk_norm_rope.restype = ctypes.c_int
+        L.oos_paged_append.argtypes = [P(OosPagedCache), P(OosBatch), c_i32, c_vp, c_i64, c_vp, c_i64, c_vp,
+                                       ctypes.c_float, P(OosRopeConfig), c_vp, c_vp, c_vp]
+        L.oos_paged_append.restype = ctypes.c_int
+        L.oos_shared_prefix_attention_workspace_bytes.argtypes = [c_i32, c_i32, P(OosPagedCache), P(OosBatch)]
+        L.oos_shared_prefix_attention_workspace_bytes.restype = ctypes.c_size_t
+        L.oos_shared_prefix_attention.argtypes = [c_i32, c_i32, c_vp, c_i64, c_vp, c_vp, c_i32, P(OosPagedCache),
+                                                  P(OosBatch), c_vp, ctypes.c_float, c_vp, c_i64, c_vp,
+                                                  ctypes.c_size_t, c_vp, c_vp]
+        L.oos_shared_prefix_attention.restype = ctypes.c_int
         L.oos_status_string.argtypes = [ctypes.c_int]
         L.oos_status_string.restype = ctypes.c_char_p
         for fn in ("oos_model_create", "oos_model_destroy", "oos_tree_verify", "oos_tree_verify_debug",
@@ -139,6 +170,13 @@ def make_config(cfg, max_T, use_graph=True):
                           float(getattr(cfg, "rope_high_freq_factor", 4.0)),
                           int(getattr(cfg, "rope_orig_max_pos", 8192)),
                           int(getattr(cfg, "cache_dtype", "") == "f16"))
+
+
+def make_rope(cfg):
+    """OosRopeConfig with the rotation of an object with the synth ModelConfig fields."""
+    c = make_config(cfg, 1)
+    return OosRopeConfig(c.rope_theta, c.rope_factor, c.rope_low_freq_factor, c.rope_high_freq_factor,
+                         c.rope_orig_max_pos)
 
 
 def oos_workspace_bytes(c_cfg):
@@ -302,6 +340,156 @@ def oos_last_status(model, stream=None):
 
 def oos_status_string(code):
     return lib().oos_status_string(code).decode()
+
+
+# ---- batch operators.  What C cannot see of a tensor -- its type, shape, strides
+# and device -- is checked here and answered like C's own refusals, by OosError.
+
+_DTYPES = {torch.float32: OOS_DTYPE_F32, torch.bfloat16: OOS_DTYPE_BF16, torch.float16: OOS_DTYPE_F16}
+
+
+def _require(ok, what):
+    if not ok:
+        raise OosError(OOS_EINVAL, what)
+
+
+def _dense(t, dtype, shape, device, what):
+    """Address of a contiguous device tensor; None for None."""
+    if t is None:
+        return None
+    _require(t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous(), what)
+    return t.data_ptr()
+
+
+def _head_rows(t, dtype, n, heads, d, device, what):
+    """Address and token stride of rows [n, heads, d] whose heads are contiguous."""
+    _require(t.dtype is dtype and t.shape == (n, heads, d) and t.device == device, what)
+    s0, s1, s2 = t.stride()
+    _require((s2 == 1 or d == 1) and (s1 == d or heads == 1), what)
+    return t.data_ptr(), s0 if n > 1 else heads * d
+
+
+def _here(t, what):
+    """The device of `t`, which must be the current one: the library launches there."""
+    dev = t.device
+    _require(dev.type == "cuda" and dev.index == torch.cuda.current_device(), what)
+    return dev
+
+
+class PagedCache:
+    """One layer's pages: k and v device tensors [n_pages, page_size, nkv, d] plus the C view."""
+
+    def __init__(self, k, v):
+        _require(k.dim() == 4 and k.dtype in _DTYPES and k.is_contiguous() and k.device.type == "cuda", "PagedCache: k")
+        _require(v.dtype is k.dtype and v.shape == k.shape and v.is_contiguous() and v.device == k.device,
+                 "PagedCache: v")
+        self.k, self.v = k, v
+        self.device = k.device
+        n_pages, page_size, nkv, d = k.shape
+        self.c = OosPagedCache(_DTYPES[k.dtype], nkv, d, page_size, n_pages, k.data_ptr(), v.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def empty(n_pages, page_size, n_kv_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
+        k = torch.zeros(n_pages, page_size, n_kv_heads, head_dim, dtype=dtype, device=device)
+        return PagedCache(k, torch.zeros_like(k))
+
+
+class Batch:
+    """The ragged rows of one step: int32 device tensors q_start [B + 1], seq_len [B] and block_table
+    [B, max_pages], and the number of rows, plus the C view."""
+
+    def __init__(self, q_start, seq_len, block_table, n_tokens):
+        _require(block_table.dim() == 2, "Batch: block_table")
+        B, width = block_table.shape
+        dev = block_table.device
+        _require(dev.type == "cuda", "Batch: block_table")
+        self.device = dev
+        self.q_start, self.seq_len, self.block_table, self.n_tokens = q_start, seq_len, block_table, int(n_tokens)
+        i32 = torch.int32
+        self.c = OosBatch(B, self.n_tokens, width, _dense(q_start, i32, (B + 1,), dev, "Batch: q_start"),
+                          _dense(seq_len, i32, (B,), dev, "Batch: seq_len"),
+                          _dense(block_table, i32, (B, width), dev, "Batch: block_table"))
+        self.ref = ctypes.byref(self.c)
+
+
+def oos_qk_norm_rope(q, k, q_norm, k_norm, eps, rope, positions, q_out, k_out, stream=None):
+    """q [n, nq, d] and k [n, nkv, d] (either None), rows any stride apart; q_out / k_out may be q / k."""
+    x = q if q is not None else k
+    _require(x is not None and x.dim() == 3 and x.dtype in _DTYPES, "oos_qk_norm_rope: q, k")
+    dt, dev = x.dtype, _here(x, "oos_qk_norm_rope: device")
+    n, _, d = x.shape
+    args = []
+    heads = [0, 0]
+    outs = []
+    for i, (a, o, name) in enumerate(((q, q_out, "q"), (k, k_out, "k"))):
+        if a is None:
+            args += [None, 0]
+            outs += [None, 0]
+            continue
+        _require(a.dim() == 3 and o is not None, "oos_qk_norm_rope: " + name)
+        heads[i] = a.shape[1]
+        args += _head_rows(a, dt, n, heads[i], d, dev, "oos_qk_norm_rope: " + name)
+        outs += _head_rows(o, dt, n, heads[i], d, dev, "oos_qk_norm_rope: %s_out" % name)
+    _check(lib().oos_qk_norm_rope(_DTYPES[dt], n, heads[0], heads[1], d, *args,
+                                  _dense(q_norm, dt, (d,), dev, "oos_qk_norm_rope: q_norm"),
+                                  _dense(k_norm, dt, (d,), dev, "oos_qk_norm_rope: k_norm"), eps,
+                                  None if rope is None else ctypes.byref(rope),
+                                  _dense(positions, torch.int32, (n,), dev, "oos_qk_norm_rope: positions"), *outs,
+                                  _raw_stream(stream)), "oos_qk_norm_rope")
+
+
+def _raw_stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def oos_paged_append(cache, batch, k, v, k_norm, eps, rope, positions, out_status, stream=None):
+    """k, v: [batch.n_tokens, nkv, d] rows, any stride apart; positions: int32 [n_tokens]; out_status: int32 [1]."""
+    _require(k.dtype in _DTYPES, "oos_paged_append: k")
+    dt, dev, n = k.dtype, _here(k, "oos_paged_append: device"), batch.n_tokens
+    nkv, d = cache.c.n_kv_heads, cache.c.head_dim
+    _require(cache.device == dev and batch.device == dev, "oos_paged_append: device")
+    kp, ks = _head_rows(k, dt, n, nkv, d, dev, "oos_paged_append: k")
+    vp, vs = _head_rows(v, dt, n, nkv, d, dev, "oos_paged_append: v")
+    _check(lib().oos_paged_append(cache.ref, batch.ref, _DTYPES[dt], kp, ks, vp, vs,
+                                  _dense(k_norm, dt, (d,), dev, "oos_paged_append: k_norm"), eps,
+                                  None if rope is None else ctypes.byref(rope),
+                                  _dense(positions, torch.int32, (n,), dev, "oos_paged_append: positions"),
+                                  _dense(out_status, torch.int32, (1,), dev, "oos_paged_append: out_status"),
+                                  _raw_stream(stream)), "oos_paged_append")
+
+
+def oos_shared_prefix_attention_workspace_bytes(q, prefix_len, cache, batch):
+    return int(lib().oos_shared_prefix_attention_workspace_bytes(q.shape[1], prefix_len, cache.ref, batch.ref))
+
+
+def oos_shared_prefix_attention(q, prefix_k, prefix_v, prefix_len, cache, batch, tree_parent, scale, out, workspace,
+                                out_status, stream=None):
+    """q, out: [batch.n_tokens, nq, d] rows, any stride apart; prefix_k / prefix_v: one layer of a KVCache
+    ([capacity, nkv, d], capacity >= prefix_len; None with prefix_len 0); tree_parent: int32 [n_tokens] or None;
+    workspace: uint8; out_status: int32 [1]."""
+    name = "oos_shared_prefix_attention"
+    _require(q.dim() == 3 and q.dtype in _DTYPES, name + ": q")
+    dt, dev, n = q.dtype, _here(q, name + ": device"), batch.n_tokens
+    nkv, d = cache.c.n_kv_heads, cache.c.head_dim
+    _require(cache.device == dev and batch.device == dev and workspace.device == dev, name + ": device")
+    nq = q.shape[1]
+    qp, qs = _head_rows(q, dt, n, nq, d, dev, name + ": q")
+    op, os_ = _head_rows(out, dt, n, nq, d, dev, name + ": out")
+    pk = pv = None
+    if prefix_len > 0:
+        _require(prefix_k is not None and prefix_v is not None and prefix_k.dim() == 3, name + ": prefix_k, prefix_v")
+        shape = prefix_k.shape
+        _require(shape[0] >= prefix_len and shape[1] == nkv and shape[2] == d, name + ": prefix_k")
+        pk = _dense(prefix_k, cache.k.dtype, shape, dev, name + ": prefix_k")
+        pv = _dense(prefix_v, cache.k.dtype, shape, dev, name + ": prefix_v")
+    _require(workspace.is_contiguous(), name + ": workspace")
+    _check(lib().oos_shared_prefix_attention(_DTYPES[dt], nq, qp, qs, pk, pv, prefix_len, cache.ref, batch.ref,
+                                             _dense(tree_parent, torch.int32, (n,), dev, name + ": tree_parent"),
+                                             scale, op, os_, workspace.data_ptr(),
+                                             workspace.numel() * workspace.element_size(),
+                                             _dense(out_status, torch.int32, (1,), dev, name + ": out_status"),
+                                             _raw_stream(stream)), name)
 
 
 class VerifyOutputs:

@@ -1,0 +1,461 @@
+// Attention of a batch step over a shared prefix and each sequence's pages.
+//
+// Row (token i, q head h) of sequence b sees the prefix's keys and, of its own
+// sequence, the positions up to its own (or, with a tree, the committed ones and
+// its ancestors).  The keys fall into parts -- ranges of the prefix, ranges of the
+// sequence's positions -- and each part leaves an unnormalised row
+//   O = sum 2^(s - m) v,  m = max s,  l = sum 2^(s - m),  s = scale log2(e) q.k
+// in the workspace; a last kernel joins a row's parts.  In the prefix's parts the
+// rows of all sequences stand in one tile, so that its keys are read once for
+// all; in the sequence's parts a tile holds rows of one sequence.
+//
+// k_attn_rows: CUDA cores, fp32 products, for every type and head size.
+#include <math.h>
+
+#include <algorithm>
+
+#include "batch.cuh"
+
+namespace oos {
+
+constexpr int kRowKeys = 32;       // keys per tile
+constexpr int kRowThreads = 128;
+constexpr int kMaxParts = 32;      // parts of a row (a lane each in the join)
+constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
+
+struct BatchAttnArgs {
+  PagesView pages;
+  BatchView batch;
+  const void* q;
+  long long q_stride;
+  const uint8_t* pk;
+  const uint8_t* pv;
+  int prefix_len;
+  const int32_t* parent;
+  int nq, group;
+  float scale_log2;
+  void* out;
+  long long out_stride;
+  float* part_o;      // [part][token][head][d]
+  float2* part_ml;    // [part][token][head]
+  int p_tiles, p_splits, s_tiles, s_splits;
+  int32_t* status;
+};
+
+OOS_DEV float max_nan(float a, float b) {   // a NaN wins, so that it reaches the output
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Rows of a tile and the keys they may see
+struct TileRows {
+  int seq;            // -1: the prefix's keys
+  int q0;             // first token of the rows counted
+  long long r0;       // first row of the tile: token q0 + r / group, head r % group
+  int rows;           // rows of the tile
+  int n;              // rows of the sequence in this step
+  int first;          // its positions before them
+  int len;            // its positions
+};
+
+// Tile `i` of the sequences' tiles of `tile_rows` rows.  Sequence b's tiles start at
+// b + floor(q_start[b] group / tile_rows): a count known without a scan, at the price
+// of some numbers that no tile has.  The whole warp; false: no such tile.
+OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRows* t) {
+  const BatchView& b = a.batch;
+  auto start = [&](int s) { return s + (long long)b.q_start[s] * a.group / tile_rows; };
+  const int seq = warp_count_le(b.n_seqs - 1, start, i);
+  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = b.seq_len[seq];
+  const long long most = (long long)b.max_pages * a.pages.page_size;
+  bool ok = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1 && (!a.parent || q1 - q0 <= kMaxTreeRows);
+  if (!ok || len < q1 - q0 || len > most) {
+    if (threadIdx.x == 0) *a.status = ok || !a.parent ? OOS_EBATCH : OOS_ETREE;
+  }
+  if (!ok || i < start(seq)) return false;
+  t->seq = seq;
+  t->q0 = q0;
+  t->r0 = (i - start(seq)) * tile_rows;
+  t->rows = (int)max(0ll, min((long long)tile_rows, (long long)(q1 - q0) * a.group - t->r0));
+  t->n = q1 - q0;
+  t->first = len - t->n;
+  t->len = (int)min((long long)len, most);
+  return t->rows > 0;
+}
+
+// Ancestor sets of the sequence's rows, [row] -> 128 bits, itself included, by pointer
+// doubling in shared memory.  The whole block; n <= kMaxTreeRows.
+struct TreeScratch {
+  unsigned long long anc[2][kMaxTreeRows][2];
+  int up[2][kMaxTreeRows];
+};
+OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int n, TreeScratch* t))[2] {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    int p = a.parent[q0 + i];
+    if (p < -1 || p >= i) {
+      *a.status = OOS_ETREE;
+      p = -1;
+    }
+    t->up[0][i] = p;
+    t->anc[0][i][0] = i < 64 ? 1ull << i : 0ull;
+    t->anc[0][i][1] = i < 64 ? 0ull : 1ull << (i - 64);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (int step = 1; step < n; step *= 2, cur ^= 1) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+      const int p = t->up[cur][i];
+      t->anc[cur ^ 1][i][0] = t->anc[cur][i][0] | (p >= 0 ? t->anc[cur][p][0] : 0ull);
+      t->anc[cur ^ 1][i][1] = t->anc[cur][i][1] | (p >= 0 ? t->anc[cur][p][1] : 0ull);
+      t->up[cur ^ 1][i] = p >= 0 ? t->up[cur][p] : -1;
+    }
+    __syncthreads();
+  }
+  return t->anc[cur];
+}
+
+// RT rows x 32 keys per step, 128 threads: thread (r, c) of 16 x 8 has RT / 16 rows and
+// keys c, c + 8, c + 16, c + 24 of S, and four columns in 32 of O.  The eight threads of
+// a row share its statistics by shuffles.
+template <typename TQ, typename TK, int RT, int VEC>
+__global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a) {
+  extern __shared__ __align__(16) float sm[];
+  constexpr int RPT = RT / 16;
+  const int d = a.pages.d, ld = ((d + 3) & ~3) + 4, tid = threadIdx.x;
+  float* s_q = sm;                          // [RT][ld]
+  float* s_k = s_q + RT * ld;               // [32][ld]
+  float* s_v = s_k + kRowKeys * ld;
+  float* s_p = s_v + kRowKeys * ld;         // [RT][36]
+  constexpr int ldp = kRowKeys + 4;
+  __shared__ TreeScratch s_tree;
+  __shared__ long long s_at[kRowKeys];      // slot of each key in its buffer, -1: none
+
+  const int g = blockIdx.y;
+  const bool prefix = (int)blockIdx.x < a.p_tiles * a.p_splits;
+  const int local = prefix ? blockIdx.x : blockIdx.x - a.p_tiles * a.p_splits;
+  const int tile = prefix ? local / a.p_splits : local / a.s_splits;
+  const int split = prefix ? local % a.p_splits : local % a.s_splits;
+  const int splits = prefix ? a.p_splits : a.s_splits;
+  TileRows t;
+  if (prefix) {
+    t.seq = -1;
+    t.q0 = 0;
+    t.r0 = (long long)tile * RT;
+    t.rows = (int)min((long long)RT, (long long)a.batch.n_tokens * a.group - t.r0);
+    t.first = t.len = a.prefix_len;
+  } else if (!sequence_tile(a, tile, RT, &t)) {
+    return;
+  }
+  const unsigned long long (*anc)[2] = nullptr;
+  if (!prefix && a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
+  // the keys any row of the tile sees, dealt to the splits in whole tiles
+  const int last = (int)((t.r0 + t.rows - 1) / a.group);   // its last token, counted from q0
+  const int n_keys = prefix || anc ? t.len : max(0, min(t.len, t.first + last + 1));
+  const int n_tiles = (n_keys + kRowKeys - 1) / kRowKeys;
+  const int k0 = (int)((long long)n_tiles * split / splits) * kRowKeys;
+  const int k1 = min(n_keys, (int)((long long)n_tiles * (split + 1) / splits) * kRowKeys);
+
+  for (int i = tid; i < RT * (ld - 4); i += kRowThreads) {
+    const int r = i / (ld - 4), c = i % (ld - 4);
+    float v = 0.f;
+    if (r < t.rows && c < d) {
+      const long long row = t.r0 + r;
+      v = to_f32(((const TQ*)a.q)[(t.q0 + row / a.group) * a.q_stride + (g * a.group + row % a.group) * d + c]);
+    }
+    s_q[r * ld + c] = v;
+  }
+  const int tr = tid >> 3, tc = tid & 7;
+  float o[RPT][4][4], m[RPT], l[RPT];
+#pragma unroll
+  for (int r = 0; r < RPT; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[r][c][e] = 0.f;
+  }
+  const long long heads_d = (long long)a.pages.nkv * d;
+  for (int key0 = k0; key0 < k1; key0 += kRowKeys) {
+    __syncthreads();   // the tile before is read
+    if (tid < kRowKeys) {
+      const int key = key0 + tid;
+      long long at = -1;
+      if (key < k1) {
+        at = prefix ? key : page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
+        if (at < 0) *a.status = OOS_EBATCH;
+      }
+      s_at[tid] = at;
+    }
+    __syncthreads();
+    const TK* kb = (const TK*)(prefix ? a.pk : a.pages.k);
+    const TK* vb = (const TK*)(prefix ? a.pv : a.pages.v);
+    const int chunks = (ld - 4) / VEC;
+    for (int i = tid; i < kRowKeys * chunks; i += kRowThreads) {
+      const int key = i / chunks, c = (i % chunks) * VEC;
+      float kv[VEC], vv[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) kv[e] = vv[e] = 0.f;   // keys that are not there must not reach a sum
+      if (s_at[key] >= 0 && c < d) {
+        const long long off = s_at[key] * heads_d + (long long)g * d + c;
+        load_vec<TK, VEC>(kb + off, kv);
+        load_vec<TK, VEC>(vb + off, vv);
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        s_k[key * ld + c + e] = kv[e];
+        s_v[key * ld + c + e] = vv[e];
+      }
+    }
+    __syncthreads();
+    float s[RPT][4];
+#pragma unroll
+    for (int r = 0; r < RPT; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[r][j] = 0.f;
+    for (int c = 0; c < ld - 4; c += 4) {
+      float4 kk[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kk[j] = *reinterpret_cast<const float4*>(s_k + (tc + 8 * j) * ld + c);
+#pragma unroll
+      for (int r = 0; r < RPT; ++r) {
+        const float4 qq = *reinterpret_cast<const float4*>(s_q + (tr * RPT + r) * ld + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          s[r][j] += qq.x * kk[j].x + qq.y * kk[j].y + qq.z * kk[j].z + qq.w * kk[j].w;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RPT; ++r) {
+      const int token = (int)((t.r0 + tr * RPT + r) / a.group);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = key0 + tc + 8 * j, own = key - t.first;
+        bool see = s_at[tc + 8 * j] >= 0;
+        if (!prefix && own >= 0)
+          see = see && (anc ? token < t.n && own < kMaxTreeRows && ((anc[token][own >> 6] >> (own & 63)) & 1) : own <= token);
+        s[r][j] = see ? s[r][j] * a.scale_log2 : -INFINITY;
+        mx = max_nan(mx, s[r][j]);
+      }
+#pragma unroll
+      for (int x = 1; x < 8; x *= 2) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+      const float mn = max_nan(m[r], mx);
+      const bool live = mn != -INFINITY;
+      const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mn);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = live ? exp2f(s[r][j] - mn) : 0.f;
+        sum += p;
+        s_p[(tr * RPT + r) * ldp + tc + 8 * j] = p;
+      }
+#pragma unroll
+      for (int x = 1; x < 8; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      l[r] = l[r] * f + sum;
+      m[r] = mn;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[r][c][e] *= f;
+    }
+    __syncwarp();   // a row's weights are written and read by the same eight lanes
+#pragma unroll 2
+    for (int key = 0; key < kRowKeys; ++key) {
+      float p[RPT];
+#pragma unroll
+      for (int r = 0; r < RPT; ++r) p[r] = s_p[(tr * RPT + r) * ldp + key];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int col = tc * 4 + 32 * c;
+        if (col >= d) continue;
+        const float4 v = *reinterpret_cast<const float4*>(s_v + key * ld + col);
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+          o[r][c][0] += p[r] * v.x;
+          o[r][c][1] += p[r] * v.y;
+          o[r][c][2] += p[r] * v.z;
+          o[r][c][3] += p[r] * v.w;
+        }
+      }
+    }
+    __syncwarp();
+  }
+  const int part = prefix ? split : a.p_splits + split;
+  const long long n_rows = (long long)a.batch.n_tokens * a.nq;
+#pragma unroll
+  for (int r = 0; r < RPT; ++r) {
+    const int lr = tr * RPT + r;
+    if (lr >= t.rows) continue;
+    const long long row = t.r0 + lr;
+    const long long at = part * n_rows + (t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
+    if (tc == 0) a.part_ml[at] = make_float2(m[r], l[r]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int col = tc * 4 + 32 * c + e;
+        if (col < d) a.part_o[at * d + col] = o[r][c][e];
+      }
+  }
+}
+
+// A warp per row adds its parts up: weights 2^(m - max m), the sum divided by the
+// weighted l.  Parts are taken in order, so the result does not depend on timing.
+template <typename T>
+__global__ void __launch_bounds__(128) k_attn_join(const BatchAttnArgs a) {
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, d = a.pages.d;
+  const long long n_rows = (long long)a.batch.n_tokens * a.nq;
+  if (row >= n_rows) return;
+  const long long token = row / a.nq;
+  if (token >= a.batch.q_start[a.batch.n_seqs] || token < a.batch.q_start[0]) return;   // padding
+  const int parts = a.p_splits + a.s_splits;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < parts) ml = a.part_ml[lane * n_rows + row];
+  const float M = warp_max(ml.x);
+  const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+  const float den = warp_sum(ml.x == -INFINITY ? 0.f : w * ml.y);
+  T* out = (T*)a.out + token * a.out_stride + (row - token * a.nq) * d;
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; ++p) {
+    const float wp = __shfl_sync(0xffffffffu, w, p);
+    if (wp == 0.f) continue;   // a part without keys leaves its row unwritten
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (lane + 32 * c < d) acc[c] += wp * a.part_o[(p * n_rows + row) * d + lane + 32 * c];
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    if (lane + 32 * c < d) out[lane + 32 * c] = from_f32<T>(den == 0.f ? 0.f : acc[c] / den);
+}
+
+// ---- host: how a call is cut up
+struct BatchAttnPlan {
+  int rt, p_tiles, p_splits, s_tiles, s_splits;
+  size_t ml_off, bytes;
+};
+
+static int device_sms() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  return n;
+}
+
+static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, const oos_batch& b, BatchAttnPlan* p) {
+  const int sms = device_sms();
+  if (sms <= 0) return false;
+  const int G = nq / c.n_kv_heads;
+  const long long rows = (long long)b.n_tokens * G;
+  p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
+  p->p_tiles = prefix_len > 0 ? (int)((rows + p->rt - 1) / p->rt) : 0;
+  p->s_tiles = (int)(b.n_seqs + rows / p->rt);
+  // enough blocks for four per SM, each with eight tiles of keys at least
+  auto splits = [&](long long tiles, long long keys) {
+    const long long want = tiles > 0 ? 4ll * sms / (tiles * c.n_kv_heads) : 1;
+    return (int)std::max(1ll, std::min({want, keys / (8 * kRowKeys), (long long)kMaxParts / 2}));
+  };
+  p->p_splits = prefix_len > 0 ? splits(p->p_tiles, prefix_len) : 0;
+  p->s_splits = splits(p->s_tiles, std::min<long long>((long long)b.max_pages * c.page_size, 1ll << 31));
+  const size_t n = (size_t)(p->p_splits + p->s_splits) * b.n_tokens * nq;
+  p->ml_off = (n * c.head_dim * 4 + 255) / 256 * 256;
+  p->bytes = p->ml_off + (n * 8 + 255) / 256 * 256;
+  return true;
+}
+
+template <typename TQ, typename TK, int RT, int VEC>
+static cudaError_t launch_rows(const BatchAttnArgs& a, int blocks, cudaStream_t st) {
+  const int ld = ((a.pages.d + 3) & ~3) + 4;
+  const size_t smem = ((RT + 2 * kRowKeys) * ld + RT * (kRowKeys + 4)) * 4;
+  cudaError_t e = cudaFuncSetAttribute(k_attn_rows<TQ, TK, RT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  e = launch(false, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)a.batch.n_tokens * a.nq;
+  return launch(false, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);
+}
+
+template <typename TQ, typename TK>
+static cudaError_t launch_batch_attn(const BatchAttnArgs& a, const BatchAttnPlan& p, cudaStream_t st) {
+  const int blocks = a.p_tiles * a.p_splits + a.s_tiles * a.s_splits;
+  // rows of whole aligned 4-element groups, else one element at a time
+  const uintptr_t any = (uintptr_t)a.pages.k | (uintptr_t)a.pages.v | (uintptr_t)a.pk | (uintptr_t)a.pv;
+  const bool vec = a.pages.d % 4 == 0 && any % (4 * sizeof(TK)) == 0;
+  if (p.rt == 16) return vec ? launch_rows<TQ, TK, 16, 4>(a, blocks, st) : launch_rows<TQ, TK, 16, 1>(a, blocks, st);
+  return vec ? launch_rows<TQ, TK, 64, 4>(a, blocks, st) : launch_rows<TQ, TK, 64, 1>(a, blocks, st);
+}
+
+static bool attn_shape_ok(int nq, int prefix_len, const oos_paged_cache* c, const oos_batch* b) {
+  if (!c || !b || nq < 1 || prefix_len < 0 || c->n_kv_heads < 1 || c->page_size < 1 || c->n_pages < 1) return false;
+  if (nq % c->n_kv_heads || c->n_kv_heads > 65535 || b->n_seqs < 1 || b->n_tokens < 0 || b->max_pages < 1) return false;
+  return (long long)b->n_tokens * nq + b->n_seqs < (1ll << 31) / kMaxParts && nq <= (1 << 20);
+}
+
+}  // namespace oos
+
+using namespace oos;
+
+extern "C" {
+
+size_t oos_shared_prefix_attention_workspace_bytes(int32_t n_q_heads, int32_t prefix_len, const oos_paged_cache* cache,
+                                                   const oos_batch* batch) {
+  if (!attn_shape_ok(n_q_heads, prefix_len, cache, batch)) return 0;
+  if (!dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return 0;
+  BatchAttnPlan p;
+  return plan_batch_attn(n_q_heads, prefix_len, *cache, *batch, &p) ? std::max<size_t>(p.bytes, 256) : 0;
+}
+
+int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q, int64_t q_stride,
+                                const void* prefix_k, const void* prefix_v, int32_t prefix_len,
+                                const oos_paged_cache* cache, const oos_batch* batch, const int32_t* tree_parent,
+                                float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                                int32_t* out_status, void* stream) {
+  if (!attn_shape_ok(n_q_heads, prefix_len, cache, batch) || !pages_ok(cache) || !batch_ok(batch) || !out_status)
+    return OOS_EINVAL;
+  if (!(scale > 0.f) || !(scale < INFINITY)) return OOS_EINVAL;
+  if (!dtype_ok(dtype) || !dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return OOS_EUNSUPPORTED;
+  if (dtype != cache->dtype && !(dtype == OOS_DTYPE_BF16 && cache->dtype == OOS_DTYPE_F16)) return OOS_EUNSUPPORTED;
+  if (prefix_len > 0 && (!prefix_k || !prefix_v)) return OOS_EINVAL;
+  if (cache->dtype != OOS_DTYPE_F32) {
+    const uintptr_t any = (uintptr_t)cache->k | (uintptr_t)cache->v |
+                          (prefix_len > 0 ? (uintptr_t)prefix_k | (uintptr_t)prefix_v : 0);
+    if (any & 15) return OOS_EINVAL;
+  }
+  if (batch->n_tokens == 0) return OOS_OK;
+  const long long w = (long long)n_q_heads * cache->head_dim;
+  if (!q || !out || q_stride < w || out_stride < w) return OOS_EINVAL;
+  BatchAttnPlan p;
+  if (!plan_batch_attn(n_q_heads, prefix_len, *cache, *batch, &p)) return OOS_ECUDA;
+  if (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < p.bytes) return OOS_EWORKSPACE;
+  BatchAttnArgs a = {};
+  a.pages = view_of(*cache);
+  a.batch = view_of(*batch);
+  a.q = q;
+  a.q_stride = q_stride;
+  a.pk = prefix_len > 0 ? (const uint8_t*)prefix_k : nullptr;
+  a.pv = prefix_len > 0 ? (const uint8_t*)prefix_v : nullptr;
+  a.prefix_len = prefix_len;
+  a.parent = tree_parent;
+  a.nq = n_q_heads;
+  a.group = n_q_heads / cache->n_kv_heads;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.out = out;
+  a.out_stride = out_stride;
+  a.part_o = (float*)workspace;
+  a.part_ml = (float2*)((uint8_t*)workspace + p.ml_off);
+  a.p_tiles = p.p_tiles;
+  a.p_splits = p.p_splits;
+  a.s_tiles = p.s_tiles;
+  a.s_splits = p.s_splits;
+  a.status = out_status;
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e;
+  if (dtype == OOS_DTYPE_F32) e = launch_batch_attn<float, float>(a, p, st);
+  else if (cache->dtype == OOS_DTYPE_BF16) e = launch_batch_attn<__nv_bfloat16, __nv_bfloat16>(a, p, st);
+  else if (dtype == OOS_DTYPE_BF16) e = launch_batch_attn<__nv_bfloat16, __half>(a, p, st);
+  else e = launch_batch_attn<__half, __half>(a, p, st);
+  return e == cudaSuccess ? OOS_OK : OOS_ECUDA;
+}
+
+}  // extern "C"

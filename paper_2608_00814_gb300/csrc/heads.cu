@@ -1,0 +1,332 @@
+// Per-head operators of a batch step: RMSNorm of q and k heads with the position
+// rotation in the same pass, and the append of K (normed and turned on the way)
+// and V to pages.
+//
+// One head x of d values becomes y = x * rsqrt(mean(x^2) + eps) * gain, and the
+// pair (y_m, y_{m+d/2}) turns by a_m = position * rate_m.  Both are one pass over
+// memory: a few lanes hold a head, each of them chunks of VEC values of the first
+// half and the same chunks of the second, so that every pair is in one lane, the
+// norm is a few shuffles and nothing goes through shared memory.  Bound by HBM.
+//
+// Angles: rate_m / 2 pi is kept as a 64-bit fraction of a turn; times the position
+// modulo 2^64 it is the angle's fraction of a turn to 2^-33 at position 2^31 (the
+// rate's own rounding to 53 bits), by integer products alone.  The nearest
+// quarter turn comes off exactly, so the fp32 sine and cosine see at most an
+// eighth of a turn.  A warp forms them once per token and keeps them over its
+// heads: at a warp per head they were the kernel's largest cost.
+#include <math.h>
+
+#include <algorithm>
+
+#include "batch.cuh"
+
+namespace oos {
+
+constexpr int kHeadWarps = 4;   // warps per block
+
+struct HeadArgs {
+  int n, d, d2, lanes;            // tokens, head size and half of it, lanes per head (a power of two)
+  int heads[2];                   // q and k heads (append: 0 and the K heads)
+  int slices;                     // warps that share a token's heads
+  const void* in[2];
+  long long in_stride[2];         // elements
+  const void* gain[2];
+  void* out[2];
+  long long out_stride[2];
+  const int32_t* positions;       // nullptr: no rotation
+  float eps;
+  // append
+  const void* v;
+  long long v_stride;
+  PagesView pages;
+  BatchView batch;
+  int32_t* status;
+};
+
+// cos and sin of pos * rate, the rate in units of 2^-64 turns
+OOS_DEV void turn(unsigned long long rate, int pos, float& c, float& s) {
+  const unsigned long long t = (unsigned long long)(long long)pos * rate;
+  const unsigned long long quarter = (t + (1ull << 61)) >> 62;
+  const float x = (float)(long long)(t - (quarter << 62)) * 0x1p-63f;   // in half turns, |x| <= 1/4
+  float sn, cs;
+  sincospif(x, &sn, &cs);
+  const float a = quarter & 1 ? sn : cs, b = quarter & 1 ? cs : sn;
+  c = (quarter + 1) & 2 ? -a : a;
+  s = quarter & 2 ? -b : b;
+}
+
+// T: elements of the inputs and gains, O: of the outputs.  VEC: values per access.
+// NC: chunks of half a head per lane.  APPEND: in[1] goes to the pages' K, v to
+// their V.
+template <typename T, typename O, int VEC, int NC, bool APPEND>
+__global__ void __launch_bounds__(kHeadWarps * 32) k_heads(const HeadArgs a, const __grid_constant__ RopeTurns rope) {
+  const long long w = (long long)blockIdx.x * kHeadWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const int t = (int)(w / a.slices), slice = (int)(w % a.slices);
+  if (t >= a.n) return;
+  // where an appended row goes (the whole warp; a row without a place is left out)
+  long long slot = 0;
+  if (APPEND) {
+    const BatchView& b = a.batch;
+    const int seq = warp_count_le(b.n_seqs, [&](int i) { return (long long)b.q_start[i]; }, t);
+    if (seq >= b.n_seqs) return;                       // behind the last sequence
+    const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1];
+    slot = t < q0 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, b.seq_len[seq] - (q1 - t));
+    if (slot < 0) {
+      if (lane == 0) *a.status = OOS_EBATCH;
+      return;
+    }
+  }
+  const int sub = lane & (a.lanes - 1), group = lane / a.lanes, groups = 32 / a.lanes;
+  float cs[NC][VEC], sn[NC][VEC];
+  if (a.positions) {
+    const int pos = a.positions[t];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int m = (c * a.lanes + sub) * VEC + i;
+        if (m < a.d2) turn(rope.f[m], pos, cs[c][i], sn[c][i]);
+      }
+  }
+  // heads [h0, h1) of this warp, counted over q's and k's
+  const int total = a.heads[0] + a.heads[1];
+  const int h0 = (int)((long long)total * slice / a.slices), h1 = (int)((long long)total * (slice + 1) / a.slices);
+#pragma unroll 1
+  for (int side = APPEND ? 1 : 0; side < 2; ++side) {
+    const int lo = max(0, h0 - (side ? a.heads[0] : 0)), hi = min(a.heads[side], h1 - (side ? a.heads[0] : 0));
+    const T* in = (const T*)a.in[side] + (long long)t * a.in_stride[side];
+    O* out = APPEND ? (O*)a.pages.k + slot * a.pages.nkv * a.d : (O*)a.out[side] + (long long)t * a.out_stride[side];
+    const T* gain = (const T*)a.gain[side];
+    float g[NC][2][VEC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int m = (c * a.lanes + sub) * VEC;
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) g[c][half][i] = gain && m < a.d2 ? to_f32(gain[half * a.d2 + m + i]) : 1.f;
+    }
+    constexpr int U = NC * VEC > 8 ? 1 : 2;   // heads in flight per lane
+#pragma unroll 1
+    for (int h = lo; h < hi; h += U * groups) {
+      float x[U][NC][2][VEC];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int hh = h + u * groups + group, m = (c * a.lanes + sub) * VEC;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if (hh < hi && m < a.d2) load_vec<T, VEC>(in + (long long)hh * a.d + half * a.d2 + m, x[u][c][half]);
+            else
+#pragma unroll
+              for (int i = 0; i < VEC; ++i) x[u][c][half][i] = 0.f;
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (gain) {
+          float ss = 0.f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) ss += x[u][c][0][i] * x[u][c][0][i] + x[u][c][1][i] * x[u][c][1][i];
+          for (int o = a.lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          const float r = rsqrtf(ss / (float)a.d + a.eps);
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int i = 0; i < VEC; ++i) x[u][c][half][i] = x[u][c][half][i] * r * g[c][half][i];
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int hh = h + u * groups + group, m = (c * a.lanes + sub) * VEC;
+          if (a.positions) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+              const float lo_ = x[u][c][0][i], hi_ = x[u][c][1][i];
+              x[u][c][0][i] = lo_ * cs[c][i] - hi_ * sn[c][i];
+              x[u][c][1][i] = hi_ * cs[c][i] + lo_ * sn[c][i];
+            }
+          }
+          if (hh < hi && m < a.d2) {
+            store_vec<O, VEC>(out + (long long)hh * a.d + m, x[u][c][0]);
+            store_vec<O, VEC>(out + (long long)hh * a.d + a.d2 + m, x[u][c][1]);
+          }
+        }
+      }
+    }
+    if (APPEND) {   // the same heads of V
+      const T* vin = (const T*)a.v + (long long)t * a.v_stride;
+      O* vout = (O*)a.pages.v + slot * a.pages.nkv * a.d;
+      const int chunks = (hi - lo) * a.d / VEC;
+#pragma unroll 4
+      for (int i = lane; i < chunks; i += 32) {
+        float x[VEC];
+        load_vec<T, VEC>(vin + (long long)lo * a.d + i * VEC, x);
+        store_vec<O, VEC>(vout + (long long)lo * a.d + i * VEC, x);
+      }
+    }
+  }
+}
+
+bool rope_ok(const oos_rope_config* r) {
+  if (!(r->theta > 0.f) || !(r->theta < INFINITY) || !(r->factor == r->factor)) return false;
+  return r->factor <= 1.f || (r->low_freq_factor > 0.f && r->high_freq_factor > r->low_freq_factor && r->orig_max_pos >= 1);
+}
+
+void rope_turns(const oos_rope_config& r, int d, RopeTurns* out) {
+  for (int m = 0; m < kMaxHeadDim / 2; ++m) {
+    out->f[m] = 0;
+    if (m >= d / 2) continue;
+    const double f = rope_rate(r.theta, m, d, r.factor, r.low_freq_factor, r.high_freq_factor, r.orig_max_pos);
+    const double t = f / (2.0 * M_PI);
+    out->f[m] = (unsigned long long)ldexp(t - floor(t), 64);   // t - floor(t) <= 1 - 2^-53
+  }
+}
+
+bool pages_ok(const oos_paged_cache* c) {
+  return c->n_kv_heads >= 1 && c->page_size >= 1 && c->n_pages >= 1 && c->k && c->v;
+}
+bool batch_ok(const oos_batch* b) {
+  return b->n_seqs >= 1 && b->n_tokens >= 0 && b->max_pages >= 1 && b->q_start && b->seq_len && b->block_table;
+}
+
+// Rows of the widest access: 16 bytes of T (and the same count of O) where half a
+// head divides into them and every row starts on such a boundary, else one element.
+static bool wide(const HeadArgs& a, int es, int vec, int out_es) {
+  if (a.d2 % vec) return false;
+  auto rows = [&](const void* p, long long stride, int es_) {
+    return ((uintptr_t)p % (vec * es_)) == 0 && (stride * es_) % (vec * es_) == 0;
+  };
+  bool ok = true;
+  for (int s = 0; s < 2; ++s) {
+    if (a.heads[s] && a.in[s]) ok = ok && rows(a.in[s], a.in_stride[s], es);
+    if (a.heads[s] && a.out[s]) ok = ok && rows(a.out[s], a.out_stride[s], out_es);
+  }
+  if (a.v) ok = ok && rows(a.v, a.v_stride, es) && rows(a.pages.k, 0, out_es) && rows(a.pages.v, 0, out_es);
+  return ok;
+}
+
+static int pow2_at_least(int x) {
+  int p = 1;
+  while (p < x) p *= 2;
+  return p;
+}
+
+template <typename T, typename O, bool APPEND>
+static cudaError_t launch_heads(HeadArgs& a, const RopeTurns& rope, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool w = wide(a, sizeof(T), V, sizeof(O));
+  const int chunks = w ? a.d2 / V : a.d2;
+  a.lanes = std::min(32, pow2_at_least(chunks));
+  const bool two = chunks > a.lanes;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  // A token's heads go to as many warps as it takes to give every SM 16, so that a
+  // few tokens are spread out while many share the angles over all their heads.
+  const int total = a.heads[0] + a.heads[1], per_warp = 32 / a.lanes;
+  const int most = (total + per_warp - 1) / per_warp;
+  a.slices = (int)std::max(1ll, std::min<long long>(most, 16ll * sms / a.n));
+  const long long warps = (long long)a.n * a.slices;
+  const dim3 grid((unsigned)((warps + kHeadWarps - 1) / kHeadWarps)), block(kHeadWarps * 32);
+  if (w && two) return cudaErrorInvalidValue;   // 64 values are at most 16 chunks of 4
+  if (w) return launch(false, k_heads<T, O, V, 1, APPEND>, grid, block, 0, st, a, rope);
+  if (two) return launch(false, k_heads<T, O, 1, 2, APPEND>, grid, block, 0, st, a, rope);
+  return launch(false, k_heads<T, O, 1, 1, APPEND>, grid, block, 0, st, a, rope);
+}
+
+template <typename T>
+static cudaError_t launch_append(int out_dtype, HeadArgs& a, const RopeTurns& rope, cudaStream_t st) {
+  if (out_dtype == OOS_DTYPE_F32) return launch_heads<T, float, true>(a, rope, st);
+  if (out_dtype == OOS_DTYPE_BF16) return launch_heads<T, __nv_bfloat16, true>(a, rope, st);
+  return launch_heads<T, __half, true>(a, rope, st);
+}
+
+}  // namespace oos
+
+using namespace oos;
+
+extern "C" {
+
+int oos_qk_norm_rope(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* q,
+                     int64_t q_stride, const void* k, int64_t k_stride, const void* q_norm, const void* k_norm,
+                     float eps, const oos_rope_config* rope, const int32_t* positions, void* q_out,
+                     int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream) {
+  if (n < 0 || n_q_heads < 0 || n_kv_heads < 0 || n_q_heads + (long long)n_kv_heads < 1 ||
+      n_q_heads + (long long)n_kv_heads > (1 << 20) || !(eps >= 0.f))
+    return OOS_EINVAL;
+  if (!dtype_ok(dtype) || !head_dim_ok(head_dim)) return OOS_EUNSUPPORTED;
+  if (rope && !rope_ok(rope)) return OOS_EINVAL;
+  if (n == 0) return OOS_OK;
+  const long long qw = (long long)n_q_heads * head_dim, kw = (long long)n_kv_heads * head_dim;
+  if (n_q_heads && (!q || !q_out || q_stride < qw || q_out_stride < qw)) return OOS_EINVAL;
+  if (n_kv_heads && (!k || !k_out || k_stride < kw || k_out_stride < kw)) return OOS_EINVAL;
+  if (rope && !positions) return OOS_EINVAL;
+  HeadArgs a = {};
+  a.n = n;
+  a.d = head_dim;
+  a.d2 = head_dim / 2;
+  a.heads[0] = n_q_heads;
+  a.heads[1] = n_kv_heads;
+  a.in[0] = q;
+  a.in[1] = k;
+  a.in_stride[0] = q_stride;
+  a.in_stride[1] = k_stride;
+  a.gain[0] = q_norm;
+  a.gain[1] = k_norm;
+  a.out[0] = q_out;
+  a.out[1] = k_out;
+  a.out_stride[0] = q_out_stride;
+  a.out_stride[1] = k_out_stride;
+  a.positions = rope ? positions : nullptr;
+  a.eps = eps;
+  RopeTurns turns = {};
+  if (rope) rope_turns(*rope, head_dim, &turns);
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = dtype == OOS_DTYPE_F32    ? launch_heads<float, float, false>(a, turns, st)
+                        : dtype == OOS_DTYPE_BF16 ? launch_heads<__nv_bfloat16, __nv_bfloat16, false>(a, turns, st)
+                                                  : launch_heads<__half, __half, false>(a, turns, st);
+  return e == cudaSuccess ? OOS_OK : OOS_ECUDA;
+}
+
+int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32_t dtype, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, const void* k_norm, float eps,
+                     const oos_rope_config* rope, const int32_t* positions, int32_t* out_status, void* stream) {
+  if (!cache || !batch || !pages_ok(cache) || !batch_ok(batch) || !out_status || !(eps >= 0.f)) return OOS_EINVAL;
+  if (!dtype_ok(dtype) || !dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return OOS_EUNSUPPORTED;
+  if (rope && !rope_ok(rope)) return OOS_EINVAL;
+  if (batch->n_tokens == 0) return OOS_OK;
+  const long long w = (long long)cache->n_kv_heads * cache->head_dim;
+  if (!k || !v || k_stride < w || v_stride < w || w > (1 << 24)) return OOS_EINVAL;
+  if (rope && !positions) return OOS_EINVAL;
+  HeadArgs a = {};
+  a.n = batch->n_tokens;
+  a.d = cache->head_dim;
+  a.d2 = cache->head_dim / 2;
+  a.heads[1] = cache->n_kv_heads;
+  a.in[1] = k;
+  a.in_stride[1] = k_stride;
+  a.gain[1] = k_norm;
+  a.v = v;
+  a.v_stride = v_stride;
+  a.positions = rope ? positions : nullptr;
+  a.eps = eps;
+  a.pages = view_of(*cache);
+  a.batch = view_of(*batch);
+  a.status = out_status;
+  RopeTurns turns = {};
+  if (rope) rope_turns(*rope, cache->head_dim, &turns);
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = dtype == OOS_DTYPE_F32    ? launch_append<float>(cache->dtype, a, turns, st)
+                        : dtype == OOS_DTYPE_BF16 ? launch_append<__nv_bfloat16>(cache->dtype, a, turns, st)
+                                                  : launch_append<__half>(cache->dtype, a, turns, st);
+  return e == cudaSuccess ? OOS_OK : OOS_ECUDA;
+}
+
+}  // extern "C"

@@ -131,6 +131,10 @@ struct Model {
 
 size_t carve_workspace(const oos_model_config& c, int n_sms, uint8_t* base, Workspace* ws);
 
+// rotation rate of the pair (m, m + d/2), radians per position; F, lo, hi, L: the
+// rescaling's factor, low and high frequency factors and original context
+double rope_rate(float theta, int m, int d, double F, double lo, double hi, double L);
+
 // launch with or without programmatic dependent launch (PDL)
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch(bool pdl, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,

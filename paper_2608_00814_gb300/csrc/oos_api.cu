@@ -76,22 +76,17 @@ size_t carve_workspace(const oos_model_config& c, int n_sms, uint8_t* base, Work
   return align_up(off, 256);
 }
 
-// Llama-3.1 rotary frequency rescaling of the pair rates theta^(-2m/d) (see
-// oos_model_config): pairs of short wavelength keep their rate, long ones turn
-// rope_factor times slower, the band between blends the two.
-static void rope_rescale(std::vector<double>& inv, const oos_model_config& c) {
-  const double F = c.rope_factor, lo = c.rope_low_freq_factor, hi = c.rope_high_freq_factor;
-  const double L = (double)c.rope_orig_max_pos;
-  for (double& f : inv) {
-    const double wavelen = 2.0 * M_PI / f;
-    if (wavelen < L / hi) continue;
-    if (wavelen > L / lo) {
-      f = f / F;
-    } else {
-      const double w = (L / wavelen - lo) / (hi - lo);
-      f = (1.0 - w) * f / F + w * f;
-    }
-  }
+// Rate of pair m, with the Llama-3.1 rotary frequency rescaling (see oos_model_config)
+// where F > 1: pairs of short wavelength keep their rate, long ones turn F times
+// slower, the band between blends the two.
+double rope_rate(float theta, int m, int d, double F, double lo, double hi, double L) {
+  const double f = pow((double)theta, -2.0 * m / (double)d);
+  if (!(F > 1.0)) return f;
+  const double wavelen = 2.0 * M_PI / f;
+  if (wavelen < L / hi) return f;
+  if (wavelen > L / lo) return f / F;
+  const double w = (L / wavelen - lo) / (hi - lo);
+  return (1.0 - w) * f / F + w * f;
 }
 
 static bool config_ok(const oos_model_config* c) {
@@ -353,8 +348,9 @@ int oos_model_create(const oos_model_config* cfg, const oos_weights* w, void* wo
       break;
     }
     std::vector<double> inv(c.head_dim / 2);
-    for (int j = 0; j < c.head_dim / 2; ++j) inv[j] = pow((double)c.rope_theta, -2.0 * j / (double)c.head_dim);
-    if (c.rope_factor > 1.f) rope_rescale(inv, c);
+    for (int j = 0; j < c.head_dim / 2; ++j)
+      inv[j] = rope_rate(c.rope_theta, j, c.head_dim, c.rope_factor, c.rope_low_freq_factor, c.rope_high_freq_factor,
+                         c.rope_orig_max_pos);
     if (cudaMemcpy(m->ws.inv_freq, inv.data(), inv.size() * 8, cudaMemcpyHostToDevice) != cudaSuccess) {
       rc = OOS_ECUDA;
       break;
@@ -575,6 +571,7 @@ const char* oos_status_string(int code) {
     case OOS_ETIMEOUT: return "device pipeline wait exceeded its limit";
     case OOS_EUNSUPPORTED: return "model shape not supported by the kernels";
     case OOS_EWORKSPACE: return "workspace missing, misaligned or too small";
+    case OOS_EBATCH: return "batch offsets, a length or a page out of range";
     default: return "unknown status";
   }
 }
