@@ -9,110 +9,20 @@
 // rows of all sequences stand in one tile, so that its keys are read once for
 // all; in the sequence's parts a tile holds rows of one sequence.
 //
-// k_attn_rows: CUDA cores, fp32 products, for every type and head size.
+// k_attn_rows: CUDA cores, fp32 products, for every type and head size.  The 16-bit
+// types with heads of 128 take the tensor-core kernels of batch_prefix.cu and
+// batch_pages.cu.
 #include <math.h>
 
 #include <algorithm>
 
-#include "batch.cuh"
+#include "batch_attn.cuh"
 
 namespace oos {
 
 constexpr int kRowKeys = 32;       // keys per tile
 constexpr int kRowThreads = 128;
 constexpr int kMaxParts = 32;      // parts of a row (a lane each in the join)
-constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
-
-struct BatchAttnArgs {
-  PagesView pages;
-  BatchView batch;
-  const void* q;
-  long long q_stride;
-  const uint8_t* pk;
-  const uint8_t* pv;
-  int prefix_len;
-  const int32_t* parent;
-  int nq, group;
-  float scale_log2;
-  void* out;
-  long long out_stride;
-  float* part_o;      // [part][token][head][d]
-  float2* part_ml;    // [part][token][head]
-  int p_tiles, p_splits, s_tiles, s_splits;
-  int32_t* status;
-};
-
-OOS_DEV float max_nan(float a, float b) {   // a NaN wins, so that it reaches the output
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-
-// Rows of a tile and the keys they may see
-struct TileRows {
-  int seq;            // -1: the prefix's keys
-  int q0;             // first token of the rows counted
-  long long r0;       // first row of the tile: token q0 + r / group, head r % group
-  int rows;           // rows of the tile
-  int n;              // rows of the sequence in this step
-  int first;          // its positions before them
-  int len;            // its positions
-};
-
-// Tile `i` of the sequences' tiles of `tile_rows` rows.  Sequence b's tiles start at
-// b + floor(q_start[b] group / tile_rows): a count known without a scan, at the price
-// of some numbers that no tile has.  The whole warp; false: no such tile.
-OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRows* t) {
-  const BatchView& b = a.batch;
-  auto start = [&](int s) { return s + (long long)b.q_start[s] * a.group / tile_rows; };
-  const int seq = warp_count_le(b.n_seqs - 1, start, i);
-  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = b.seq_len[seq];
-  const long long most = (long long)b.max_pages * a.pages.page_size;
-  bool ok = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1 && (!a.parent || q1 - q0 <= kMaxTreeRows);
-  if (!ok || len < q1 - q0 || len > most) {
-    if (threadIdx.x == 0) *a.status = ok || !a.parent ? OOS_EBATCH : OOS_ETREE;
-  }
-  if (!ok || i < start(seq)) return false;
-  t->seq = seq;
-  t->q0 = q0;
-  t->r0 = (i - start(seq)) * tile_rows;
-  t->rows = (int)max(0ll, min((long long)tile_rows, (long long)(q1 - q0) * a.group - t->r0));
-  t->n = q1 - q0;
-  t->first = len - t->n;
-  t->len = (int)min((long long)len, most);
-  return t->rows > 0;
-}
-
-// Ancestor sets of the sequence's rows, [row] -> 128 bits, itself included, by pointer
-// doubling in shared memory.  The whole block; n <= kMaxTreeRows.
-struct TreeScratch {
-  unsigned long long anc[2][kMaxTreeRows][2];
-  int up[2][kMaxTreeRows];
-};
-OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int n, TreeScratch* t))[2] {
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    int p = a.parent[q0 + i];
-    if (p < -1 || p >= i) {
-      *a.status = OOS_ETREE;
-      p = -1;
-    }
-    t->up[0][i] = p;
-    t->anc[0][i][0] = i < 64 ? 1ull << i : 0ull;
-    t->anc[0][i][1] = i < 64 ? 0ull : 1ull << (i - 64);
-  }
-  __syncthreads();
-  int cur = 0;
-  for (int step = 1; step < n; step *= 2, cur ^= 1) {
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-      const int p = t->up[cur][i];
-      t->anc[cur ^ 1][i][0] = t->anc[cur][i][0] | (p >= 0 ? t->anc[cur][p][0] : 0ull);
-      t->anc[cur ^ 1][i][1] = t->anc[cur][i][1] | (p >= 0 ? t->anc[cur][p][1] : 0ull);
-      t->up[cur ^ 1][i] = p >= 0 ? t->up[cur][p] : -1;
-    }
-    __syncthreads();
-  }
-  return t->anc[cur];
-}
 
 // RT rows x 32 keys per step, 128 threads: thread (r, c) of 16 x 8 has RT / 16 rows and
 // keys c, c + 8, c + 16, c + 24 of S, and four columns in 32 of O.  The eight threads of
@@ -332,7 +242,10 @@ __global__ void __launch_bounds__(128) k_attn_join(const BatchAttnArgs a) {
 
 // ---- host: how a call is cut up
 struct BatchAttnPlan {
-  int rt, p_tiles, p_splits, s_tiles, s_splits;
+  bool tc;             // tensor cores: 16-bit types with heads of 128
+  PrefixPlan prefix;
+  PagesPlan pages;
+  int rt, p_tiles, p_splits, s_tiles, s_splits;   // CUDA cores
   size_t ml_off, bytes;
 };
 
@@ -348,6 +261,16 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   if (sms <= 0) return false;
   const int G = nq / c.n_kv_heads;
   const long long rows = (long long)b.n_tokens * G;
+  const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, 1ll << 31);
+  p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
+  if (p->tc) {
+    if (rows > 0 && prefix_len > 0 && !plan_prefix_tc(rows, c.n_kv_heads, prefix_len, &p->prefix)) return false;
+    p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
+    const size_t n = prefix_len > 0 ? (size_t)b.n_tokens * nq : 0;
+    p->ml_off = n * 128 * 4;
+    p->bytes = p->ml_off + (n * 8 + 255) / 256 * 256;
+    return true;
+  }
   p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
   p->p_tiles = prefix_len > 0 ? (int)((rows + p->rt - 1) / p->rt) : 0;
   p->s_tiles = (int)(b.n_seqs + rows / p->rt);
@@ -357,7 +280,7 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     return (int)std::max(1ll, std::min({want, keys / (8 * kRowKeys), (long long)kMaxParts / 2}));
   };
   p->p_splits = prefix_len > 0 ? splits(p->p_tiles, prefix_len) : 0;
-  p->s_splits = splits(p->s_tiles, std::min<long long>((long long)b.max_pages * c.page_size, 1ll << 31));
+  p->s_splits = splits(p->s_tiles, most_keys);
   const size_t n = (size_t)(p->p_splits + p->s_splits) * b.n_tokens * nq;
   p->ml_off = (n * c.head_dim * 4 + 255) / 256 * 256;
   p->bytes = p->ml_off + (n * 8 + 255) / 256 * 256;
@@ -377,7 +300,11 @@ static cudaError_t launch_rows(const BatchAttnArgs& a, int blocks, cudaStream_t 
 }
 
 template <typename TQ, typename TK>
-static cudaError_t launch_batch_attn(const BatchAttnArgs& a, const BatchAttnPlan& p, cudaStream_t st) {
+static cudaError_t launch_batch_rows(BatchAttnArgs& a, const BatchAttnPlan& p, cudaStream_t st) {
+  a.p_tiles = p.p_tiles;
+  a.p_splits = p.p_splits;
+  a.s_tiles = p.s_tiles;
+  a.s_splits = p.s_splits;
   const int blocks = a.p_tiles * a.p_splits + a.s_tiles * a.s_splits;
   // rows of whole aligned 4-element groups, else one element at a time
   const uintptr_t any = (uintptr_t)a.pages.k | (uintptr_t)a.pages.v | (uintptr_t)a.pk | (uintptr_t)a.pv;
@@ -444,17 +371,22 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
   a.out_stride = out_stride;
   a.part_o = (float*)workspace;
   a.part_ml = (float2*)((uint8_t*)workspace + p.ml_off);
-  a.p_tiles = p.p_tiles;
-  a.p_splits = p.p_splits;
-  a.s_tiles = p.s_tiles;
-  a.s_splits = p.s_splits;
   a.status = out_status;
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
-  if (dtype == OOS_DTYPE_F32) e = launch_batch_attn<float, float>(a, p, st);
-  else if (cache->dtype == OOS_DTYPE_BF16) e = launch_batch_attn<__nv_bfloat16, __nv_bfloat16>(a, p, st);
-  else if (dtype == OOS_DTYPE_BF16) e = launch_batch_attn<__nv_bfloat16, __half>(a, p, st);
-  else e = launch_batch_attn<__half, __half>(a, p, st);
+  if (p.tc) {
+    a.s_splits = p.pages.splits;
+    e = prefix_len > 0 ? launch_prefix_tc(a, p.prefix, dtype, cache->dtype, st) : cudaSuccess;
+    if (e == cudaSuccess) e = launch_pages_tc(a, p.pages, dtype, cache->dtype, st);
+  } else if (dtype == OOS_DTYPE_F32) {
+    e = launch_batch_rows<float, float>(a, p, st);
+  } else if (cache->dtype == OOS_DTYPE_BF16) {
+    e = launch_batch_rows<__nv_bfloat16, __nv_bfloat16>(a, p, st);
+  } else if (dtype == OOS_DTYPE_BF16) {
+    e = launch_batch_rows<__nv_bfloat16, __half>(a, p, st);
+  } else {
+    e = launch_batch_rows<__half, __half>(a, p, st);
+  }
   return e == cudaSuccess ? OOS_OK : OOS_ECUDA;
 }
 

@@ -1,0 +1,136 @@
+// Attention of a batch step: what its kernels share (batch_attn.cu, batch_prefix.cu,
+// batch_pages.cu).
+#pragma once
+
+#include "batch.cuh"
+
+namespace oos {
+
+constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
+
+struct BatchAttnArgs {
+  PagesView pages;
+  BatchView batch;
+  const void* q;
+  long long q_stride;
+  const uint8_t* pk;
+  const uint8_t* pv;
+  int prefix_len;
+  const int32_t* parent;
+  int nq, group;
+  float scale_log2;
+  void* out;
+  long long out_stride;
+  float* part_o;      // [part][token][head][d]
+  float2* part_ml;    // [part][token][head]
+  int p_tiles, p_splits, s_tiles, s_splits;
+  int32_t* status;
+};
+
+OOS_DEV float max_nan(float a, float b) {   // a NaN wins, so that it reaches the output
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Rows of a tile and the keys they may see
+struct TileRows {
+  int seq;            // -1: the prefix's keys
+  int q0;             // first token of the rows counted
+  long long r0;       // first row of the tile: token q0 + r / group, head r % group
+  int rows;           // rows of the tile
+  int n;              // rows of the sequence in this step
+  int first;          // its positions before them
+  int len;            // its positions
+};
+
+// Tile `i` of the sequences' tiles of `tile_rows` rows.  Sequence b's tiles start at
+// b + floor(q_start[b] group / tile_rows): a count known without a scan, at the price
+// of some numbers that no tile has.  The whole warp; false: no such tile.
+OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRows* t) {
+  const BatchView& b = a.batch;
+  auto start = [&](int s) { return s + (long long)b.q_start[s] * a.group / tile_rows; };
+  const int seq = warp_count_le(b.n_seqs - 1, start, i);
+  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = b.seq_len[seq];
+  const long long most = (long long)b.max_pages * a.pages.page_size;
+  bool ok = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1 && (!a.parent || q1 - q0 <= kMaxTreeRows);
+  if (!ok || len < q1 - q0 || len > most) {
+    if (threadIdx.x == 0) *a.status = ok || !a.parent ? OOS_EBATCH : OOS_ETREE;
+  }
+  if (!ok || i < start(seq)) return false;
+  t->seq = seq;
+  t->q0 = q0;
+  t->r0 = (i - start(seq)) * tile_rows;
+  t->rows = (int)max(0ll, min((long long)tile_rows, (long long)(q1 - q0) * a.group - t->r0));
+  t->n = q1 - q0;
+  t->first = len - t->n;
+  t->len = (int)min((long long)len, most);
+  return t->rows > 0;
+}
+
+// Ancestor sets of the sequence's rows, [row] -> 128 bits, itself included, by pointer
+// doubling in shared memory.  The whole block; n <= kMaxTreeRows.
+struct TreeScratch {
+  unsigned long long anc[2][kMaxTreeRows][2];
+  int up[2][kMaxTreeRows];
+};
+OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int n, TreeScratch* t))[2] {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    int p = a.parent[q0 + i];
+    if (p < -1 || p >= i) {
+      *a.status = OOS_ETREE;
+      p = -1;
+    }
+    t->up[0][i] = p;
+    t->anc[0][i][0] = i < 64 ? 1ull << i : 0ull;
+    t->anc[0][i][1] = i < 64 ? 0ull : 1ull << (i - 64);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (int step = 1; step < n; step *= 2, cur ^= 1) {
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+      const int p = t->up[cur][i];
+      t->anc[cur ^ 1][i][0] = t->anc[cur][i][0] | (p >= 0 ? t->anc[cur][p][0] : 0ull);
+      t->anc[cur ^ 1][i][1] = t->anc[cur][i][1] | (p >= 0 ? t->anc[cur][p][1] : 0ull);
+      t->up[cur ^ 1][i] = p >= 0 ? t->up[cur][p] : -1;
+    }
+    __syncthreads();
+  }
+  return t->anc[cur];
+}
+
+// ---- 16-bit types with heads of 128 (tensor cores)
+
+// bf16 queries of a binary16 cache: a power of two per row brings the largest element
+// to [1, 2), where binary16 holds bf16's 8 bits exactly (elements below 2^-14 of it
+// to 2^-25 of it, far below what their scores are rounded by); the power goes into
+// the row's scale.  Zero, infinite or NaN rows stay as they are.
+OOS_DEV int row_exponent(float mx) {
+  if (!(mx > 0.f) || mx == INFINITY) return 0;
+  return max(-126, min(126, (int)(__float_as_uint(mx) >> 23) - 127));
+}
+OOS_DEV float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+OOS_DEV float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+OOS_DEV float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+OOS_DEV uint32_t scaled_half2(uint32_t w, float f) {
+  const __half2 v = __floats2half2_rn(bf16_lo(w) * f, bf16_hi(w) * f);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// clusters of the prefix kernel: what a call is cut into
+struct PrefixPlan {
+  int splits;   // key ranges of the same rows, the blocks of a cluster
+  int pairs;    // pairs of 128-row tiles
+};
+bool plan_prefix_tc(long long rows, int nkv, int prefix_len, PrefixPlan* p);
+struct PagesPlan {
+  bool wide;    // 64 rows per block, else 16
+  int tiles, splits;
+};
+PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
+// the prefix's part of every row: unnormalised O in part_o, (m, l) in part_ml
+cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dtype, int kv_dtype, cudaStream_t st);
+// the sequences' own keys, joined with the prefix's part (where there is one) into out
+cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
+
+}  // namespace oos

@@ -1,0 +1,433 @@
+// Attention of a batch step over the sequences' own pages, 16-bit types with heads of
+// 128, and the join with the prefix's part.
+//
+// A block owns a tile of rows (token, head of one kv head's group) of one sequence and a
+// range of its keys; the blocks of the other ranges of the same rows are its cluster.
+// Pages are gathered by 16-byte asynchronous copies, a key row of 256 bytes by 16 lanes,
+// whatever the page size: keys that are not there arrive as zeros.  Products run on
+// mma.sync m16n8k16, operands by ldmatrix from rows whose 16-byte chunks are swizzled by
+// the key, S and O in registers.
+//   narrow  16 rows (a decoding token's group): the keys are dealt to the block's four
+//           warps in chunks of 16, each warp with a three-stage ring of its own, no
+//           block barrier before the end.  Bound by HBM.
+//   wide    64 rows (trees, prompts): 16 rows per warp, chunks of 64 keys shared by
+//           the block, so that a key is read once for 64 rows.
+// Every row keeps its maximum, moved only when a chunk exceeds it by 2^8, and its sum in
+// fp32.  Weights enter P.V in the pages' type: binary16, or bf16 (narrow: as two bf16
+// halves, whose second product costs nothing beside the reads).
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attn.cuh"
+#include "batch_attn.cuh"
+
+namespace oos {
+
+constexpr int kPgWarps = 4;
+constexpr int kPgStages = 3;
+constexpr int kPgD = 128;
+constexpr int kPgRow = 2 * kPgD;                 // bytes of a key row
+constexpr int kPgChunkBytes = 2 * 16 * kPgRow;   // 16 keys, K and V
+constexpr int kPgSmem = kPgStages * kPgWarps * kPgChunkBytes;
+constexpr int kPgLd = kPgD + 4;                  // staged O rows, floats: the row, m, l
+static_assert(64 * kPgLd * 4 <= kPgSmem, "staged rows over the rings");
+
+OOS_DEV void cp_async16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+OOS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+OOS_DEV void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+OOS_DEV void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+OOS_DEV void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+template <bool F16>
+OOS_DEV void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <typename TQ, bool F16, bool WIDE>
+__global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int ROWS = WIDE ? 64 : 16, KC = WIDE ? 64 : 16;   // rows of the block, keys a warp takes at once
+  constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
+  __shared__ TreeScratch s_tree;
+  __shared__ uint32_t s_valid[kPgStages][kPgWarps];           // keys of a chunk that are there
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = blockIdx.y, S = a.s_splits, split = blockIdx.x % S;
+  pdl_trigger();
+  TileRows t;
+  if (!sequence_tile(a, blockIdx.x / S, ROWS, &t)) {          // the whole cluster
+    if (blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();       // the grid must not end before the one it follows
+    return;
+  }
+  const unsigned long long (*anc)[2] = nullptr;
+  if (a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
+  const int last = (int)((t.r0 + t.rows - 1) / a.group);
+  const int n_keys = anc ? t.len : max(0, min(t.len, t.first + last + 1));
+  const int units = (n_keys + 63) / 64;
+  const int k0 = (int)((long long)units * split / S) * 64;
+  const int k1 = min(n_keys, (int)((long long)units * (split + 1) / S) * 64);
+  const int n_chunks = max(0, k1 - k0 + 63) / 64;             // of 64 keys: one per warp each, or one for all
+
+  // ---- copies: this warp's 16 keys of 64-key chunk c (narrow: its own chunk)
+  const uint32_t ring = smem_addr(smem);
+  auto slot_of = [&](int c) -> long long {   // lane & 15: a key
+    const int key = k0 + c * 64 + warp * 16 + (lane & 15);
+    if (c >= n_chunks || key >= k1) return -1;
+    const long long at = page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
+    if (at < 0) *a.status = OOS_EBATCH;
+    return at;
+  };
+  const long long key_bytes = (long long)a.pages.nkv * kPgRow;
+  const uint8_t* kg = a.pages.k + (long long)g * kPgRow + (lane & 15) * 16;
+  const uint8_t* vg = a.pages.v + (long long)g * kPgRow + (lane & 15) * 16;
+  auto copy = [&](int c, long long slot) {
+    const int st = c % kPgStages;
+    const uint32_t dst = ring + (st * kPgWarps + warp) * kPgChunkBytes;
+    if (c < n_chunks) {
+      const uint32_t valid = __ballot_sync(0xffffffffu, slot >= 0) & 0xffffu;
+      if (lane == 0) s_valid[st][warp] = valid;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = 2 * i + (lane >> 4);
+        const long long at = __shfl_sync(0xffffffffu, slot, key);
+        const uint32_t o = key * kPgRow + (((lane & 15) ^ (key & 7)) << 4);
+        const bool ok = at >= 0;
+        const long long off = ok ? at * key_bytes : 0;
+        cp_async16(dst + o, kg + off, ok);
+        cp_async16(dst + 16 * kPgRow + o, vg + off, ok);
+      }
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int c = 0; c < kPgStages - 1; ++c) copy(c, slot_of(c));
+
+  // ---- queries: A fragments of this warp's 16 rows, all of d
+  const int row0 = WIDE ? warp * 16 : 0;          // rows of the tile
+  const int rr[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
+  int token[2];
+  uint32_t qf[8][4];
+  float sc[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const long long row = t.r0 + rr[h];
+    token[h] = (int)(row / a.group);
+    const bool on = rr[h] < t.rows;
+    const TQ* q = (const TQ*)a.q + (t.q0 + (on ? token[h] : 0)) * a.q_stride + (g * a.group + (int)(row % a.group)) * kPgD;
+    uint32_t x[8][2];   // two elements each
+    const bool pairs = ((uintptr_t)q & 3) == 0;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c = kk * 16 + e * 8 + (lane & 3) * 2;
+        x[kk][e] = 0;
+        if (on) {
+          const uint16_t* p = reinterpret_cast<const uint16_t*>(q) + c;
+          x[kk][e] = pairs ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)p[0] | (uint32_t)p[1] << 16;
+        }
+      }
+    sc[h] = a.scale_log2;
+    if constexpr (CONVERT) {
+      float mx = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(x[kk][e])), fabsf(bf16_hi(x[kk][e]))));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const int e2 = row_exponent(mx);
+      sc[h] *= exp2i(e2);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[kk][e] = scaled_half2(x[kk][e], exp2i(-e2));
+    }
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) qf[kk][2 * e + h] = x[kk][e];
+  }
+  unsigned long long an[2][2] = {};
+  if (anc) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (rr[h] < t.rows) {
+        an[h][0] = anc[token[h]][0];
+        an[h][1] = anc[token[h]][1];
+      }
+  }
+
+  float o[16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
+
+  // ldmatrix rows of this lane: K, keys by d; V, transposed on the way
+  const uint32_t k_key = ((lane >> 4) << 3) + (lane & 7), k_chunk = (lane >> 3) & 1;
+  const uint32_t v_key = (((lane >> 3) & 1) << 3) + (lane & 7), v_chunk = lane >> 4;
+
+  for (int c = 0; c < n_chunks; ++c) {
+    const long long next = slot_of(c + kPgStages - 1);
+    cp_async_wait<kPgStages - 2>();
+    if (WIDE) __syncthreads();   // every warp's keys are there, and the stage before is free
+    else __syncwarp();
+    const int st = c % kPgStages;
+    copy(c + kPgStages - 1, next);
+    unsigned long long valid;
+    if (WIDE) {
+      valid = 0;
+#pragma unroll
+      for (int w = 0; w < kPgWarps; ++w) valid |= (unsigned long long)s_valid[st][w] << (16 * w);
+    } else {
+      valid = s_valid[st][warp];
+    }
+    if (valid == 0) continue;    // warp-uniform
+    const int key0 = k0 + c * 64 + (WIDE ? 0 : warp * 16);
+    const uint32_t buf = ring + (st * kPgWarps + (WIDE ? 0 : warp)) * kPgChunkBytes;
+    // keys 16 j .. of the chunk: K rows, then V rows, of the warp that copied them
+    float s[KC / 8][4];
+#pragma unroll
+    for (int i = 0; i < KC / 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int j = 0; j < KC / 16; ++j) {
+        uint32_t b[4];
+        ldsm4(buf + j * kPgChunkBytes + k_key * kPgRow + (((2 * kk + k_chunk) ^ (k_key & 7)) << 4), b);
+        mma16816<F16>(s[2 * j], qf[kk], b[0], b[1]);
+        mma16816<F16>(s[2 * j + 1], qf[kk], b[2], b[3]);
+      }
+    // keys of the chunk that each row sees
+    const int seen = t.first - key0;   // those before it are committed
+    const bool full = valid == (KC == 64 ? ~0ull : 0xffffull) && seen >= KC;
+    if (!full) {
+      unsigned long long bits[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int lead = max(0, min(64, anc ? seen : seen + token[h] + 1));
+        unsigned long long b = lead >= 64 ? ~0ull : (1ull << lead) - 1;
+        if (anc) {
+          unsigned long long lo, hi;
+          if (seen >= 0) shl128(an[h][0], an[h][1], min(seen, 128), lo, hi);
+          else shr128(an[h][0], an[h][1], min(-seen, 128), lo, hi);
+          b |= lo;
+        }
+        bits[h] = b & valid;
+      }
+#pragma unroll
+      for (int i = 0; i < KC / 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!((bits[e >> 1] >> (8 * i + (lane & 3) * 2 + (e & 1))) & 1)) s[i][e] = -INFINITY;
+    }
+    bool move = false;
+    float mn[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < KC / 8; ++i) {
+        s[i][2 * h] *= sc[h];
+        s[i][2 * h + 1] *= sc[h];
+        mx = max_nan(mx, max_nan(s[i][2 * h], s[i][2 * h + 1]));
+      }
+      mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      mn[h] = !(mx <= m[h] + 8.f) ? mx : m[h];   // a NaN moves it, and stays
+      move = move || mn[h] != m[h];
+    }
+    if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float f = m[h] == mn[h] ? 1.f : m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn[h]);
+        l[h] *= f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          o[i][2 * h] *= f;
+          o[i][2 * h + 1] *= f;
+        }
+        m[h] = mn[h];
+      }
+    }
+    uint32_t p[KC / 8][2], p_lo[KC / 8][2];
+#pragma unroll
+    for (int i = 0; i < KC / 8; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool live = m[h] != -INFINITY;
+        const float p0 = live ? ex2_approx(s[i][2 * h] - m[h]) : 0.f, p1 = live ? ex2_approx(s[i][2 * h + 1] - m[h]) : 0.f;
+        l[h] += p0 + p1;
+        if constexpr (F16) {
+          const __half2 v = __floats2half2_rn(p0, p1);
+          p[i][h] = *reinterpret_cast<const uint32_t*>(&v);
+        } else {
+          const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+          p[i][h] = *reinterpret_cast<const uint32_t*>(&v);
+          if constexpr (!WIDE) {
+            const __nv_bfloat162 r = __floats2bfloat162_rn(p0 - __low2float(v), p1 - __high2float(v));
+            p_lo[i][h] = *reinterpret_cast<const uint32_t*>(&r);
+          }
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < KC / 16; ++j) {
+      const uint32_t pa[4] = {p[2 * j][0], p[2 * j][1], p[2 * j + 1][0], p[2 * j + 1][1]};
+#pragma unroll
+      for (int dn = 0; dn < 8; ++dn) {
+        uint32_t b[4];
+        ldsm4_trans(buf + j * kPgChunkBytes + (16 + v_key) * kPgRow + (((2 * dn + v_chunk) ^ (v_key & 7)) << 4), b);
+        mma16816<F16>(o[2 * dn], pa, b[0], b[1]);
+        mma16816<F16>(o[2 * dn + 1], pa, b[2], b[3]);
+        if constexpr (!F16 && !WIDE) {
+          const uint32_t pl[4] = {p_lo[2 * j][0], p_lo[2 * j][1], p_lo[2 * j + 1][0], p_lo[2 * j + 1][1]};
+          mma16816<F16>(o[2 * dn], pl, b[0], b[1]);
+          mma16816<F16>(o[2 * dn + 1], pl, b[2], b[3]);
+        }
+      }
+    }
+  }
+  cp_async_wait<0>();
+  __syncthreads();
+  // ---- join: O rows with (m, l), staged over the rings, of every warp that had keys of
+  // the row (narrow: four), of every block of the cluster, and the prefix's part
+  float* stage = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+    float* row = stage + (size_t)(warp * 16 + (lane >> 2) + 8 * h) * kPgLd;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) *reinterpret_cast<float2*>(row + 8 * i + (lane & 3) * 2) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
+    if ((lane & 3) == 0) *reinterpret_cast<float2*>(row + kPgD) = make_float2(m[h], l[h]);
+  }
+  pdl_wait();   // the prefix's part
+  __syncthreads();
+  if (S > 1) {
+    cluster_arrive_release();
+    cluster_wait_acquire();
+  }
+  constexpr int LOCAL = WIDE ? 1 : kPgWarps;
+  const int r_lo = t.rows * split / S, r_hi = t.rows * (split + 1) / S;
+  for (int r = r_lo + warp; r < r_hi; r += kPgWarps) {
+    const long long row = t.r0 + r;
+    const long long tok = t.q0 + row / a.group;
+    const int head = g * a.group + (int)(row % a.group);
+    // lane i: (m, l) of part i; the prefix's is the last
+    const int parts = LOCAL * S;   // <= 32 - 1
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < parts) {
+      const float* p = stage + (size_t)((WIDE ? 0 : lane % LOCAL) * 16 + r) * kPgLd + kPgD;
+      ml = S > 1 ? ld_cluster2(dsmem_addr(p, lane / LOCAL)) : *reinterpret_cast<const float2*>(p);
+    } else if (lane == parts && a.prefix_len > 0) {
+      ml = a.part_ml[tok * a.nq + head];
+    }
+    const float M = warp_max(ml.x);
+    const bool on = ml.x != -INFINITY;   // true for a NaN
+    const float w = on ? exp2f(ml.x - M) : 0.f;
+    const float den = warp_sum(on ? w * ml.y : 0.f);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](int i, float4 v) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      if (wi == 0.f) return;
+      acc.x += wi * v.x;
+      acc.y += wi * v.y;
+      acc.z += wi * v.z;
+      acc.w += wi * v.w;
+    };
+    float4 pre = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.prefix_len > 0) pre = *reinterpret_cast<const float4*>(a.part_o + (tok * a.nq + head) * kPgD + 4 * lane);
+    for (int i = 0; i < parts; ++i) {
+      const float* p = stage + (size_t)((WIDE ? 0 : i % LOCAL) * 16 + r) * kPgLd + 4 * lane;
+      add(i, S > 1 ? ld_cluster4(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float4*>(p));
+    }
+    if (a.prefix_len > 0) add(parts, pre);
+    const float f = den == 0.f ? 0.f : 1.f / den;
+    const float v[4] = {acc.x * f, acc.y * f, acc.z * f, acc.w * f};
+    TQ* out = (TQ*)a.out + tok * a.out_stride + head * kPgD + 4 * lane;
+    if (((uintptr_t)out & 7) == 0) {
+      store_vec<TQ, 4>(out, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = from_f32<TQ>(v[i]);
+    }
+  }
+  if (S > 1) {   // a peer may still read this block's rows
+    cluster_arrive_release();
+    cluster_wait_acquire();
+  }
+}
+
+PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms) {
+  PagesPlan p;
+  p.wide = rows > 16ll * n_seqs;
+  p.tiles = (int)(n_seqs + rows / (p.wide ? 64 : 16));
+  // blocks for every SM twice, each with 128 keys at least; a cluster holds 4 ranges
+  // (their parts and the prefix's fit the join's 32 lanes)
+  const long long want = 4ll * n_sms / std::max(1ll, (long long)p.tiles * nkv);
+  p.splits = (int)std::max(1ll, std::min({want, most_keys / 128, 4ll}));
+  return p;
+}
+
+template <typename TQ, bool F16, bool WIDE>
+static cudaError_t launch_pages(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(k_attn_pages<TQ, F16, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPgSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)(p.tiles * p.splits), a.pages.nkv);
+  lc.blockDim = dim3(kPgWarps * 32);
+  lc.dynamicSmemBytes = kPgSmem;
+  lc.stream = st;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (p.splits > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = p.splits;
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
+  if (a.prefix_len > 0) {   // starts while the prefix's kernel drains, and waits for it before the join
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  lc.attrs = attr;
+  lc.numAttrs = n;
+  return cudaLaunchKernelEx(&lc, k_attn_pages<TQ, F16, WIDE>, a);
+}
+
+cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st) {
+  if (kv_dtype == OOS_DTYPE_BF16)
+    return p.wide ? launch_pages<__nv_bfloat16, false, true>(a, p, st) : launch_pages<__nv_bfloat16, false, false>(a, p, st);
+  if (dtype == OOS_DTYPE_BF16)
+    return p.wide ? launch_pages<__nv_bfloat16, true, true>(a, p, st) : launch_pages<__nv_bfloat16, true, false>(a, p, st);
+  return p.wide ? launch_pages<__half, true, true>(a, p, st) : launch_pages<__half, true, false>(a, p, st);
+}
+
+}  // namespace oos

@@ -1,0 +1,493 @@
+// Attention of a batch step over the shared prefix, 16-bit types with heads of 128:
+// the rows of all sequences against the prefix's keys, so that each key tile is read
+// once per 256 rows.  Leaves every row's unnormalised O, maximum and sum for the join
+// with the sequence's own keys (batch_pages.cu).
+//
+// tcgen05, rows (token, head of one kv head's group) packed without regard to the
+// sequences.  A block has two streams of work, each with its scores S and its O in
+// TMEM and four softmax warps of its own, a thread per row:
+//   two row tiles   (more than 128 rows left): both streams take every key tile
+//   one row tile    the streams take the even and the odd key tiles
+// so that one stream's softmax runs under the other's products.  A unit of work is a
+// (key tile, stream) pair, taken in turn.  One thread issues the scores, one the P.V
+// products, so that neither waits behind the other's barriers; a stream's next scores
+// overwrite its P, and wait for the P.V product that reads it.
+//
+// P overlays S in TMEM as packed 16-bit pairs and is the A operand of P.V; the sum l
+// is of the unrounded weights.  The running maximum moves only when a tile exceeds it
+// by 2^8 (the threads rescale their O rows in TMEM then, between two products).
+// Keys past the prefix's end arrive as zeros (the tensor map ends there), so masking
+// their scores is enough.
+//
+// The blocks of the key ranges of the same rows form a cluster: every block stages its
+// rows over the K/V ring, and past a cluster barrier the rows are dealt to the blocks,
+// which pull them from every range and add them up in order.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <atomic>
+#include <mutex>
+
+#include "attn.cuh"
+#include "batch_attn.cuh"
+
+namespace oos {
+
+constexpr int kPxRows = 128, kPxKeys = 128, kPxD = 128;
+constexpr int kPxDBlock = kPxKeys * 128;            // 64 of d by 128 keys, 128-byte swizzle
+constexpr int kPxTile = 2 * kPxDBlock;              // 32 KB
+constexpr int kPxKStages = 3, kPxVStages = 2;
+constexpr int kPxOffK = 0;
+constexpr int kPxOffV = kPxOffK + kPxKStages * kPxTile;
+constexpr int kPxOffQ = kPxOffV + kPxVStages * kPxTile;   // two row tiles
+constexpr int kPxOffExp = kPxOffQ + 2 * kPxTile;          // row exponents of converted queries
+constexpr int kPxOffBar = kPxOffExp + 2 * kPxRows * 4;
+constexpr int kPxSmem = kPxOffBar + 256 + 1024;           // + alignment slack
+constexpr int kPxThreads = 384;
+constexpr int kPxSoft0 = 4;                               // softmax warps 4..7 and 8..11
+constexpr int kPxRegsIo = 56, kPxRegsSoft = 224, kPxRegsLaunch = 168;
+constexpr int kPxMaxSplits = 16;
+constexpr int kPxLd = kPxD + 4;                           // staged row: O, m, l
+static_assert(128 * kPxRegsIo + (kPxThreads - 128) * kPxRegsSoft <= kPxThreads * kPxRegsLaunch, "register split");
+static_assert(2 * kPxRows * kPxLd * 4 <= kPxOffQ, "staged rows over the ring");
+static_assert(kPxSmem <= 227 * 1024, "shared memory per block");
+// TMEM columns: S (P over its first 64) of either stream, O of either
+constexpr int kPxTmS = 0, kPxTmO = 2 * kPxKeys, kPxTmCols = 512;
+
+struct PrefixArgs {
+  CUtensorMap kmap, vmap;   // [prefix_len][nkv][d] as (d, kv head, slot)
+  BatchAttnArgs a;
+  int splits;
+};
+
+// A wait of at most kWaitLimitNs; false: it ran out here or elsewhere in the block
+OOS_DEV bool px_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int32_t* status) {
+  const uint32_t addr = smem_addr(bar);
+  if (mbar_test(addr, parity)) return true;
+  const unsigned long long t0 = globaltimer();
+  while (true) {
+    if (mbar_test_sleep(addr, parity, 20000u)) return true;
+    if (*abort) return false;
+    if (globaltimer() - t0 > kWaitLimitNs) {
+      *abort = 1;
+      *status = OOS_ETIMEOUT;
+      return false;
+    }
+  }
+}
+
+OOS_DEV float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+template <typename TQ, bool F16>
+__global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_constant__ PrefixArgs p) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
+  // binary16 weights carry 2^4, so that fewer of the small ones fall below its range
+  constexpr float kBias = F16 ? 4.f : 0.f;
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sm + kPxOffBar);
+  uint64_t* kfull = bar;           // [3] transaction bytes
+  uint64_t* kempty = bar + 3;      // [3] its score products done
+  uint64_t* vfull = bar + 6;       // [2] transaction bytes
+  uint64_t* vempty = bar + 8;      // [2] its P.V products done
+  uint64_t* sfull = bar + 10;      // [2] scores of a stream done (and its P.V before them)
+  uint64_t* pfull = bar + 12;      // [2] four softmax warps: P written
+  uint64_t* pvdone = bar + 14;     // [2] P.V of a stream done
+  uint64_t* qready = bar + 16;     // eight warps: queries in shared memory
+  uint64_t* odone = bar + 17;      // both issuers: all products done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 18);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const BatchAttnArgs& a = p.a;
+  int32_t* status = a.status;
+  const int S = p.splits, split = blockIdx.x % S, pair = blockIdx.x / S, g = blockIdx.y;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row0 = (long long)pair * 2 * kPxRows;
+  const int rows = (int)min(2ll * kPxRows, (long long)a.batch.n_tokens * a.group - row0);
+  const int dual = rows > kPxRows ? 1 : 0;
+  const int n_all = (a.prefix_len + kPxKeys - 1) / kPxKeys;
+  const int t0 = (int)((long long)n_all * split / S);
+  const int n_tiles = (int)((long long)n_all * (split + 1) / S) - t0;
+  const int units = n_tiles << dual;                  // unit u: tile u >> dual, stream u & 1
+  pdl_trigger();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&kfull[i], 1);
+      mbar_init(&kempty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&vfull[i], 1);
+      mbar_init(&vempty[i], 1);
+      mbar_init(&sfull[i], 1);
+      mbar_init(&pfull[i], 4);
+      mbar_init(&pvdone[i], 1);
+    }
+    mbar_init(qready, 8);
+    mbar_init(odone, 2);
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 2) tmem_alloc(tmem_slot, kPxTmCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  float* stage = reinterpret_cast<float*>(sm);
+
+  if (warp < kPxSoft0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPxRegsIo));
+    if ((warp == 0 || warp == 3) && lane == 0) {
+      // ---------------------------------------------------------- loaders: K and V tiles
+      const bool v = warp == 3;
+      const CUtensorMap* map = v ? &p.vmap : &p.kmap;
+      uint64_t* full = v ? vfull : kfull;
+      uint64_t* empty = v ? vempty : kempty;
+      const int stages = v ? kPxVStages : kPxKStages;
+      tma_prefetch_desc(map);
+      const uint64_t pol = policy_evict_last();   // the other row tiles read it too
+      int n = 0;
+      for (; n < n_tiles; ++n) {
+        const int st = n % stages;
+        if (n >= stages && !px_wait(&empty[st], (uint32_t)(n / stages - 1) & 1u, abort_flag, status)) break;
+        unsigned char* dst = sm + (v ? kPxOffV : kPxOffK) + st * kPxTile;
+        mbar_arrive_expect_tx(&full[st], kPxTile);
+        tma_load_3d(dst, map, &full[st], 0, g, (t0 + n) * kPxKeys, pol);
+        tma_load_3d(dst + kPxDBlock, map, &full[st], 64, g, (t0 + n) * kPxKeys, pol);
+      }
+      // every copy issued has landed before the block goes on
+      for (int i = n > stages ? n - stages : 0; i < n; ++i) drain_wait(&full[i % stages], (uint32_t)(i / stages) & 1u);
+    } else if (warp == 1 && lane == 0) {
+      // ---------------------------------------------------------- scores
+      constexpr uint32_t idesc = F16 ? idesc_f16_f32(kPxRows, kPxKeys) : idesc_bf16_f32(kPxRows, kPxKeys);
+      const uint64_t kdesc = smem_desc_sw128(smem_addr(sm + kPxOffK)), qdesc = smem_desc_sw128(smem_addr(sm + kPxOffQ));
+      bool ok = px_wait(qready, 0, abort_flag, status);
+      for (int u = 0; u < units && ok; ++u) {
+        const int i = u >> dual, st = i % kPxKStages, x = u & 1, use = u >> 1;   // use: of this stream
+        if (!dual || x == 0) ok = px_wait(&kfull[st], (uint32_t)(i / kPxKStages) & 1u, abort_flag, status);
+        if (ok && use > 0) ok = px_wait(&pvdone[x], (uint32_t)(use - 1) & 1u, abort_flag, status);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < kPxD / 16; ++k) {
+          const uint64_t o = (uint64_t)(((k >> 2) * kPxDBlock) >> 4) + 2 * (k & 3);
+          tc_mma_bf16(tmem + kPxTmS + x * kPxKeys, qdesc + o + (uint64_t)(((dual ? x : 0) * kPxTile) >> 4),
+                      kdesc + o + (uint64_t)((st * kPxTile) >> 4), idesc, k > 0 ? 1u : 0u);
+        }
+        tc_commit(&sfull[x]);
+        if (!dual || x == 1) tc_commit(&kempty[st]);
+      }
+      tc_commit(odone);
+    } else if (warp == 2 && lane == 0) {
+      // ---------------------------------------------------------- P.V
+      constexpr uint32_t idesc = (F16 ? idesc_f16_f32(kPxRows, kPxD) : idesc_bf16_f32(kPxRows, kPxD)) | (1u << 16);
+      const uint64_t vdesc = smem_desc_sw128_mn(smem_addr(sm + kPxOffV), kPxDBlock);
+      bool ok = true;
+      for (int u = 0; u < units; ++u) {
+        const int i = u >> dual, st = i % kPxVStages, x = u & 1, use = u >> 1;
+        if (!dual || x == 0) ok = px_wait(&vfull[st], (uint32_t)(i / kPxVStages) & 1u, abort_flag, status);
+        ok = ok && px_wait(&pfull[x], (uint32_t)use & 1u, abort_flag, status);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int k = 0; k < kPxKeys / 16; ++k)
+          tc_mma_bf16_ts(tmem + kPxTmO + x * kPxD, tmem + kPxTmS + x * kPxKeys + 8 * k,
+                         vdesc + (uint64_t)((st * kPxTile + k * 16 * 128) >> 4), idesc, (k > 0 || use > 0) ? 1u : 0u);
+        tc_commit(&pvdone[x]);
+        if (!dual || x == 1) tc_commit(&vempty[st]);
+      }
+      tc_commit(odone);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();   // rows staged
+    tc_fence_after();
+    cluster_arrive_release();
+    __syncwarp();
+    cluster_wait_acquire();
+    cluster_arrive_release();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPxRegsSoft));
+    // ------------------------------------------------------------ softmax: stream x, a thread per row
+    const int x = (warp - kPxSoft0) >> 2, q4 = warp & 3;
+    const int lrow = q4 * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(q4 * 32) << 16;
+    float* s_exp = reinterpret_cast<float*>(sm + kPxOffExp);
+    // queries of the stream's row tile (one row tile: the first stream's warps), two rows
+    // of 16 lanes at a time, into the swizzled layout
+    if (x == 0 || dual) {
+      unsigned char* qs = sm + kPxOffQ + x * kPxTile;
+      const int c = lane & 15;
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const int r = q4 * 32 + 2 * i + (lane >> 4);
+        const long long row = row0 + x * kPxRows + r;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (x * kPxRows + r < rows) {
+          const uint16_t* q = (const uint16_t*)a.q + (row / a.group) * a.q_stride +
+                              (long long)(g * a.group + (int)(row % a.group)) * kPxD + c * 8;
+          if (((uintptr_t)q & 15) == 0) {
+            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(q);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)q[2 * e] | (uint32_t)q[2 * e + 1] << 16;
+          }
+        }
+        if constexpr (CONVERT) {
+          float mx = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(w[e])), fabsf(bf16_hi(w[e]))));
+#pragma unroll
+          for (int s = 1; s < 16; s *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+          const int e2 = row_exponent(mx);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = scaled_half2(w[e], exp2i(-e2));
+          if (c == 0) s_exp[x * kPxRows + r] = exp2i(e2);
+        }
+        *reinterpret_cast<uint4*>(qs + (c >> 3) * kPxDBlock + sw128(r, c & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      fence_async_smem();
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(qready);
+    float sc = a.scale_log2;
+    if constexpr (CONVERT) {
+      // one row tile: the second stream's rows are the first's, written by its warps
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      sc *= s_exp[(dual ? x : 0) * kPxRows + lrow];
+    }
+    const int mine = dual ? n_tiles : (n_tiles + 1 - x) >> 1;   // tiles of this stream
+    const uint32_t ts = tmem + lane_off + kPxTmS + x * kPxKeys, to = tmem + lane_off + kPxTmO + x * kPxD;
+    float m = -INFINITY, l = 0.f;
+    for (int j = 0; j < mine; ++j) {
+      if (!__all_sync(0xffffffffu, px_wait(&sfull[x], (uint32_t)j & 1u, abort_flag, status))) break;
+      tc_fence_after();
+      const int key0 = (t0 + (dual ? j : 2 * j + x)) * kPxKeys;
+      float sv[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32_nowait(ts + 32 * c, sv + 32 * c);
+      tmem_wait_ld_regs(sv);
+      const int n_ok = a.prefix_len - key0;
+      if (n_ok < kPxKeys) {
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (i >= n_ok) sv[i] = -INFINITY;
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < 128; i += 2) mx[(i >> 1) & 3] = max3_nan(mx[(i >> 1) & 3], sv[i], sv[i + 1]);
+      const float tmax = max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3])) * sc - kBias;
+      const bool move = !(tmax <= m + 8.f);   // a NaN moves it, and stays
+      if (__any_sync(0xffffffffu, move)) {
+        const float f = !move ? 1.f : m == -INFINITY ? 0.f : exp2f(m - tmax);
+        if (j > 0) {
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float ov[32];
+            tmem_ld32_nowait(to + 32 * c, ov);
+            tmem_wait_ld_regs(ov);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) ov[i] *= f;
+            tmem_st16u(to + 32 * c, reinterpret_cast<const uint32_t*>(ov));
+            tmem_st16u(to + 32 * c + 16, reinterpret_cast<const uint32_t*>(ov + 16));
+          }
+        }
+        l *= f;
+        if (move) m = tmax;
+      }
+      // weights 2^(s sc - m); a row without a finite score yet has none
+      const bool live = m != -INFINITY;
+      const float neg = live ? -m : 0.f;
+      float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float p0 = live ? ex2_approx(fmaf(sv[32 * c + i], sc, neg)) : 0.f;
+          const float p1 = live ? ex2_approx(fmaf(sv[32 * c + i + 1], sc, neg)) : 0.f;
+          ps[(i >> 1) & 3] += p0 + p1;
+          if constexpr (F16) {
+            const __half2 v = __floats2half2_rn(p0, p1);
+            pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+          } else {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+            pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+          }
+        }
+        tmem_st16u(ts + 16 * c, pk);
+      }
+      l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&pfull[x]);
+    }
+    // the ring and TMEM are free once all products are done (the issuer always says so)
+    drain_wait(odone, 0);
+    tc_fence_after();
+    const bool have = mine > 0 && !*abort_flag;
+    float* row = stage + (size_t)(x * kPxRows + lrow) * kPxLd;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+      float ov[32];
+      tmem_ld32_nowait(to + 32 * c, ov);
+      tmem_wait_ld_regs(ov);
+#pragma unroll
+      for (int i = 0; i < 32; i += 4)
+        *reinterpret_cast<float4*>(row + 32 * c + i) =
+            have ? make_float4(ov[i], ov[i + 1], ov[i + 2], ov[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    *reinterpret_cast<float2*>(row + kPxD) = make_float2(have ? m : -INFINITY, have ? l : 0.f);
+    tc_fence_before();
+    __syncthreads();   // rows staged
+    tc_fence_after();
+    cluster_arrive_release();
+    __syncwarp();
+    cluster_wait_acquire();
+    // ------------------------------------------------------------ the rows' parts added up
+    // rows of the pair dealt to the cluster's blocks, a warp per row: lane i holds (m, l) of
+    // part i, every lane four columns
+    const int halves = dual ? 1 : 2, parts = S * halves;   // <= 32
+    const int lo = (int)((long long)rows * split / S), hi = (int)((long long)rows * (split + 1) / S);
+    for (int r = lo + warp - kPxSoft0; r < hi; r += 8) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (lane < parts)
+        ml = ld_cluster2(dsmem_addr(stage + (size_t)((lane % halves) * kPxRows + r) * kPxLd + kPxD, lane / halves));
+      const float M = warp_max(ml.x);
+      const bool on = ml.x != -INFINITY;
+      const float w = on ? exp2f(ml.x - M) : 0.f;
+      const float den = warp_sum(on ? w * ml.y : 0.f);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i0 = 0; i0 < parts; i0 += 4) {
+        float4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[i] = i0 + i < parts ? ld_cluster4(dsmem_addr(stage + (size_t)(((i0 + i) % halves) * kPxRows + r) * kPxLd + 4 * lane, (i0 + i) / halves))
+                                : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float wi = i0 + i < parts ? __shfl_sync(0xffffffffu, w, i0 + i) : 0.f;
+          acc.x += wi * v[i].x;
+          acc.y += wi * v[i].y;
+          acc.z += wi * v[i].z;
+          acc.w += wi * v[i].w;
+        }
+      }
+      const long long grow = row0 + r;
+      const long long at = (grow / a.group) * a.nq + g * a.group + grow % a.group;
+      *reinterpret_cast<float4*>(a.part_o + at * kPxD + 4 * lane) = acc;
+      if (lane == 0) a.part_ml[at] = make_float2(den == den ? M : den, den);   // a NaN stays one in the join
+    }
+    cluster_arrive_release();
+  }
+  __syncwarp();
+  cluster_wait_acquire();   // no peer reads this block's rows any more
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kPxTmCols);
+  }
+}
+
+// ---- host
+static cudaLaunchConfig_t px_config(dim3 grid, int splits, cudaLaunchAttribute* attr, cudaStream_t st) {
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = grid;
+  lc.blockDim = dim3(kPxThreads);
+  lc.dynamicSmemBytes = kPxSmem;
+  lc.stream = st;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = splits;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  return lc;
+}
+
+template <typename TQ, bool F16>
+static cudaError_t px_attributes() {
+  cudaError_t e = cudaFuncSetAttribute(k_attn_prefix<TQ, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPxSmem);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(k_attn_prefix<TQ, F16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  // the register split must not ask for more than the block is launched with
+  return e == cudaSuccess ? check_launch_regs((const void*)k_attn_prefix<TQ, F16>, kPxRegsLaunch) : e;
+}
+
+// What does not change while a process lives, of each device: that the kernels may use
+// their shared memory, and how many clusters of s blocks the device holds at once.
+struct PxDevice {
+  std::atomic<int> state{0};   // 1: ready
+  int clusters[kPxMaxSplits + 1] = {0};
+};
+static PxDevice* px_device() {
+  static PxDevice devices[64];
+  static std::mutex lock;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  PxDevice& d = devices[dev];
+  if (d.state.load(std::memory_order_acquire) == 1) return &d;
+  std::lock_guard<std::mutex> hold(lock);
+  if (d.state.load(std::memory_order_relaxed) == 1) return &d;
+  if (px_attributes<__nv_bfloat16, false>() != cudaSuccess || px_attributes<__nv_bfloat16, true>() != cudaSuccess ||
+      px_attributes<__half, true>() != cudaSuccess)
+    return nullptr;
+  for (int s = 1; s <= kPxMaxSplits; ++s) {
+    cudaLaunchAttribute attr[1];
+    cudaLaunchConfig_t lc = px_config(dim3(s), s, attr, nullptr);
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, (const void*)k_attn_prefix<__nv_bfloat16, false>, &lc) != cudaSuccess) n = 0;
+    cudaGetLastError();
+    d.clusters[s] = n;
+  }
+  d.state.store(1, std::memory_order_release);
+  return &d;
+}
+
+// The count of key ranges with the shortest schedule: waves of resident clusters, each
+// of a block's tiles and what a block costs besides (in units of a row tile's work on a
+// key tile, about 0.6 us).
+bool plan_prefix_tc(long long rows, int nkv, int prefix_len, PrefixPlan* p) {
+  const PxDevice* d = px_device();
+  if (!d) return false;
+  p->pairs = (int)((rows + 2 * kPxRows - 1) / (2 * kPxRows));
+  p->splits = 0;
+  const long long items = (long long)p->pairs * nkv;
+  const int tiles = (prefix_len + kPxKeys - 1) / kPxKeys;
+  const double tile = rows > kPxRows ? 2.0 : 1.0;
+  double best = 0;
+  for (int s = 1; s <= kPxMaxSplits && s <= tiles; ++s) {
+    if (d->clusters[s] < 1) continue;
+    const double cost = (double)((items + d->clusters[s] - 1) / d->clusters[s]) * (tile * ((tiles + s - 1) / s) + 6.0 + 0.2 * s);
+    if (p->splits == 0 || cost < best) {
+      best = cost;
+      p->splits = s;
+    }
+  }
+  return p->splits > 0;
+}
+
+cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& plan, int dtype, int kv_dtype, cudaStream_t st) {
+  PrefixArgs p;
+  memset(&p, 0, sizeof(p));
+  p.a = a;
+  p.splits = plan.splits;
+  const uint64_t dims[3] = {(uint64_t)kPxD, (uint64_t)a.pages.nkv, (uint64_t)a.prefix_len};
+  const uint64_t strides[2] = {(uint64_t)kPxD * 2, (uint64_t)a.pages.nkv * kPxD * 2};
+  const uint32_t box[3] = {64, 1, (uint32_t)kPxKeys};
+  const bool f16 = kv_dtype == OOS_DTYPE_F16;
+  if (!encode_bf16_map(&p.kmap, a.pk, 3, dims, strides, box, f16) || !encode_bf16_map(&p.vmap, a.pv, 3, dims, strides, box, f16))
+    return cudaErrorInvalidValue;
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t lc = px_config(dim3((unsigned)(plan.pairs * plan.splits), a.pages.nkv), plan.splits, attr, st);
+  if (!f16) return cudaLaunchKernelEx(&lc, k_attn_prefix<__nv_bfloat16, false>, p);
+  if (dtype == OOS_DTYPE_BF16) return cudaLaunchKernelEx(&lc, k_attn_prefix<__nv_bfloat16, true>, p);
+  return cudaLaunchKernelEx(&lc, k_attn_prefix<__half, true>, p);
+}
+
+}  // namespace oos
