@@ -50,8 +50,8 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   if (prefix) {
     t.seq = -1;
     t.q0 = 0;
-    t.r0 = (long long)tile * RT;
-    t.rows = (int)min((long long)RT, (long long)a.batch.n_tokens * a.group - t.r0);
+    t.r0 = tile * RT;
+    t.rows = min(RT, a.batch.n_tokens * a.group - t.r0);
     t.first = t.len = a.prefix_len;
   } else if (!sequence_tile(a, tile, RT, &t)) {
     return;
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   const unsigned long long (*anc)[2] = nullptr;
   if (!prefix && a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
   // the keys any row of the tile sees, dealt to the splits in whole tiles
-  const int last = (int)((t.r0 + t.rows - 1) / a.group);   // its last token, counted from q0
+  const int last = (t.r0 + t.rows - 1) / a.group;   // its last token, counted from q0
   const int n_keys = prefix || anc ? t.len : max(0, min(t.len, t.first + last + 1));
   const int n_tiles = (n_keys + kRowKeys - 1) / kRowKeys;
   const int k0 = (int)((long long)n_tiles * split / splits) * kRowKeys;
@@ -69,8 +69,8 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     const int r = i / (ld - 4), c = i % (ld - 4);
     float v = 0.f;
     if (r < t.rows && c < d) {
-      const long long row = t.r0 + r;
-      v = to_f32(((const TQ*)a.q)[(t.q0 + row / a.group) * a.q_stride + (g * a.group + row % a.group) * d + c]);
+      const int row = t.r0 + r;
+      v = to_f32(((const TQ*)a.q)[(long long)(t.q0 + row / a.group) * a.q_stride + (g * a.group + row % a.group) * d + c]);
     }
     s_q[r * ld + c] = v;
   }
@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     }
     __syncthreads();
     float s[RPT][4];
+    bool see[RPT][4];
 #pragma unroll
     for (int r = 0; r < RPT; ++r)
 #pragma unroll
@@ -137,15 +138,16 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     }
 #pragma unroll
     for (int r = 0; r < RPT; ++r) {
-      const int token = (int)((t.r0 + tr * RPT + r) / a.group);
+      const int token = (t.r0 + tr * RPT + r) / a.group;
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = key0 + tc + 8 * j, own = key - t.first;
-        bool see = s_at[tc + 8 * j] >= 0;
+        bool ok = s_at[tc + 8 * j] >= 0;
         if (!prefix && own >= 0)
-          see = see && (anc ? token < t.n && own < kMaxTreeRows && ((anc[token][own >> 6] >> (own & 63)) & 1) : own <= token);
-        s[r][j] = see ? s[r][j] * a.scale_log2 : -INFINITY;
+          ok = ok && (anc ? token < t.n && own < kMaxTreeRows && ((anc[token][own >> 6] >> (own & 63)) & 1) : own <= token);
+        see[r][j] = ok;
+        s[r][j] = ok ? s[r][j] * a.scale_log2 : -INFINITY;
         mx = max_nan(mx, s[r][j]);
       }
 #pragma unroll
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
       for (int j = 0; j < 4; ++j) {
         const float p = live ? exp2f(s[r][j] - mn) : 0.f;
         sum += p;
-        s_p[(tr * RPT + r) * ldp + tc + 8 * j] = p;
+        s_p[(tr * RPT + r) * ldp + tc + 8 * j] = see[r][j] ? p : -1.f;   // negative: not seen
       }
 #pragma unroll
       for (int x = 1; x < 8; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
@@ -182,6 +184,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
         const float4 v = *reinterpret_cast<const float4*>(s_v + key * ld + col);
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
+          if (p[r] < 0.f) continue;   // whatever its v is
           o[r][c][0] += p[r] * v.x;
           o[r][c][1] += p[r] * v.y;
           o[r][c][2] += p[r] * v.z;
@@ -197,8 +200,8 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   for (int r = 0; r < RPT; ++r) {
     const int lr = tr * RPT + r;
     if (lr >= t.rows) continue;
-    const long long row = t.r0 + lr;
-    const long long at = part * n_rows + (t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
+    const int row = t.r0 + lr;
+    const long long at = part * n_rows + (long long)(t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
     if (tc == 0) a.part_ml[at] = make_float2(m[r], l[r]);
 #pragma unroll
     for (int c = 0; c < 4; ++c)

@@ -37,7 +37,7 @@ OOS_DEV float max_nan(float a, float b) {   // a NaN wins, so that it reaches th
 struct TileRows {
   int seq;            // -1: the prefix's keys
   int q0;             // first token of the rows counted
-  long long r0;       // first row of the tile: token q0 + r / group, head r % group
+  int r0;             // first row of the tile: token q0 + r / group, head r % group
   int rows;           // rows of the tile
   int n;              // rows of the sequence in this step
   int first;          // its positions before them
@@ -60,12 +60,15 @@ OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRow
   if (!ok || i < start(seq)) return false;
   t->seq = seq;
   t->q0 = q0;
-  t->r0 = (i - start(seq)) * tile_rows;
-  t->rows = (int)max(0ll, min((long long)tile_rows, (long long)(q1 - q0) * a.group - t->r0));
+  // counts of rows stay below 2^26 (n_tokens * nq is), those of a table out of order do not
+  const long long r0 = (i - start(seq)) * tile_rows, all = (long long)(q1 - q0) * a.group;
+  if (r0 >= all) return false;
+  t->r0 = (int)r0;
+  t->rows = (int)min((long long)tile_rows, all - r0);
   t->n = q1 - q0;
   t->first = len - t->n;
   t->len = (int)min((long long)len, most);
-  return t->rows > 0;
+  return true;
 }
 
 // Ancestor sets of the sequence's rows, [row] -> 128 bits, itself included, by pointer
@@ -100,6 +103,52 @@ OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int
 }
 
 // ---- 16-bit types with heads of 128 (tensor cores)
+
+// Rows lo + warp, + n_warps, .. below hi, a warp per row and R rows at a time (their
+// loads in flight together: one row at a time, the join waited on each row's latency,
+// 2 us a row): part i of row r has (m, l) = ml_of(r, i), its four columns of this lane
+// v_of(r, i), i < parts <= 32.  out(r, O, max m, weighted l) takes the sum.
+template <int R, typename ML, typename V, typename OUT>
+OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_of, V v_of, OUT out) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r0 = lo + warp; r0 < hi; r0 += R * n_warps) {
+    float2 ml[R];
+    float w[R], top[R], den[R];
+    float4 acc[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int r = r0 + k * n_warps;
+      ml[k] = make_float2(-INFINITY, 0.f);
+      if (r < hi && lane < parts) ml[k] = ml_of(r, lane);
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const bool on = ml[k].x != -INFINITY;   // a NaN is, and reaches the sum
+      top[k] = warp_max(ml[k].x);
+      w[k] = on ? exp2f(ml[k].x - top[k]) : 0.f;
+      den[k] = warp_sum(on ? w[k] * ml[k].y : 0.f);
+      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll 2
+    for (int i = 0; i < parts; ++i) {
+      float4 v[R];
+#pragma unroll
+      for (int k = 0; k < R; ++k) v[k] = v_of(min(r0 + k * n_warps, hi - 1), i);
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const float wi = __shfl_sync(0xffffffffu, w[k], i);
+        acc[k].x += wi * v[k].x;
+        acc[k].y += wi * v[k].y;
+        acc[k].z += wi * v[k].z;
+        acc[k].w += wi * v[k].w;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+      if (r0 + k * n_warps < hi) out(r0 + k * n_warps, acc[k], top[k], den[k]);
+  }
+}
 
 // bf16 queries of a binary16 cache: a power of two per row brings the largest element
 // to [1, 2), where binary16 holds bf16's 8 bits exactly (elements below 2^-14 of it

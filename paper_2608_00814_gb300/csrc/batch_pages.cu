@@ -37,6 +37,14 @@ static_assert(64 * kPgLd * 4 <= kPgSmem, "staged rows over the rings");
 OOS_DEV void cp_async16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+OOS_DEV void lds128(uint32_t addr, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
+}
+OOS_DEV uint32_t lds32(uint32_t addr) {
+  uint32_t w;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(addr) : "memory");
+  return w;
+}
 OOS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 OOS_DEV void cp_async_wait() {
@@ -68,6 +76,22 @@ OOS_DEV void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// whether a value of the chunk's V is infinite or NaN (16-key pieces at buf)
+template <bool F16>
+OOS_DEV bool chunk_not_finite(uint32_t buf, int pieces) {
+  constexpr uint32_t kExp = F16 ? 0x7c007c00u : 0x7f807f80u;
+  uint32_t bad = 0;
+  for (int j = 0; j < pieces; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t w[4];
+      lds128(buf + j * kPgChunkBytes + 16 * kPgRow + (i * 32 + (threadIdx.x & 31)) * 16, w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bad |= __vcmpeq2(w[e] & kExp, kExp);
+    }
+  return __any_sync(0xffffffffu, bad != 0);
+}
+
 template <typename TQ, bool F16, bool WIDE>
 __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
@@ -85,7 +109,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
   }
   const unsigned long long (*anc)[2] = nullptr;
   if (a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
-  const int last = (int)((t.r0 + t.rows - 1) / a.group);
+  const int last = (t.r0 + t.rows - 1) / a.group;
   const int n_keys = anc ? t.len : max(0, min(t.len, t.first + last + 1));
   const int units = (n_keys + 63) / 64;
   const int k0 = (int)((long long)units * split / S) * 64;
@@ -134,10 +158,10 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
   float sc[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const long long row = t.r0 + rr[h];
-    token[h] = (int)(row / a.group);
+    const int row = t.r0 + rr[h];
+    token[h] = row / a.group;
     const bool on = rr[h] < t.rows;
-    const TQ* q = (const TQ*)a.q + (t.q0 + (on ? token[h] : 0)) * a.q_stride + (g * a.group + (int)(row % a.group)) * kPgD;
+    const TQ* q = (const TQ*)a.q + (long long)(t.q0 + (on ? token[h] : 0)) * a.q_stride + (g * a.group + row % a.group) * kPgD;
     uint32_t x[8][2];   // two elements each
     const bool pairs = ((uintptr_t)q & 3) == 0;
 #pragma unroll
@@ -172,6 +196,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
 #pragma unroll
       for (int e = 0; e < 2; ++e) qf[kk][2 * e + h] = x[kk][e];
   }
+  // first and last token of the warp's rows
+  const int tok_lo = (t.r0 + row0) / a.group, tok_hi = (t.r0 + min(row0 + 15, t.rows - 1)) / a.group;
   unsigned long long an[2][2] = {};
   if (anc) {
 #pragma unroll
@@ -207,8 +233,9 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
     } else {
       valid = s_valid[st][warp];
     }
-    if (valid == 0) continue;    // warp-uniform
     const int key0 = k0 + c * 64 + (WIDE ? 0 : warp * 16);
+    // nothing there, no row of this warp, or no row that sees the first key (warp-uniform)
+    if (valid == 0 || row0 >= t.rows || (!anc && key0 > t.first + tok_hi)) continue;
     const uint32_t buf = ring + (st * kPgWarps + (WIDE ? 0 : warp)) * kPgChunkBytes;
     // keys 16 j .. of the chunk: K rows, then V rows, of the warp that copied them
     float s[KC / 8][4];
@@ -227,12 +254,12 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
       }
     // keys of the chunk that each row sees
     const int seen = t.first - key0;   // those before it are committed
-    const bool full = valid == (KC == 64 ? ~0ull : 0xffffull) && seen >= KC;
+    const bool full = valid == (KC == 64 ? ~0ull : 0xffffull) && (anc ? seen : seen + tok_lo + 1) >= KC;
+    unsigned long long bits[2] = {~0ull, ~0ull};
     if (!full) {
-      unsigned long long bits[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        int lead = max(0, min(64, anc ? seen : seen + token[h] + 1));
+        const int lead = max(0, min(64, anc ? seen : seen + token[h] + 1));
         unsigned long long b = lead >= 64 ? ~0ull : (1ull << lead) - 1;
         if (anc) {
           unsigned long long lo, hi;
@@ -248,6 +275,9 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
         for (int e = 0; e < 4; ++e)
           if (!((bits[e >> 1] >> (8 * i + (lane & 3) * 2 + (e & 1))) & 1)) s[i][e] = -INFINITY;
     }
+    // A key that some of the rows do not see must not reach them through 0 times a v
+    // that is not finite: such a chunk (the last ones of a sequence only) is summed apart.
+    const bool apart = !full && chunk_not_finite<F16>(buf, KC / 16);
     bool move = false;
     float mn[2];
 #pragma unroll
@@ -284,6 +314,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
       for (int h = 0; h < 2; ++h) {
         const bool live = m[h] != -INFINITY;
         const float p0 = live ? ex2_approx(s[i][2 * h] - m[h]) : 0.f, p1 = live ? ex2_approx(s[i][2 * h + 1] - m[h]) : 0.f;
+        s[i][2 * h] = p0;
+        s[i][2 * h + 1] = p1;
         l[h] += p0 + p1;
         if constexpr (F16) {
           const __half2 v = __floats2half2_rn(p0, p1);
@@ -297,6 +329,34 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
           }
         }
       }
+    if (apart) {
+#pragma unroll
+      for (int i = 0; i < KC / 8; ++i)
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+          const int key = 8 * i + j;
+          float pj[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float mine = j & 1 ? s[i][2 * h + 1] : s[i][2 * h];
+            pj[h] = __shfl_sync(0xffffffffu, mine, (lane & ~3) | (j >> 1));
+          }
+          const uint32_t vrow = buf + (key >> 4) * kPgChunkBytes + (16 + (key & 15)) * kPgRow + (lane & 3) * 4;
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const uint32_t w = lds32(vrow + ((c ^ (key & 7)) << 4));
+            const float v0 = F16 ? __low2float(*reinterpret_cast<const __half2*>(&w)) : bf16_lo(w);
+            const float v1 = F16 ? __high2float(*reinterpret_cast<const __half2*>(&w)) : bf16_hi(w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if ((bits[h] >> key) & 1) {
+                o[c][2 * h] += pj[h] * v0;
+                o[c][2 * h + 1] += pj[h] * v1;
+              }
+          }
+        }
+      continue;
+    }
 #pragma unroll
     for (int j = 0; j < KC / 16; ++j) {
       const uint32_t pa[4] = {p[2 * j][0], p[2 * j][1], p[2 * j + 1][0], p[2 * j + 1][1]};
@@ -334,51 +394,38 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
     cluster_arrive_release();
     cluster_wait_acquire();
   }
+  // parts of a row: LOCAL of every block, then the prefix's; at most 17
   constexpr int LOCAL = WIDE ? 1 : kPgWarps;
-  const int r_lo = t.rows * split / S, r_hi = t.rows * (split + 1) / S;
-  for (int r = r_lo + warp; r < r_hi; r += kPgWarps) {
-    const long long row = t.r0 + r;
-    const long long tok = t.q0 + row / a.group;
-    const int head = g * a.group + (int)(row % a.group);
-    // lane i: (m, l) of part i; the prefix's is the last
-    const int parts = LOCAL * S;   // <= 32 - 1
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < parts) {
-      const float* p = stage + (size_t)((WIDE ? 0 : lane % LOCAL) * 16 + r) * kPgLd + kPgD;
-      ml = S > 1 ? ld_cluster2(dsmem_addr(p, lane / LOCAL)) : *reinterpret_cast<const float2*>(p);
-    } else if (lane == parts && a.prefix_len > 0) {
-      ml = a.part_ml[tok * a.nq + head];
-    }
-    const float M = warp_max(ml.x);
-    const bool on = ml.x != -INFINITY;   // true for a NaN
-    const float w = on ? exp2f(ml.x - M) : 0.f;
-    const float den = warp_sum(on ? w * ml.y : 0.f);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](int i, float4 v) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      if (wi == 0.f) return;
-      acc.x += wi * v.x;
-      acc.y += wi * v.y;
-      acc.z += wi * v.z;
-      acc.w += wi * v.w;
-    };
-    float4 pre = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.prefix_len > 0) pre = *reinterpret_cast<const float4*>(a.part_o + (tok * a.nq + head) * kPgD + 4 * lane);
-    for (int i = 0; i < parts; ++i) {
-      const float* p = stage + (size_t)((WIDE ? 0 : i % LOCAL) * 16 + r) * kPgLd + 4 * lane;
-      add(i, S > 1 ? ld_cluster4(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float4*>(p));
-    }
-    if (a.prefix_len > 0) add(parts, pre);
-    const float f = den == 0.f ? 0.f : 1.f / den;
-    const float v[4] = {acc.x * f, acc.y * f, acc.z * f, acc.w * f};
-    TQ* out = (TQ*)a.out + tok * a.out_stride + head * kPgD + 4 * lane;
-    if (((uintptr_t)out & 7) == 0) {
-      store_vec<TQ, 4>(out, v);
-    } else {
+  const int own = LOCAL * S;
+  auto at = [&](int r) {
+    const int row = t.r0 + r;
+    return (long long)(t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
+  };
+  auto staged = [&](int r, int i) { return stage + ((WIDE ? 0 : i % LOCAL) * 16 + r) * kPgLd; };
+  join_rows<WIDE ? 4 : 1>(
+      t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + (a.prefix_len > 0 ? 1 : 0),
+      [&](int r, int i) {
+        if (i == own) return a.part_ml[at(r)];
+        const float* p = staged(r, i) + kPgD;
+        return S > 1 ? ld_cluster2(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float2*>(p);
+      },
+      [&](int r, int i) {
+        if (i == own) return *reinterpret_cast<const float4*>(a.part_o + at(r) * kPgD + 4 * lane);
+        const float* p = staged(r, i) + 4 * lane;
+        return S > 1 ? ld_cluster4(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float4*>(p);
+      },
+      [&](int r, float4 o, float, float den) {
+        const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
+        const float v[4] = {o.x * f, o.y * f, o.z * f, o.w * f};
+        const int row = t.r0 + r;
+        TQ* out = (TQ*)a.out + (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kPgD + 4 * lane;
+        if (((uintptr_t)out & 7) == 0) {
+          store_vec<TQ, 4>(out, v);
+        } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) out[i] = from_f32<TQ>(v[i]);
-    }
-  }
+          for (int e = 0; e < 4; ++e) out[e] = from_f32<TQ>(v[e]);
+        }
+      });
   if (S > 1) {   // a peer may still read this block's rows
     cluster_arrive_release();
     cluster_wait_acquire();

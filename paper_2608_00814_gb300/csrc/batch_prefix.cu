@@ -106,8 +106,8 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
   int32_t* status = a.status;
   const int S = p.splits, split = blockIdx.x % S, pair = blockIdx.x / S, g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row0 = (long long)pair * 2 * kPxRows;
-  const int rows = (int)min(2ll * kPxRows, (long long)a.batch.n_tokens * a.group - row0);
+  const int row0 = pair * 2 * kPxRows;
+  const int rows = min(2 * kPxRows, a.batch.n_tokens * a.group - row0);
   const int dual = rows > kPxRows ? 1 : 0;
   const int n_all = (a.prefix_len + kPxKeys - 1) / kPxKeys;
   const int t0 = (int)((long long)n_all * split / S);
@@ -224,11 +224,11 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
 #pragma unroll 4
       for (int i = 0; i < 16; ++i) {
         const int r = q4 * 32 + 2 * i + (lane >> 4);
-        const long long row = row0 + x * kPxRows + r;
+        const int row = row0 + x * kPxRows + r;
         uint32_t w[4] = {0, 0, 0, 0};
         if (x * kPxRows + r < rows) {
-          const uint16_t* q = (const uint16_t*)a.q + (row / a.group) * a.q_stride +
-                              (long long)(g * a.group + (int)(row % a.group)) * kPxD + c * 8;
+          const uint16_t* q = (const uint16_t*)a.q + (long long)(row / a.group) * a.q_stride +
+                              (g * a.group + row % a.group) * kPxD + c * 8;
           if (((uintptr_t)q & 15) == 0) {
             *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(q);
           } else {
@@ -349,39 +349,21 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
     __syncwarp();
     cluster_wait_acquire();
     // ------------------------------------------------------------ the rows' parts added up
-    // rows of the pair dealt to the cluster's blocks, a warp per row: lane i holds (m, l) of
-    // part i, every lane four columns
-    const int halves = dual ? 1 : 2, parts = S * halves;   // <= 32
+    // rows of the pair dealt to the cluster's blocks; with one row tile a block holds two parts
+    const int halves = dual ? 1 : 2;
     const int lo = (int)((long long)rows * split / S), hi = (int)((long long)rows * (split + 1) / S);
-    for (int r = lo + warp - kPxSoft0; r < hi; r += 8) {
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (lane < parts)
-        ml = ld_cluster2(dsmem_addr(stage + (size_t)((lane % halves) * kPxRows + r) * kPxLd + kPxD, lane / halves));
-      const float M = warp_max(ml.x);
-      const bool on = ml.x != -INFINITY;
-      const float w = on ? exp2f(ml.x - M) : 0.f;
-      const float den = warp_sum(on ? w * ml.y : 0.f);
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i0 = 0; i0 < parts; i0 += 4) {
-        float4 v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          v[i] = i0 + i < parts ? ld_cluster4(dsmem_addr(stage + (size_t)(((i0 + i) % halves) * kPxRows + r) * kPxLd + 4 * lane, (i0 + i) / halves))
-                                : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float wi = i0 + i < parts ? __shfl_sync(0xffffffffu, w, i0 + i) : 0.f;
-          acc.x += wi * v[i].x;
-          acc.y += wi * v[i].y;
-          acc.z += wi * v[i].z;
-          acc.w += wi * v[i].w;
-        }
-      }
-      const long long grow = row0 + r;
-      const long long at = (grow / a.group) * a.nq + g * a.group + grow % a.group;
-      *reinterpret_cast<float4*>(a.part_o + at * kPxD + 4 * lane) = acc;
-      if (lane == 0) a.part_ml[at] = make_float2(den == den ? M : den, den);   // a NaN stays one in the join
-    }
+    join_rows<4>(
+        lo, hi, warp - kPxSoft0, 8, S * halves,
+        [&](int r, int i) { return ld_cluster2(dsmem_addr(stage + ((i % halves) * kPxRows + r) * kPxLd + kPxD, i / halves)); },
+        [&](int r, int i) {
+          return ld_cluster4(dsmem_addr(stage + ((i % halves) * kPxRows + r) * kPxLd + 4 * lane, i / halves));
+        },
+        [&](int r, float4 o, float top, float den) {
+          const int row = row0 + r;
+          const long long at = (long long)(row / a.group) * a.nq + g * a.group + row % a.group;
+          *reinterpret_cast<float4*>(a.part_o + at * kPxD + 4 * lane) = o;
+          if (lane == 0) a.part_ml[at] = make_float2(den == den ? top : den, den);   // a NaN stays one in the next join
+        });
     cluster_arrive_release();
   }
   __syncwarp();

@@ -336,6 +336,35 @@ def test_attention_large_and_special_scores(dtype, kv):
     assert torch.equal(nan, want)
 
 
+@pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_attention_masked_places_hold_anything(dtype, kv, tree, value):
+    """A v or k that is not finite at one of the step's own positions reaches the rows that see it, and no other."""
+    counts, lens = [3, 1, 90, 30], [3, 20, 200, 31]
+    step = R.Step(counts, lens, 16)
+    parent = [j - 1 for j in range(3)] + [-1] + [-1 if j == 0 else j // 2 for j in range(90)] + [-1] * 30 if tree else None
+    par = torch.tensor(parent, dtype=torch.int32, device="cuda") if tree else None
+    q, pk, pv, kp, vp = inputs(step, 50, 6, 2, 128, dtype, kv)
+    base, _ = attend(step, q, pk, pv, 50, kp, vp, par)
+    sees = torch.zeros(step.n, dtype=torch.bool)
+    for b, node in ((0, 2), (2, 40), (3, 7)):
+        lo, c, n = step.q_start[b], counts[b], lens[b]
+        p, e = step.where(b, n - c + node)
+        vp[p, e, 1, 3] = value
+        rel = R.ancestors(parent[lo:lo + c]) if tree else torch.ones(c, c).tril() > 0
+        sees[lo:lo + c] |= rel[:, node]
+    out, st = attend(step, q, pk, pv, 50, kp, vp, par)
+    assert int(st) == 0
+    got, want = out.float().cpu(), base.float().cpu()
+    want[sees, 3:, 3] = value
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    same = torch.isfinite(want)
+    assert torch.equal(got[~same & ~torch.isnan(want)], want[~same & ~torch.isnan(want)])
+    # both sums are within their bounds of the exact one; compare with twice a loose one
+    assert float((got - want)[same].abs().max()) <= 0.05 * float(want[same].abs().max())
+
+
 @pytest.mark.parametrize("dtype, kv", TYPES[1:])
 def test_attention_queries_of_any_size(dtype, kv):
     """Queries far above and below one: with binary16 pages they must neither overflow nor vanish."""
