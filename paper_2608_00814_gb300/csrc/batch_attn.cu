@@ -267,11 +267,10 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, 1ll << 31);
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc) {
-    if (rows > 0 && prefix_len > 0 && !plan_prefix_tc(rows, c.n_kv_heads, prefix_len, &p->prefix)) return false;
+    p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, sms) : PrefixPlan{0, 0};
     p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
-    const size_t n = prefix_len > 0 ? (size_t)b.n_tokens * nq : 0;
-    p->ml_off = n * 128 * 4;
-    p->bytes = p->ml_off + (n * 8 + 255) / 256 * 256;
+    p->ml_off = 0;
+    p->bytes = ((size_t)p->prefix.splits * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
     return true;
   }
   p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
@@ -378,6 +377,7 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
   if (p.tc) {
+    a.p_splits = p.prefix.splits;
     a.s_splits = p.pages.splits;
     e = prefix_len > 0 ? launch_prefix_tc(a, p.prefix, dtype, cache->dtype, st) : cudaSuccess;
     if (e == cudaSuccess) e = launch_pages_tc(a, p.pages, dtype, cache->dtype, st);

@@ -7,6 +7,7 @@
 namespace oos {
 
 constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
+constexpr int kPartLd = 128 + 4;   // a row of a part: O, m, l, padded to 16 bytes
 
 struct BatchAttnArgs {
   PagesView pages;
@@ -21,8 +22,11 @@ struct BatchAttnArgs {
   float scale_log2;
   void* out;
   long long out_stride;
-  float* part_o;      // [part][token][head][d]
-  float2* part_ml;    // [part][token][head]
+  // parts in the workspace: of all rows and keys, part_o [part][token][head][d] and
+  // part_ml [part][token][head]; on tensor cores of the prefix only, in part_o
+  // [part][kv head][row][kPartLd], row = token * group + head in group: O, m, l
+  float* part_o;
+  float2* part_ml;
   int p_tiles, p_splits, s_tiles, s_splits;
   int32_t* status;
 };
@@ -108,7 +112,7 @@ OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int
 // loads in flight together: one row at a time, the join waited on each row's latency,
 // 2 us a row): part i of row r has (m, l) = ml_of(r, i), its four columns of this lane
 // v_of(r, i), i < parts <= 32.  out(r, O, max m, weighted l) takes the sum.
-template <int R, typename ML, typename V, typename OUT>
+template <int R, int UNROLL, typename ML, typename V, typename OUT>
 OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_of, V v_of, OUT out) {
   const int lane = threadIdx.x & 31;
 #pragma unroll 1
@@ -130,19 +134,26 @@ OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_o
       den[k] = warp_sum(on ? w[k] * ml[k].y : 0.f);
       acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-#pragma unroll 2
-    for (int i = 0; i < parts; ++i) {
-      float4 v[R];
+#pragma unroll 1
+    for (int i0 = 0; i0 < parts; i0 += UNROLL) {
+      float4 v[UNROLL][R];
 #pragma unroll
-      for (int k = 0; k < R; ++k) v[k] = v_of(min(r0 + k * n_warps, hi - 1), i);
+      for (int i = 0; i < UNROLL; ++i)
 #pragma unroll
-      for (int k = 0; k < R; ++k) {
-        const float wi = __shfl_sync(0xffffffffu, w[k], i);
-        acc[k].x += wi * v[k].x;
-        acc[k].y += wi * v[k].y;
-        acc[k].z += wi * v[k].z;
-        acc[k].w += wi * v[k].w;
-      }
+        for (int k = 0; k < R; ++k) v[i][k] = v_of(min(r0 + k * n_warps, hi - 1), min(i0 + i, parts - 1));
+#pragma unroll
+      for (int i = 0; i < UNROLL; ++i)
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          float wi = __shfl_sync(0xffffffffu, w[k], (i0 + i) & 31);
+          if (i0 + i >= parts) wi = 0.f;
+          if (wi != 0.f) {   // a part without weight counts for nothing, whatever it holds
+            acc[k].x += wi * v[i][k].x;
+            acc[k].y += wi * v[i][k].y;
+            acc[k].z += wi * v[i][k].z;
+            acc[k].w += wi * v[i][k].w;
+          }
+        }
     }
 #pragma unroll
     for (int k = 0; k < R; ++k)
@@ -168,18 +179,18 @@ OOS_DEV uint32_t scaled_half2(uint32_t w, float f) {
 
 // clusters of the prefix kernel: what a call is cut into
 struct PrefixPlan {
-  int splits;   // key ranges of the same rows, the blocks of a cluster
+  int splits;   // key ranges, a part each
   int pairs;    // pairs of 128-row tiles
 };
-bool plan_prefix_tc(long long rows, int nkv, int prefix_len, PrefixPlan* p);
+PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int n_sms);
 struct PagesPlan {
   bool wide;    // 64 rows per block, else 16
   int tiles, splits;
 };
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
-// the prefix's part of every row: unnormalised O in part_o, (m, l) in part_ml
+// the prefix's parts of every row
 cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dtype, int kv_dtype, cudaStream_t st);
-// the sequences' own keys, joined with the prefix's part (where there is one) into out
+// the sequences' own keys, joined with the prefix's p_splits parts into out
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
 
 }  // namespace oos

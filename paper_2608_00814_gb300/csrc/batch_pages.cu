@@ -26,13 +26,13 @@
 namespace oos {
 
 constexpr int kPgWarps = 4;
-constexpr int kPgStages = 3;
+__host__ __device__ constexpr int pg_stages(bool wide) { return 3; }
+__host__ __device__ constexpr int pg_blocks(bool wide) { return 2; }   // per SM
 constexpr int kPgD = 128;
 constexpr int kPgRow = 2 * kPgD;                 // bytes of a key row
 constexpr int kPgChunkBytes = 2 * 16 * kPgRow;   // 16 keys, K and V
-constexpr int kPgSmem = kPgStages * kPgWarps * kPgChunkBytes;
-constexpr int kPgLd = kPgD + 4;                  // staged O rows, floats: the row, m, l
-static_assert(64 * kPgLd * 4 <= kPgSmem, "staged rows over the rings");
+constexpr int pg_smem(bool wide) { return pg_stages(wide) * kPgWarps * kPgChunkBytes; }
+static_assert(64 * kPartLd * 4 <= pg_smem(false) && 64 * kPartLd * 4 <= pg_smem(true), "staged rows over the rings");
 
 OOS_DEV void cp_async16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -93,12 +93,13 @@ OOS_DEV bool chunk_not_finite(uint32_t buf, int pieces) {
 }
 
 template <typename TQ, bool F16, bool WIDE>
-__global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
+__global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int ROWS = WIDE ? 64 : 16, KC = WIDE ? 64 : 16;   // rows of the block, keys a warp takes at once
+  constexpr int STAGES = pg_stages(WIDE);
   constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
   __shared__ TreeScratch s_tree;
-  __shared__ uint32_t s_valid[kPgStages][kPgWarps];           // keys of a chunk that are there
+  __shared__ uint32_t s_valid[STAGES][kPgWarps];           // keys of a chunk that are there
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = blockIdx.y, S = a.s_splits, split = blockIdx.x % S;
   pdl_trigger();
@@ -116,6 +117,30 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
   const int k1 = min(n_keys, (int)((long long)units * (split + 1) / S) * 64);
   const int n_chunks = max(0, k1 - k0 + 63) / 64;             // of 64 keys: one per warp each, or one for all
 
+  // ---- queries: the loads go out first, over the page lookups that follow
+  const int row0 = WIDE ? warp * 16 : 0;          // rows of the tile
+  const int rr[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
+  int token[2];
+  uint32_t qf[8][4];   // A fragments of 16 rows, all of d
+  float sc[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int row = t.r0 + rr[h];
+    token[h] = row / a.group;
+    const bool on = rr[h] < t.rows;
+    const TQ* q = (const TQ*)a.q + (long long)(t.q0 + (on ? token[h] : 0)) * a.q_stride + (g * a.group + row % a.group) * kPgD;
+    const bool pairs = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 3) == 0;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(q) + kk * 16 + e * 8 + (lane & 3) * 2;
+        uint32_t x = 0;
+        if (on) x = pairs ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)p[0] | (uint32_t)p[1] << 16;
+        qf[kk][2 * e + h] = x;
+      }
+  }
+
   // ---- copies: this warp's 16 keys of 64-key chunk c (narrow: its own chunk)
   const uint32_t ring = smem_addr(smem);
   auto slot_of = [&](int c) -> long long {   // lane & 15: a key
@@ -129,7 +154,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
   const uint8_t* kg = a.pages.k + (long long)g * kPgRow + (lane & 15) * 16;
   const uint8_t* vg = a.pages.v + (long long)g * kPgRow + (lane & 15) * 16;
   auto copy = [&](int c, long long slot) {
-    const int st = c % kPgStages;
+    const int st = c % STAGES;
     const uint32_t dst = ring + (st * kPgWarps + warp) * kPgChunkBytes;
     if (c < n_chunks) {
       const uint32_t valid = __ballot_sync(0xffffffffu, slot >= 0) & 0xffffu;
@@ -147,41 +172,23 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
     }
     cp_async_commit();
   };
+  {
+    long long slot[STAGES - 1];
 #pragma unroll
-  for (int c = 0; c < kPgStages - 1; ++c) copy(c, slot_of(c));
+    for (int c = 0; c < STAGES - 1; ++c) slot[c] = slot_of(c);
+#pragma unroll
+    for (int c = 0; c < STAGES - 1; ++c) copy(c, slot[c]);
+  }
 
-  // ---- queries: A fragments of this warp's 16 rows, all of d
-  const int row0 = WIDE ? warp * 16 : 0;          // rows of the tile
-  const int rr[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
-  int token[2];
-  uint32_t qf[8][4];
-  float sc[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int row = t.r0 + rr[h];
-    token[h] = row / a.group;
-    const bool on = rr[h] < t.rows;
-    const TQ* q = (const TQ*)a.q + (long long)(t.q0 + (on ? token[h] : 0)) * a.q_stride + (g * a.group + row % a.group) * kPgD;
-    uint32_t x[8][2];   // two elements each
-    const bool pairs = ((uintptr_t)q & 3) == 0;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int c = kk * 16 + e * 8 + (lane & 3) * 2;
-        x[kk][e] = 0;
-        if (on) {
-          const uint16_t* p = reinterpret_cast<const uint16_t*>(q) + c;
-          x[kk][e] = pairs ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)p[0] | (uint32_t)p[1] << 16;
-        }
-      }
     sc[h] = a.scale_log2;
     if constexpr (CONVERT) {
       float mx = 0.f;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(x[kk][e])), fabsf(bf16_hi(x[kk][e]))));
+        for (int e = 0; e < 2; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(qf[kk][2 * e + h])), fabsf(bf16_hi(qf[kk][2 * e + h]))));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
       const int e2 = row_exponent(mx);
@@ -189,12 +196,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[kk][e] = scaled_half2(x[kk][e], exp2i(-e2));
+        for (int e = 0; e < 2; ++e) qf[kk][2 * e + h] = scaled_half2(qf[kk][2 * e + h], exp2i(-e2));
     }
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) qf[kk][2 * e + h] = x[kk][e];
   }
   // first and last token of the warp's rows
   const int tok_lo = (t.r0 + row0) / a.group, tok_hi = (t.r0 + min(row0 + 15, t.rows - 1)) / a.group;
@@ -219,12 +222,12 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
   const uint32_t v_key = (((lane >> 3) & 1) << 3) + (lane & 7), v_chunk = lane >> 4;
 
   for (int c = 0; c < n_chunks; ++c) {
-    const long long next = slot_of(c + kPgStages - 1);
-    cp_async_wait<kPgStages - 2>();
+    const long long next = slot_of(c + STAGES - 1);
+    cp_async_wait<STAGES - 2>();
     if (WIDE) __syncthreads();   // every warp's keys are there, and the stage before is free
     else __syncwarp();
-    const int st = c % kPgStages;
-    copy(c + kPgStages - 1, next);
+    const int st = c % STAGES;
+    copy(c + STAGES - 1, next);
     unsigned long long valid;
     if (WIDE) {
       valid = 0;
@@ -284,13 +287,9 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
     for (int h = 0; h < 2; ++h) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < KC / 8; ++i) {
-        s[i][2 * h] *= sc[h];
-        s[i][2 * h + 1] *= sc[h];
-        mx = max_nan(mx, max_nan(s[i][2 * h], s[i][2 * h + 1]));
-      }
+      for (int i = 0; i < KC / 8; ++i) mx = max_nan(mx, max_nan(s[i][2 * h], s[i][2 * h + 1]));
       mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) * sc[h];
       mn[h] = !(mx <= m[h] + 8.f) ? mx : m[h];   // a NaN moves it, and stays
       move = move || mn[h] != m[h];
     }
@@ -307,13 +306,14 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
         m[h] = mn[h];
       }
     }
+    // without a finite score yet every score is -inf, and gives 0
+    const float neg[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
     uint32_t p[KC / 8][2], p_lo[KC / 8][2];
 #pragma unroll
     for (int i = 0; i < KC / 8; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bool live = m[h] != -INFINITY;
-        const float p0 = live ? ex2_approx(s[i][2 * h] - m[h]) : 0.f, p1 = live ? ex2_approx(s[i][2 * h + 1] - m[h]) : 0.f;
+        const float p0 = ex2_approx(fmaf(s[i][2 * h], sc[h], neg[h])), p1 = ex2_approx(fmaf(s[i][2 * h + 1], sc[h], neg[h]));
         s[i][2 * h] = p0;
         s[i][2 * h + 1] = p1;
         l[h] += p0 + p1;
@@ -376,49 +376,117 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages(const __grid_co
   }
   cp_async_wait<0>();
   __syncthreads();
-  // ---- join: O rows with (m, l), staged over the rings, of every warp that had keys of
-  // the row (narrow: four), of every block of the cluster, and the prefix's part
-  float* stage = reinterpret_cast<float*>(smem);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
     l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-    float* row = stage + (size_t)(warp * 16 + (lane >> 2) + 8 * h) * kPgLd;
+  }
+  const int n_pre = a.p_splits;   // the prefix's parts
+  const long long part_rows = (long long)a.batch.n_tokens * a.group;
+  // the prefix's row of tile row r, its first part; part_step floats to the next
+  auto prefix_row = [&](int r) {
+    return a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0 + r) * kPartLd;
+  };
+  const long long part_step = (long long)a.pages.nkv * part_rows * kPartLd;
+  auto out_row = [&](int r) {
+    const int row = t.r0 + r;
+    return (TQ*)a.out + (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kPgD;
+  };
+
+  if (WIDE && S == 1) {
+    // ---- join in registers: a warp has all of its rows' own keys
+    pdl_wait();   // the prefix's parts
+    if (row0 >= t.rows) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float* pr = prefix_row(min(rr[h], t.rows - 1));
+      float top = m[h];
+      for (int i = 0; i < n_pre; ++i) top = fmaxf(top, pr[i * part_step + kPgD]);
+      float w = m[h] == -INFINITY ? 0.f : exp2f(m[h] - top);
+      l[h] *= w;
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        o[c][2 * h] *= w;
+        o[c][2 * h + 1] *= w;
+      }
+      for (int i = 0; i < n_pre; ++i) {
+        const float2 ml = *reinterpret_cast<const float2*>(pr + i * part_step + kPgD);
+        float2 v[16];
+#pragma unroll
+        for (int c = 0; c < 16; ++c) v[c] = *reinterpret_cast<const float2*>(pr + i * part_step + 8 * c + (lane & 3) * 2);
+        w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
+        if (w != 0.f) {
+          l[h] += w * ml.y;
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            o[c][2 * h] += w * v[c].x;
+            o[c][2 * h + 1] += w * v[c].y;
+          }
+        }
+      }
+      const float f = l[h] == 0.f ? 0.f : 1.f / l[h];   // a row without keys: zeros
+      // through this warp's stage, for whole-row stores
+      TQ* srow = reinterpret_cast<TQ*>(smem + (warp * 16 + (lane >> 2) + 8 * h) * (2 * kPgD + 16));
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const float v[2] = {o[c][2 * h] * f, o[c][2 * h + 1] * f};
+        store_vec<TQ, 2>(srow + 8 * c + (lane & 3) * 2, v);
+      }
+    }
+    __syncwarp();
+    const bool vec = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * 2)) & 15) == 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 2 * i + (lane >> 4);
+      if (row0 + r >= t.rows) continue;
+      const Vec<TQ, 8> v = *reinterpret_cast<const Vec<TQ, 8>*>(smem + (warp * 16 + r) * (2 * kPgD + 16) + (lane & 15) * 16);
+      TQ* out = out_row(row0 + r) + (lane & 15) * 8;
+      if (vec) {
+        *reinterpret_cast<Vec<TQ, 8>*>(out) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = v.v[e];
+      }
+    }
+    return;
+  }
+
+  // ---- join through shared memory: O rows with (m, l), staged over the rings, of every
+  // warp that had keys of the row (narrow: four) and of every block of the cluster,
+  // and the prefix's parts; at most 32
+  float* stage = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float* row = stage + (size_t)(warp * 16 + (lane >> 2) + 8 * h) * kPartLd;
 #pragma unroll
     for (int i = 0; i < 16; ++i) *reinterpret_cast<float2*>(row + 8 * i + (lane & 3) * 2) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
     if ((lane & 3) == 0) *reinterpret_cast<float2*>(row + kPgD) = make_float2(m[h], l[h]);
   }
-  pdl_wait();   // the prefix's part
+  pdl_wait();   // the prefix's parts
   __syncthreads();
   if (S > 1) {
     cluster_arrive_release();
     cluster_wait_acquire();
   }
-  // parts of a row: LOCAL of every block, then the prefix's; at most 17
   constexpr int LOCAL = WIDE ? 1 : kPgWarps;
   const int own = LOCAL * S;
-  auto at = [&](int r) {
-    const int row = t.r0 + r;
-    return (long long)(t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
-  };
-  auto staged = [&](int r, int i) { return stage + ((WIDE ? 0 : i % LOCAL) * 16 + r) * kPgLd; };
-  join_rows<WIDE ? 4 : 1>(
-      t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + (a.prefix_len > 0 ? 1 : 0),
+  auto staged = [&](int r, int i) { return stage + ((WIDE ? 0 : i % LOCAL) * 16 + r) * kPartLd; };
+  join_rows<WIDE ? 4 : 1, WIDE ? 2 : 8>(
+      t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + n_pre,
       [&](int r, int i) {
-        if (i == own) return a.part_ml[at(r)];
+        if (i >= own) return *reinterpret_cast<const float2*>(prefix_row(r) + (i - own) * part_step + kPgD);
         const float* p = staged(r, i) + kPgD;
         return S > 1 ? ld_cluster2(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float2*>(p);
       },
       [&](int r, int i) {
-        if (i == own) return *reinterpret_cast<const float4*>(a.part_o + at(r) * kPgD + 4 * lane);
+        if (i >= own) return *reinterpret_cast<const float4*>(prefix_row(r) + (i - own) * part_step + 4 * lane);
         const float* p = staged(r, i) + 4 * lane;
         return S > 1 ? ld_cluster4(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float4*>(p);
       },
-      [&](int r, float4 o, float, float den) {
+      [&](int r, float4 x, float, float den) {
         const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
-        const float v[4] = {o.x * f, o.y * f, o.z * f, o.w * f};
-        const int row = t.r0 + r;
-        TQ* out = (TQ*)a.out + (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kPgD + 4 * lane;
+        const float v[4] = {x.x * f, x.y * f, x.z * f, x.w * f};
+        TQ* out = out_row(r) + 4 * lane;
         if (((uintptr_t)out & 7) == 0) {
           store_vec<TQ, 4>(out, v);
         } else {
@@ -445,12 +513,12 @@ PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys
 
 template <typename TQ, bool F16, bool WIDE>
 static cudaError_t launch_pages(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(k_attn_pages<TQ, F16, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPgSmem);
+  cudaError_t e = cudaFuncSetAttribute(k_attn_pages<TQ, F16, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, pg_smem(WIDE));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(p.tiles * p.splits), a.pages.nkv);
   lc.blockDim = dim3(kPgWarps * 32);
-  lc.dynamicSmemBytes = kPgSmem;
+  lc.dynamicSmemBytes = pg_smem(WIDE);
   lc.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;

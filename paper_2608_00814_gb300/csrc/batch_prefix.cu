@@ -19,15 +19,13 @@
 // Keys past the prefix's end arrive as zeros (the tensor map ends there), so masking
 // their scores is enough.
 //
-// The blocks of the key ranges of the same rows form a cluster: every block stages its
-// rows over the K/V ring, and past a cluster barrier the rows are dealt to the blocks,
-// which pull them from every range and add them up in order.
+// A block stages its rows over the K/V ring and stores them with one bulk copy, a part
+// per key range; the next kernel adds the parts up.  (Ranges joined inside a cluster,
+// through distributed shared memory, took 10 us for 256 rows of 11 ranges.)
 #include <math.h>
 #include <string.h>
 
 #include <algorithm>
-#include <atomic>
-#include <mutex>
 
 #include "attn.cuh"
 #include "batch_attn.cuh"
@@ -48,9 +46,8 @@ constexpr int kPxThreads = 384;
 constexpr int kPxSoft0 = 4;                               // softmax warps 4..7 and 8..11
 constexpr int kPxRegsIo = 56, kPxRegsSoft = 224, kPxRegsLaunch = 168;
 constexpr int kPxMaxSplits = 16;
-constexpr int kPxLd = kPxD + 4;                           // staged row: O, m, l
 static_assert(128 * kPxRegsIo + (kPxThreads - 128) * kPxRegsSoft <= kPxThreads * kPxRegsLaunch, "register split");
-static_assert(2 * kPxRows * kPxLd * 4 <= kPxOffQ, "staged rows over the ring");
+static_assert(2 * kPxRows * kPartLd * 4 <= kPxOffQ, "staged rows over the ring");
 static_assert(kPxSmem <= 227 * 1024, "shared memory per block");
 // TMEM columns: S (P over its first 64) of either stream, O of either
 constexpr int kPxTmS = 0, kPxTmO = 2 * kPxKeys, kPxTmCols = 512;
@@ -58,7 +55,6 @@ constexpr int kPxTmS = 0, kPxTmO = 2 * kPxKeys, kPxTmCols = 512;
 struct PrefixArgs {
   CUtensorMap kmap, vmap;   // [prefix_len][nkv][d] as (d, kv head, slot)
   BatchAttnArgs a;
-  int splits;
 };
 
 // A wait of at most kWaitLimitNs; false: it ran out here or elsewhere in the block
@@ -96,15 +92,15 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
   uint64_t* vfull = bar + 6;       // [2] transaction bytes
   uint64_t* vempty = bar + 8;      // [2] its P.V products done
   uint64_t* sfull = bar + 10;      // [2] scores of a stream done (and its P.V before them)
-  uint64_t* pfull = bar + 12;      // [2] four softmax warps: P written
-  uint64_t* pvdone = bar + 14;     // [2] P.V of a stream done
-  uint64_t* qready = bar + 16;     // eight warps: queries in shared memory
-  uint64_t* odone = bar + 17;      // both issuers: all products done
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 18);
+  uint64_t* pfull = bar + 12;      // [stream][key half] four softmax warps: P written
+  uint64_t* pvdone = bar + 16;     // [2] P.V of a stream done
+  uint64_t* qready = bar + 18;     // eight warps: queries in shared memory
+  uint64_t* odone = bar + 19;      // both issuers: all products done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 20);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const BatchAttnArgs& a = p.a;
   int32_t* status = a.status;
-  const int S = p.splits, split = blockIdx.x % S, pair = blockIdx.x / S, g = blockIdx.y;
+  const int S = a.p_splits, split = blockIdx.x % S, pair = blockIdx.x / S, g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row0 = pair * 2 * kPxRows;
   const int rows = min(2 * kPxRows, a.batch.n_tokens * a.group - row0);
@@ -123,7 +119,8 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
       mbar_init(&vfull[i], 1);
       mbar_init(&vempty[i], 1);
       mbar_init(&sfull[i], 1);
-      mbar_init(&pfull[i], 4);
+      mbar_init(&pfull[2 * i], 4);
+      mbar_init(&pfull[2 * i + 1], 4);
       mbar_init(&pvdone[i], 1);
     }
     mbar_init(qready, 8);
@@ -189,26 +186,24 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
       for (int u = 0; u < units; ++u) {
         const int i = u >> dual, st = i % kPxVStages, x = u & 1, use = u >> 1;
         if (!dual || x == 0) ok = px_wait(&vfull[st], (uint32_t)(i / kPxVStages) & 1u, abort_flag, status);
-        ok = ok && px_wait(&pfull[x], (uint32_t)use & 1u, abort_flag, status);
-        if (!ok) break;
-        tc_fence_after();
+        for (int h = 0; h < 2 && ok; ++h) {   // the first half's product runs under the second's exponentials
+          ok = px_wait(&pfull[2 * x + h], (uint32_t)use & 1u, abort_flag, status);
+          if (!ok) break;
+          tc_fence_after();
 #pragma unroll
-        for (int k = 0; k < kPxKeys / 16; ++k)
-          tc_mma_bf16_ts(tmem + kPxTmO + x * kPxD, tmem + kPxTmS + x * kPxKeys + 8 * k,
-                         vdesc + (uint64_t)((st * kPxTile + k * 16 * 128) >> 4), idesc, (k > 0 || use > 0) ? 1u : 0u);
+          for (int kk = 0; kk < 4; ++kk) {
+            const int k = 4 * h + kk;
+            tc_mma_bf16_ts(tmem + kPxTmO + x * kPxD, tmem + kPxTmS + x * kPxKeys + 8 * k,
+                           vdesc + (uint64_t)((st * kPxTile + k * 16 * 128) >> 4), idesc, (k > 0 || use > 0) ? 1u : 0u);
+          }
+        }
+        if (!ok) break;
         tc_commit(&pvdone[x]);
         if (!dual || x == 1) tc_commit(&vempty[st]);
       }
       tc_commit(odone);
     }
     __syncwarp();
-    tc_fence_before();
-    __syncthreads();   // rows staged
-    tc_fence_after();
-    cluster_arrive_release();
-    __syncwarp();
-    cluster_wait_acquire();
-    cluster_arrive_release();
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPxRegsSoft));
     // ------------------------------------------------------------ softmax: stream x, a thread per row
@@ -221,33 +216,37 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
     if (x == 0 || dual) {
       unsigned char* qs = sm + kPxOffQ + x * kPxTile;
       const int c = lane & 15;
-#pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
-        const int r = q4 * 32 + 2 * i + (lane >> 4);
-        const int row = row0 + x * kPxRows + r;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (x * kPxRows + r < rows) {
-          const uint16_t* q = (const uint16_t*)a.q + (long long)(row / a.group) * a.q_stride +
-                              (g * a.group + row % a.group) * kPxD + c * 8;
-          if (((uintptr_t)q & 15) == 0) {
-            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(q);
-          } else {
+      uint4 w[16];   // all rows' loads in flight: four at a time took 8 us
+      const uint16_t* q0 = (const uint16_t*)a.q + g * a.group * kPxD + c * 8;
+      const bool vec = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 15) == 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = (uint32_t)q[2 * e] | (uint32_t)q[2 * e + 1] << 16;
+      for (int i = 0; i < 16; ++i) {
+        const int r = x * kPxRows + q4 * 32 + 2 * i + (lane >> 4), row = row0 + r;
+        const uint16_t* q = q0 + (long long)(row / a.group) * a.q_stride + (row % a.group) * kPxD;
+        w[i] = make_uint4(0, 0, 0, 0);
+        if (r < rows) {
+          if (vec) {
+            w[i] = *reinterpret_cast<const uint4*>(q);
+          } else {
+            w[i] = make_uint4((uint32_t)q[0] | (uint32_t)q[1] << 16, (uint32_t)q[2] | (uint32_t)q[3] << 16,
+                              (uint32_t)q[4] | (uint32_t)q[5] << 16, (uint32_t)q[6] | (uint32_t)q[7] << 16);
           }
         }
-        if constexpr (CONVERT) {
-          float mx = 0.f;
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(w[e])), fabsf(bf16_hi(w[e]))));
+      for (int i = 0; i < 16; ++i) {
+        const int r = q4 * 32 + 2 * i + (lane >> 4);
+        if constexpr (CONVERT) {
+          float mx = fmaxf(fmaxf(fabsf(bf16_lo(w[i].x)), fabsf(bf16_hi(w[i].x))), fmaxf(fabsf(bf16_lo(w[i].y)), fabsf(bf16_hi(w[i].y))));
+          mx = fmaxf(mx, fmaxf(fmaxf(fabsf(bf16_lo(w[i].z)), fabsf(bf16_hi(w[i].z))), fmaxf(fabsf(bf16_lo(w[i].w)), fabsf(bf16_hi(w[i].w)))));
 #pragma unroll
           for (int s = 1; s < 16; s *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
           const int e2 = row_exponent(mx);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = scaled_half2(w[e], exp2i(-e2));
+          const float f = exp2i(-e2);
+          w[i] = make_uint4(scaled_half2(w[i].x, f), scaled_half2(w[i].y, f), scaled_half2(w[i].z, f), scaled_half2(w[i].w, f));
           if (c == 0) s_exp[x * kPxRows + r] = exp2i(e2);
         }
-        *reinterpret_cast<uint4*>(qs + (c >> 3) * kPxDBlock + sw128(r, c & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(qs + (c >> 3) * kPxDBlock + sw128(r, c & 7)) = w[i];
       }
       fence_async_smem();
     }
@@ -298,39 +297,41 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
         l *= f;
         if (move) m = tmax;
       }
-      // weights 2^(s sc - m); a row without a finite score yet has none
-      const bool live = m != -INFINITY;
-      const float neg = live ? -m : 0.f;
+      // weights 2^(s sc - m); without a finite score yet every score is -inf, and gives 0
+      const float neg = m == -INFINITY ? 0.f : -m;
       float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t pk[16];
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float p0 = live ? ex2_approx(fmaf(sv[32 * c + i], sc, neg)) : 0.f;
-          const float p1 = live ? ex2_approx(fmaf(sv[32 * c + i + 1], sc, neg)) : 0.f;
-          ps[(i >> 1) & 3] += p0 + p1;
-          if constexpr (F16) {
-            const __half2 v = __floats2half2_rn(p0, p1);
-            pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
-          } else {
-            const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
-            pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+        for (int c = 2 * h; c < 2 * h + 2; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float p0 = ex2_approx(fmaf(sv[32 * c + i], sc, neg)), p1 = ex2_approx(fmaf(sv[32 * c + i + 1], sc, neg));
+            ps[i & 2] += p0;
+            ps[(i & 2) + 1] += p1;
+            if constexpr (F16) {
+              const __half2 v = __floats2half2_rn(p0, p1);
+              pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+            } else {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+              pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+            }
           }
+          tmem_st16u(ts + 16 * c, pk);
         }
-        tmem_st16u(ts + 16 * c, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&pfull[2 * x + h]);
       }
       l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&pfull[x]);
     }
     // the ring and TMEM are free once all products are done (the issuer always says so)
     drain_wait(odone, 0);
     tc_fence_after();
     const bool have = mine > 0 && !*abort_flag;
-    float* row = stage + (size_t)(x * kPxRows + lrow) * kPxLd;
+    float* row = stage + (size_t)(x * kPxRows + lrow) * kPartLd;
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
       float ov[32];
@@ -342,134 +343,84 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
             have ? make_float4(ov[i], ov[i + 1], ov[i + 2], ov[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     *reinterpret_cast<float2*>(row + kPxD) = make_float2(have ? m : -INFINITY, have ? l : 0.f);
-    tc_fence_before();
-    __syncthreads();   // rows staged
-    tc_fence_after();
-    cluster_arrive_release();
-    __syncwarp();
-    cluster_wait_acquire();
-    // ------------------------------------------------------------ the rows' parts added up
-    // rows of the pair dealt to the cluster's blocks; with one row tile a block holds two parts
-    const int halves = dual ? 1 : 2;
-    const int lo = (int)((long long)rows * split / S), hi = (int)((long long)rows * (split + 1) / S);
-    join_rows<4>(
-        lo, hi, warp - kPxSoft0, 8, S * halves,
-        [&](int r, int i) { return ld_cluster2(dsmem_addr(stage + ((i % halves) * kPxRows + r) * kPxLd + kPxD, i / halves)); },
-        [&](int r, int i) {
-          return ld_cluster4(dsmem_addr(stage + ((i % halves) * kPxRows + r) * kPxLd + 4 * lane, i / halves));
-        },
-        [&](int r, float4 o, float top, float den) {
-          const int row = row0 + r;
-          const long long at = (long long)(row / a.group) * a.nq + g * a.group + row % a.group;
-          *reinterpret_cast<float4*>(a.part_o + at * kPxD + 4 * lane) = o;
-          if (lane == 0) a.part_ml[at] = make_float2(den == den ? top : den, den);   // a NaN stays one in the next join
-        });
-    cluster_arrive_release();
   }
-  __syncwarp();
-  cluster_wait_acquire();   // no peer reads this block's rows any more
   tc_fence_before();
-  __syncthreads();
+  __syncthreads();   // rows staged
   if (warp == 2) {
     tc_fence_after();
     tmem_dealloc(tmem, kPxTmCols);
   }
+  if (!dual && warp >= kPxSoft0) {   // both streams' sums of the same rows
+    for (int r = warp - kPxSoft0; r < rows; r += 8) {
+      float* ra = stage + r * kPartLd;
+      const float* rb = ra + kPxRows * kPartLd;
+      const float2 ma = *reinterpret_cast<const float2*>(ra + kPxD), mb = *reinterpret_cast<const float2*>(rb + kPxD);
+      const float top = max_nan(ma.x, mb.x);
+      const float wa = ma.x == -INFINITY ? 0.f : exp2f(ma.x - top), wb = mb.x == -INFINITY ? 0.f : exp2f(mb.x - top);
+      float4 va = *reinterpret_cast<const float4*>(ra + 4 * lane);
+      const float4 vb = *reinterpret_cast<const float4*>(rb + 4 * lane);
+      va = make_float4(va.x * wa + vb.x * wb, va.y * wa + vb.y * wb, va.z * wa + vb.z * wb, va.w * wa + vb.w * wb);
+      __syncwarp();
+      *reinterpret_cast<float4*>(ra + 4 * lane) = va;
+      if (lane == 0) *reinterpret_cast<float2*>(ra + kPxD) = make_float2(top, ma.y * wa + mb.y * wb);
+    }
+  }
+  fence_async_smem();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float* dst = a.part_o + (((long long)split * a.pages.nkv + g) * a.batch.n_tokens * a.group + row0) * kPartLd;
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_addr(stage)),
+                 "r"(rows * kPartLd * 4)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
 }
 
 // ---- host
-static cudaLaunchConfig_t px_config(dim3 grid, int splits, cudaLaunchAttribute* attr, cudaStream_t st) {
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = grid;
-  lc.blockDim = dim3(kPxThreads);
-  lc.dynamicSmemBytes = kPxSmem;
-  lc.stream = st;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = splits;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  lc.attrs = attr;
-  lc.numAttrs = 1;
-  return lc;
-}
-
 template <typename TQ, bool F16>
-static cudaError_t px_attributes() {
-  cudaError_t e = cudaFuncSetAttribute(k_attn_prefix<TQ, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPxSmem);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(k_attn_prefix<TQ, F16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+static cudaError_t launch_prefix(const PrefixArgs& p, dim3 grid, cudaStream_t st) {
   // the register split must not ask for more than the block is launched with
-  return e == cudaSuccess ? check_launch_regs((const void*)k_attn_prefix<TQ, F16>, kPxRegsLaunch) : e;
+  cudaError_t e = check_launch_regs((const void*)k_attn_prefix<TQ, F16>, kPxRegsLaunch);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(k_attn_prefix<TQ, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPxSmem);
+  return e == cudaSuccess ? launch(false, k_attn_prefix<TQ, F16>, grid, dim3(kPxThreads), kPxSmem, st, p) : e;
 }
 
-// What does not change while a process lives, of each device: that the kernels may use
-// their shared memory, and how many clusters of s blocks the device holds at once.
-struct PxDevice {
-  std::atomic<int> state{0};   // 1: ready
-  int clusters[kPxMaxSplits + 1] = {0};
-};
-static PxDevice* px_device() {
-  static PxDevice devices[64];
-  static std::mutex lock;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
-  PxDevice& d = devices[dev];
-  if (d.state.load(std::memory_order_acquire) == 1) return &d;
-  std::lock_guard<std::mutex> hold(lock);
-  if (d.state.load(std::memory_order_relaxed) == 1) return &d;
-  if (px_attributes<__nv_bfloat16, false>() != cudaSuccess || px_attributes<__nv_bfloat16, true>() != cudaSuccess ||
-      px_attributes<__half, true>() != cudaSuccess)
-    return nullptr;
-  for (int s = 1; s <= kPxMaxSplits; ++s) {
-    cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t lc = px_config(dim3(s), s, attr, nullptr);
-    int n = 0;
-    if (cudaOccupancyMaxActiveClusters(&n, (const void*)k_attn_prefix<__nv_bfloat16, false>, &lc) != cudaSuccess) n = 0;
-    cudaGetLastError();
-    d.clusters[s] = n;
-  }
-  d.state.store(1, std::memory_order_release);
-  return &d;
-}
-
-// The count of key ranges with the shortest schedule: waves of resident clusters, each
-// of a block's tiles and what a block costs besides (in units of a row tile's work on a
-// key tile, about 0.6 us).
-bool plan_prefix_tc(long long rows, int nkv, int prefix_len, PrefixPlan* p) {
-  const PxDevice* d = px_device();
-  if (!d) return false;
-  p->pairs = (int)((rows + 2 * kPxRows - 1) / (2 * kPxRows));
-  p->splits = 0;
-  const long long items = (long long)p->pairs * nkv;
+// The count of key ranges with the shortest schedule, in us: waves of one block per SM,
+// each of a block's tiles (about 0.7 per row tile) and its beginning and end (5), and
+// the parts, written and read once at about 8 bytes per ps.
+PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int n_sms) {
+  PrefixPlan p;
+  p.pairs = (int)((rows + 2 * kPxRows - 1) / (2 * kPxRows));
+  p.splits = 1;
+  const long long items = (long long)p.pairs * nkv;
   const int tiles = (prefix_len + kPxKeys - 1) / kPxKeys;
-  const double tile = rows > kPxRows ? 2.0 : 1.0;
+  const double tile = rows > kPxRows ? 1.4 : 0.7, part = 2.0 * rows * nkv * kPartLd * 4 / 8e6;
   double best = 0;
   for (int s = 1; s <= kPxMaxSplits && s <= tiles; ++s) {
-    if (d->clusters[s] < 1) continue;
-    const double cost = (double)((items + d->clusters[s] - 1) / d->clusters[s]) * (tile * ((tiles + s - 1) / s) + 6.0 + 0.2 * s);
-    if (p->splits == 0 || cost < best) {
-      best = cost;
-      p->splits = s;
-    }
+    const double cost = (double)((items * s + n_sms - 1) / n_sms) * (tile * ((tiles + s - 1) / s) + 5.0) + part * s;
+    if (s > 1 && cost >= best) continue;
+    best = cost;
+    p.splits = s;
   }
-  return p->splits > 0;
+  return p;
 }
 
 cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& plan, int dtype, int kv_dtype, cudaStream_t st) {
   PrefixArgs p;
   memset(&p, 0, sizeof(p));
   p.a = a;
-  p.splits = plan.splits;
   const uint64_t dims[3] = {(uint64_t)kPxD, (uint64_t)a.pages.nkv, (uint64_t)a.prefix_len};
   const uint64_t strides[2] = {(uint64_t)kPxD * 2, (uint64_t)a.pages.nkv * kPxD * 2};
   const uint32_t box[3] = {64, 1, (uint32_t)kPxKeys};
   const bool f16 = kv_dtype == OOS_DTYPE_F16;
   if (!encode_bf16_map(&p.kmap, a.pk, 3, dims, strides, box, f16) || !encode_bf16_map(&p.vmap, a.pv, 3, dims, strides, box, f16))
     return cudaErrorInvalidValue;
-  cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t lc = px_config(dim3((unsigned)(plan.pairs * plan.splits), a.pages.nkv), plan.splits, attr, st);
-  if (!f16) return cudaLaunchKernelEx(&lc, k_attn_prefix<__nv_bfloat16, false>, p);
-  if (dtype == OOS_DTYPE_BF16) return cudaLaunchKernelEx(&lc, k_attn_prefix<__nv_bfloat16, true>, p);
-  return cudaLaunchKernelEx(&lc, k_attn_prefix<__half, true>, p);
+  const dim3 grid((unsigned)(plan.pairs * plan.splits), a.pages.nkv);
+  if (!f16) return launch_prefix<__nv_bfloat16, false>(p, grid, st);
+  if (dtype == OOS_DTYPE_BF16) return launch_prefix<__nv_bfloat16, true>(p, grid, st);
+  return launch_prefix<__half, true>(p, grid, st);
 }
 
 }  // namespace oos
