@@ -108,10 +108,11 @@ OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int
 
 // ---- 16-bit types with heads of 128 (tensor cores)
 
-// Rows lo + warp, + n_warps, .. below hi, a warp per row and R rows at a time (their
-// loads in flight together: one row at a time, the join waited on each row's latency,
-// 2 us a row): part i of row r has (m, l) = ml_of(r, i), its four columns of this lane
-// v_of(r, i), i < parts <= 32.  out(r, O, max m, weighted l) takes the sum.
+// Rows lo + warp, + n_warps, .. below hi, a warp per row and R rows at a time: part i
+// of row r has (m, l) = ml_of(r, i), its four columns of this lane v_of(r, i), i < parts
+// <= 32.  out(r, O, max m, weighted l) takes the sum.  The first UNROLL parts' columns
+// are on their way before the weights are known: one row and one part at a time, the
+// join waited 2 us a row.
 template <int R, int UNROLL, typename ML, typename V, typename OUT>
 OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_of, V v_of, OUT out) {
   const int lane = threadIdx.x & 31;
@@ -119,13 +120,21 @@ OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_o
   for (int r0 = lo + warp; r0 < hi; r0 += R * n_warps) {
     float2 ml[R];
     float w[R], top[R], den[R];
-    float4 acc[R];
+    float4 acc[R], v[UNROLL][R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int r = r0 + k * n_warps;
       ml[k] = make_float2(-INFINITY, 0.f);
       if (r < hi && lane < parts) ml[k] = ml_of(r, lane);
     }
+    auto fetch = [&](int i0) {
+#pragma unroll
+      for (int i = 0; i < UNROLL; ++i)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+          if (i0 + i < parts) v[i][k] = v_of(min(r0 + k * n_warps, hi - 1), i0 + i);
+    };
+    fetch(0);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const bool on = ml[k].x != -INFINITY;   // a NaN is, and reaches the sum
@@ -136,18 +145,13 @@ OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_o
     }
 #pragma unroll 1
     for (int i0 = 0; i0 < parts; i0 += UNROLL) {
-      float4 v[UNROLL][R];
-#pragma unroll
-      for (int i = 0; i < UNROLL; ++i)
-#pragma unroll
-        for (int k = 0; k < R; ++k) v[i][k] = v_of(min(r0 + k * n_warps, hi - 1), min(i0 + i, parts - 1));
+      if (i0 > 0) fetch(i0);
 #pragma unroll
       for (int i = 0; i < UNROLL; ++i)
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-          float wi = __shfl_sync(0xffffffffu, w[k], (i0 + i) & 31);
-          if (i0 + i >= parts) wi = 0.f;
-          if (wi != 0.f) {   // a part without weight counts for nothing, whatever it holds
+          const float wi = __shfl_sync(0xffffffffu, w[k], (i0 + i) & 31);
+          if (i0 + i < parts && wi != 0.f) {   // a part without weight counts for nothing, whatever it holds
             acc[k].x += wi * v[i][k].x;
             acc[k].y += wi * v[i][k].y;
             acc[k].z += wi * v[i][k].z;
@@ -184,7 +188,7 @@ struct PrefixPlan {
 };
 PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int n_sms);
 struct PagesPlan {
-  bool wide;    // 64 rows per block, else 16
+  int tile_rows;   // of a block: 8 or 16 (decoding tokens), or 64
   int tiles, splits;
 };
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);

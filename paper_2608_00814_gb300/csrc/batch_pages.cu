@@ -26,13 +26,13 @@
 namespace oos {
 
 constexpr int kPgWarps = 4;
-__host__ __device__ constexpr int pg_stages(bool wide) { return 3; }
-__host__ __device__ constexpr int pg_blocks(bool wide) { return 2; }   // per SM
+constexpr int kWideStages = 3;
+__host__ __device__ constexpr int narrow_stages(int nt) { return nt == 1 ? 2 : 3; }
 constexpr int kPgD = 128;
 constexpr int kPgRow = 2 * kPgD;                 // bytes of a key row
 constexpr int kPgChunkBytes = 2 * 16 * kPgRow;   // 16 keys, K and V
-constexpr int pg_smem(bool wide) { return pg_stages(wide) * kPgWarps * kPgChunkBytes; }
-static_assert(64 * kPartLd * 4 <= pg_smem(false) && 64 * kPartLd * 4 <= pg_smem(true), "staged rows over the rings");
+constexpr int pg_smem(int stages) { return stages * kPgWarps * kPgChunkBytes; }
+static_assert(kPgWarps * 8 * kPartLd * 4 <= pg_smem(2) && kPgWarps * 16 * kPartLd * 4 <= pg_smem(3), "staged rows over the rings");
 
 OOS_DEV void cp_async16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -44,6 +44,17 @@ OOS_DEV uint32_t lds32(uint32_t addr) {
   uint32_t w;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(addr) : "memory");
   return w;
+}
+OOS_DEV uint32_t lds16(uint32_t addr) {
+  uint16_t w;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(addr) : "memory");
+  return w;
+}
+// an 8 x 8 block of 16-bit values, a row per four lanes, turned over its diagonal
+OOS_DEV uint32_t movmatrix_trans(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
 }
 OOS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -92,11 +103,350 @@ OOS_DEV bool chunk_not_finite(uint32_t buf, int pieces) {
   return __any_sync(0xffffffffu, bad != 0);
 }
 
-template <typename TQ, bool F16, bool WIDE>
-__global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
+// Keys by rows: S^T = K Q^T and O^T = V^T P^T, the keys (and then d) on the product's 16
+// rows and NT * 8 query rows on its columns, so that a decoding token's group of up to 8
+// heads costs one product of 8 columns where rows of 16 would cost two.
+template <typename TQ, bool F16, int NT>
+__global__ void __launch_bounds__(kPgWarps * 32, NT == 1 ? 3 : 2) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int ROWS = 8 * NT, STAGES = narrow_stages(NT);
+  constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
+  __shared__ TreeScratch s_tree;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = blockIdx.y, S = a.s_splits, split = blockIdx.x % S;
+  pdl_trigger();
+  TileRows t;
+  if (!sequence_tile(a, blockIdx.x / S, ROWS, &t)) {          // the whole cluster
+    if (blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();       // the grid must not end before the one it follows
+    return;
+  }
+  const unsigned long long (*anc)[2] = nullptr;
+  if (a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
+  const int last = (t.r0 + t.rows - 1) / a.group;
+  const int n_keys = anc ? t.len : max(0, min(t.len, t.first + last + 1));
+  const int units = (n_keys + 63) / 64;
+  const int k0 = (int)((long long)units * split / S) * 64;
+  const int k1 = min(n_keys, (int)((long long)units * (split + 1) / S) * 64);
+  const int n_chunks = max(0, k1 - k0 + 63) / 64;             // of 64 keys, 16 per warp
+
+  // ---- the first page lookups and the queries' loads go out together
+  auto slot_of = [&](int c) -> long long {   // lane & 15: a key of this warp's 16 in chunk c
+    const int key = k0 + c * 64 + warp * 16 + (lane & 15);
+    if (c >= n_chunks || key >= k1) return -1;
+    const long long at = page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
+    if (at < 0) *a.status = OOS_EBATCH;
+    return at;
+  };
+  long long slot[STAGES];
+#pragma unroll
+  for (int c = 0; c < STAGES; ++c) slot[c] = slot_of(c);
+  // B fragments of the query rows, all of d: column lane / 4 of each 8 rows
+  uint32_t qf[8][NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = 8 * n + (lane >> 2), row = t.r0 + r;
+    const bool on = r < t.rows;
+    const uint16_t* q = (const uint16_t*)a.q + (long long)(t.q0 + (on ? row / a.group : 0)) * a.q_stride +
+                        (g * a.group + row % a.group) * kPgD + (lane & 3) * 2;
+    const bool pairs = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 3) == 0;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint16_t* p = q + kk * 16 + e * 8;
+        uint32_t x = 0;
+        if (on) x = pairs ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)p[0] | (uint32_t)p[1] << 16;
+        qf[kk][n][e] = x;
+      }
+  }
+
+  // ---- copies: this warp's keys of chunk c into its own ring
+  const uint32_t ring = smem_addr(smem) + warp * (STAGES * kPgChunkBytes);
+  const long long key_bytes = (long long)a.pages.nkv * kPgRow;
+  const uint8_t* kg = a.pages.k + (long long)g * kPgRow + (lane & 15) * 16;
+  const uint8_t* vg = a.pages.v + (long long)g * kPgRow + (lane & 15) * 16;
+  auto copy = [&](int c, long long at_lane) {
+    if (c < n_chunks) {
+      const uint32_t dst = ring + (c % STAGES) * kPgChunkBytes;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = 2 * i + (lane >> 4);
+        const long long at = __shfl_sync(0xffffffffu, at_lane, key);
+        const uint32_t o = key * kPgRow + (((lane & 15) ^ (key & 7)) << 4);
+        const bool ok = at >= 0;
+        const long long off = ok ? at * key_bytes : 0;
+        cp_async16(dst + o, kg + off, ok);
+        cp_async16(dst + 16 * kPgRow + o, vg + off, ok);
+      }
+    }
+    cp_async_commit();
+  };
+  uint32_t valid[STAGES];   // keys that are there, of the chunks on their way
+#pragma unroll
+  for (int c = 0; c < STAGES - 1; ++c) {
+    copy(c, slot[c]);
+    valid[c] = __ballot_sync(0xffffffffu, slot[c] >= 0) & 0xffffu;
+  }
+  long long next = slot[STAGES - 1];   // looked up a chunk ahead
+
+  // a column's two rows of this thread: 8 n + 2 (lane & 3) + e
+  float sc[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float p2 = 1.f;
+    if constexpr (CONVERT) {
+      float mx = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(qf[kk][n][e])), fabsf(bf16_hi(qf[kk][n][e]))));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const int e2 = row_exponent(mx);
+      p2 = exp2i(e2);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) qf[kk][n][e] = scaled_half2(qf[kk][n][e], exp2i(-e2));
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) sc[n][e] = a.scale_log2 * __shfl_sync(0xffffffffu, p2, ((lane & 3) * 2 + e) * 4);
+  }
+  int token[NT][2];
+  unsigned long long an[NT][2][2] = {};
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 8 * n + (lane & 3) * 2 + e;
+      token[n][e] = (t.r0 + r) / a.group;
+      if (anc && r < t.rows) {
+        an[n][e][0] = anc[token[n][e]][0];
+        an[n][e][1] = anc[token[n][e]][1];
+      }
+    }
+  const int tok_lo = t.r0 / a.group, tok_hi = last;
+
+  float o[8][NT][4], m[NT][2], l[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      m[n][e] = -INFINITY;
+      l[n][e] = 0.f;
+    }
+  }
+  // ldmatrix rows of this lane: K as it lies, V transposed on the way
+  const uint32_t a_key = (lane & 7) + ((lane >> 3) & 1) * 8, a_chunk = lane >> 4;
+  const uint32_t v_key = (lane & 7) + (lane >> 4) * 8, v_chunk = (lane >> 3) & 1;
+
+#pragma unroll 1
+  for (int c = 0; c < n_chunks; ++c) {
+    cp_async_wait<STAGES - 2>();
+    __syncwarp();
+    const uint32_t there = valid[0];
+#pragma unroll
+    for (int i = 0; i + 2 < STAGES; ++i) valid[i] = valid[i + 1];
+    copy(c + STAGES - 1, next);
+    valid[STAGES - 2] = __ballot_sync(0xffffffffu, next >= 0) & 0xffffu;
+    next = slot_of(c + STAGES);
+    const int key0 = k0 + c * 64 + warp * 16;
+    // nothing there, or no row that sees the first key (warp-uniform)
+    if (there == 0 || (!anc && key0 > t.first + tok_hi)) continue;
+    const uint32_t buf = ring + (c % STAGES) * kPgChunkBytes;
+    float s[NT][4], s2[NT][4];   // even and odd steps of d apart: half as long a chain of products
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[n][e] = s2[n][e] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      uint32_t k4[4];
+      ldsm4(buf + a_key * kPgRow + (((2 * kk + a_chunk) ^ (a_key & 7)) << 4), k4);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) mma16816<F16>(kk & 1 ? s2[n] : s[n], k4, qf[kk][n][0], qf[kk][n][1]);
+    }
+    // keys of the chunk that each of this thread's rows sees
+    const int seen = t.first - key0;   // those before it are committed
+    const bool full = there == 0xffffu && (anc ? seen : seen + tok_lo + 1) >= 16;
+    uint32_t bits[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        bits[n][e] = 0xffffu;
+        if (!full) {
+          const int lead = max(0, min(16, anc ? seen : seen + token[n][e] + 1));
+          uint32_t b = (1u << lead) - 1;
+          if (anc) {
+            unsigned long long lo, hi;
+            if (seen >= 0) shl128(an[n][e][0], an[n][e][1], min(seen, 128), lo, hi);
+            else shr128(an[n][e][0], an[n][e][1], min(-seen, 128), lo, hi);
+            b |= (uint32_t)lo;
+          }
+          bits[n][e] = b & there;
+        }
+      }
+    // A key that some of the rows do not see must not reach them through 0 times a v
+    // that is not finite: such a chunk (the last ones of a sequence only) is summed apart.
+    const bool apart = !full && chunk_not_finite<F16>(buf, 1);
+    bool move = false;
+    float mn[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        s[n][e] += s2[n][e];
+        s[n][2 + e] += s2[n][2 + e];
+        if (!full) {
+          if (!((bits[n][e] >> (lane >> 2)) & 1)) s[n][e] = -INFINITY;
+          if (!((bits[n][e] >> (8 + (lane >> 2))) & 1)) s[n][2 + e] = -INFINITY;
+        }
+        float mx = max_nan(s[n][e], s[n][2 + e]);
+        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 16)) * sc[n][e];
+        mn[n][e] = !(mx <= m[n][e] + 8.f) ? mx : m[n][e];   // a NaN moves it, and stays
+        move = move || mn[n][e] != m[n][e];
+      }
+    if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float f = m[n][e] == mn[n][e] ? 1.f : m[n][e] == -INFINITY ? 0.f : exp2f(m[n][e] - mn[n][e]);
+          l[n][e] *= f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            o[i][n][e] *= f;
+            o[i][n][2 + e] *= f;
+          }
+          m[n][e] = mn[n][e];
+        }
+    }
+    // weights, and as B fragments: an 8 x 8 block of (key, row) turned to (row, key)
+    uint32_t pf[NT][2], pl[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      // without a finite score yet every score is -inf, and gives 0
+      const float neg[2] = {m[n][0] == -INFINITY ? 0.f : -m[n][0], m[n][1] == -INFINITY ? 0.f : -m[n][1]};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = ex2_approx(fmaf(s[n][2 * h], sc[n][0], neg[0])), p1 = ex2_approx(fmaf(s[n][2 * h + 1], sc[n][1], neg[1]));
+        s[n][2 * h] = p0;
+        s[n][2 * h + 1] = p1;
+        l[n][0] += p0;
+        l[n][1] += p1;
+        if constexpr (F16) {
+          const __half2 v = __floats2half2_rn(p0, p1);
+          pf[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&v));
+        } else {
+          const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+          const __nv_bfloat162 r = __floats2bfloat162_rn(p0 - __low2float(v), p1 - __high2float(v));
+          pf[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&v));
+          pl[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&r));
+        }
+      }
+    }
+    if (apart) {
+#pragma unroll 1
+      for (int key = 0; key < 16; ++key)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float mine = key & 8 ? s[n][2 + e] : s[n][e];
+            const float p = __shfl_sync(0xffffffffu, mine, (key & 7) * 4 + (lane & 3));
+            if (!((bits[n][e] >> key) & 1)) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t w = lds16(buf + (16 + key) * kPgRow + ((((2 * i + h)) ^ (key & 7)) << 4) + (lane >> 2) * 2);
+                o[i][n][2 * h + e] += p * (F16 ? __half2float(__ushort_as_half((unsigned short)w)) : bf16_lo(w));
+              }
+          }
+      continue;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t v4[4];
+      ldsm4_trans(buf + (16 + v_key) * kPgRow + (((2 * i + v_chunk) ^ (v_key & 7)) << 4), v4);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        mma16816<F16>(o[i][n], v4, pf[n][0], pf[n][1]);
+        if constexpr (!F16) mma16816<F16>(o[i][n], v4, pl[n][0], pl[n][1]);
+      }
+    }
+  }
+  cp_async_wait<0>();
+  __syncthreads();
+  // ---- join: O rows with (m, l), staged over the rings, of every warp and every block of
+  // the cluster, and the prefix's parts; at most 32
+  float* stage = reinterpret_cast<float*>(smem);   // [warp][row][kPartLd]
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int x = 4; x < 32; x *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], x);
+      float* row = stage + (warp * ROWS + 8 * n + (lane & 3) * 2 + e) * kPartLd;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) row[16 * i + 8 * h + (lane >> 2)] = o[i][n][2 * h + e];
+      if (lane < 4) *reinterpret_cast<float2*>(row + kPgD) = make_float2(m[n][e], l[n][e]);
+    }
+  pdl_wait();   // the prefix's parts
+  __syncthreads();
+  if (S > 1) {
+    cluster_arrive_release();
+    cluster_wait_acquire();
+  }
+  const int own = kPgWarps * S;
+  const long long part_rows = (long long)a.batch.n_tokens * a.group, part_step = (long long)a.pages.nkv * part_rows * kPartLd;
+  auto part = [&](int r, int i) {   // part i of row r: a staged one (its address in this block), or the prefix's
+    return i < own ? stage + ((i % kPgWarps) * ROWS + r) * kPartLd
+                   : a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0 + r) * kPartLd + (i - own) * part_step;
+  };
+  join_rows<1, 20>(
+      t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + a.p_splits,
+      [&](int r, int i) {
+        const float* p = part(r, i) + kPgD;
+        return i < own && S > 1 ? ld_cluster2(dsmem_addr(p, i / kPgWarps)) : *reinterpret_cast<const float2*>(p);
+      },
+      [&](int r, int i) {
+        const float* p = part(r, i) + 4 * lane;
+        return i < own && S > 1 ? ld_cluster4(dsmem_addr(p, i / kPgWarps)) : *reinterpret_cast<const float4*>(p);
+      },
+      [&](int r, float4 x, float, float den) {
+        const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
+        const float v[4] = {x.x * f, x.y * f, x.z * f, x.w * f};
+        const int row = t.r0 + r;
+        TQ* out = (TQ*)a.out + (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kPgD + 4 * lane;
+        if (((uintptr_t)out & 7) == 0) {
+          store_vec<TQ, 4>(out, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[e] = from_f32<TQ>(v[e]);
+        }
+      });
+  if (S > 1) {   // a peer may still read this block's rows
+    cluster_arrive_release();
+    cluster_wait_acquire();
+  }
+}
+
+template <typename TQ, bool F16>
+__global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages_wide(const __grid_constant__ BatchAttnArgs a) {
+  constexpr bool WIDE = true;
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int ROWS = WIDE ? 64 : 16, KC = WIDE ? 64 : 16;   // rows of the block, keys a warp takes at once
-  constexpr int STAGES = pg_stages(WIDE);
+  constexpr int STAGES = kWideStages;
   constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
   __shared__ TreeScratch s_tree;
   __shared__ uint32_t s_valid[STAGES][kPgWarps];           // keys of a chunk that are there
@@ -117,7 +467,18 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(c
   const int k1 = min(n_keys, (int)((long long)units * (split + 1) / S) * 64);
   const int n_chunks = max(0, k1 - k0 + 63) / 64;             // of 64 keys: one per warp each, or one for all
 
-  // ---- queries: the loads go out first, over the page lookups that follow
+  // ---- the first page lookups and the queries' loads go out together
+  const uint32_t ring = smem_addr(smem);
+  auto slot_of = [&](int c) -> long long {   // lane & 15: a key of this warp's 16 in 64-key chunk c
+    const int key = k0 + c * 64 + warp * 16 + (lane & 15);
+    if (c >= n_chunks || key >= k1) return -1;
+    const long long at = page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
+    if (at < 0) *a.status = OOS_EBATCH;
+    return at;
+  };
+  long long slot[STAGES];   // of the chunks up to the next one to be copied
+#pragma unroll
+  for (int c = 0; c < STAGES; ++c) slot[c] = slot_of(c);
   const int row0 = WIDE ? warp * 16 : 0;          // rows of the tile
   const int rr[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
   int token[2];
@@ -141,19 +502,11 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(c
       }
   }
 
-  // ---- copies: this warp's 16 keys of 64-key chunk c (narrow: its own chunk)
-  const uint32_t ring = smem_addr(smem);
-  auto slot_of = [&](int c) -> long long {   // lane & 15: a key
-    const int key = k0 + c * 64 + warp * 16 + (lane & 15);
-    if (c >= n_chunks || key >= k1) return -1;
-    const long long at = page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
-    if (at < 0) *a.status = OOS_EBATCH;
-    return at;
-  };
+  // ---- copies
   const long long key_bytes = (long long)a.pages.nkv * kPgRow;
   const uint8_t* kg = a.pages.k + (long long)g * kPgRow + (lane & 15) * 16;
   const uint8_t* vg = a.pages.v + (long long)g * kPgRow + (lane & 15) * 16;
-  auto copy = [&](int c, long long slot) {
+  auto copy = [&](int c, long long slot) {   // this warp's keys of chunk c
     const int st = c % STAGES;
     const uint32_t dst = ring + (st * kPgWarps + warp) * kPgChunkBytes;
     if (c < n_chunks) {
@@ -172,13 +525,9 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(c
     }
     cp_async_commit();
   };
-  {
-    long long slot[STAGES - 1];
 #pragma unroll
-    for (int c = 0; c < STAGES - 1; ++c) slot[c] = slot_of(c);
-#pragma unroll
-    for (int c = 0; c < STAGES - 1; ++c) copy(c, slot[c]);
-  }
+  for (int c = 0; c < STAGES - 1; ++c) copy(c, slot[c]);
+  long long next = slot[STAGES - 1];   // looked up a chunk ahead
 
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -222,12 +571,12 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(c
   const uint32_t v_key = (((lane >> 3) & 1) << 3) + (lane & 7), v_chunk = lane >> 4;
 
   for (int c = 0; c < n_chunks; ++c) {
-    const long long next = slot_of(c + STAGES - 1);
     cp_async_wait<STAGES - 2>();
     if (WIDE) __syncthreads();   // every warp's keys are there, and the stage before is free
     else __syncwarp();
     const int st = c % STAGES;
     copy(c + STAGES - 1, next);
+    next = slot_of(c + STAGES);
     unsigned long long valid;
     if (WIDE) {
       valid = 0;
@@ -471,7 +820,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(c
   constexpr int LOCAL = WIDE ? 1 : kPgWarps;
   const int own = LOCAL * S;
   auto staged = [&](int r, int i) { return stage + ((WIDE ? 0 : i % LOCAL) * 16 + r) * kPartLd; };
-  join_rows<WIDE ? 4 : 1, WIDE ? 2 : 8>(
+  join_rows<WIDE ? 4 : 1, WIDE ? 2 : 20>(
       t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + n_pre,
       [&](int r, int i) {
         if (i >= own) return *reinterpret_cast<const float2*>(prefix_row(r) + (i - own) * part_step + kPgD);
@@ -502,8 +851,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(WIDE)) k_attn_pages(c
 
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms) {
   PagesPlan p;
-  p.wide = rows > 16ll * n_seqs;
-  p.tiles = (int)(n_seqs + rows / (p.wide ? 64 : 16));
+  p.tile_rows = rows <= 8ll * n_seqs ? 8 : rows <= 16ll * n_seqs ? 16 : 64;
+  p.tiles = (int)(n_seqs + rows / p.tile_rows);
   // blocks for every SM twice, each with 128 keys at least; a cluster holds 4 ranges
   // (their parts and the prefix's fit the join's 32 lanes)
   const long long want = 4ll * n_sms / std::max(1ll, (long long)p.tiles * nkv);
@@ -511,14 +860,13 @@ PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys
   return p;
 }
 
-template <typename TQ, bool F16, bool WIDE>
-static cudaError_t launch_pages(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(k_attn_pages<TQ, F16, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, pg_smem(WIDE));
+static cudaError_t launch_pages(const void* kernel, int smem, const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(p.tiles * p.splits), a.pages.nkv);
   lc.blockDim = dim3(kPgWarps * 32);
-  lc.dynamicSmemBytes = pg_smem(WIDE);
+  lc.dynamicSmemBytes = smem;
   lc.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;
@@ -534,15 +882,21 @@ static cudaError_t launch_pages(const BatchAttnArgs& a, const PagesPlan& p, cuda
   }
   lc.attrs = attr;
   lc.numAttrs = n;
-  return cudaLaunchKernelEx(&lc, k_attn_pages<TQ, F16, WIDE>, a);
+  void* args[1] = {const_cast<BatchAttnArgs*>(&a)};
+  return cudaLaunchKernelExC(&lc, kernel, args);
+}
+
+template <typename TQ, bool F16>
+static cudaError_t launch_pages_of(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
+  if (p.tile_rows == 8) return launch_pages((const void*)k_attn_pages<TQ, F16, 1>, pg_smem(narrow_stages(1)), a, p, st);
+  if (p.tile_rows == 16) return launch_pages((const void*)k_attn_pages<TQ, F16, 2>, pg_smem(narrow_stages(2)), a, p, st);
+  return launch_pages((const void*)k_attn_pages_wide<TQ, F16>, pg_smem(kWideStages), a, p, st);
 }
 
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st) {
-  if (kv_dtype == OOS_DTYPE_BF16)
-    return p.wide ? launch_pages<__nv_bfloat16, false, true>(a, p, st) : launch_pages<__nv_bfloat16, false, false>(a, p, st);
-  if (dtype == OOS_DTYPE_BF16)
-    return p.wide ? launch_pages<__nv_bfloat16, true, true>(a, p, st) : launch_pages<__nv_bfloat16, true, false>(a, p, st);
-  return p.wide ? launch_pages<__half, true, true>(a, p, st) : launch_pages<__half, true, false>(a, p, st);
+  if (kv_dtype == OOS_DTYPE_BF16) return launch_pages_of<__nv_bfloat16, false>(a, p, st);
+  if (dtype == OOS_DTYPE_BF16) return launch_pages_of<__nv_bfloat16, true>(a, p, st);
+  return launch_pages_of<__half, true>(a, p, st);
 }
 
 }  // namespace oos
