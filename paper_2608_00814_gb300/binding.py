@@ -344,8 +344,11 @@ def oos_status_string(code):
 
 # ---- batch operators.  What C cannot see of a tensor -- its type, shape, strides
 # and device -- is checked here and answered like C's own refusals, by OosError.
+# These calls are short on the GPU, so the checks are kept to a few attribute reads.
 
 _DTYPES = {torch.float32: OOS_DTYPE_F32, torch.bfloat16: OOS_DTYPE_BF16, torch.float16: OOS_DTYPE_F16}
+_I32 = torch.int32
+_raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # a tenth of current_stream()'s time
 
 
 def _require(ok, what):
@@ -353,27 +356,37 @@ def _require(ok, what):
         raise OosError(OOS_EINVAL, what)
 
 
-def _dense(t, dtype, shape, device, what):
-    """Address of a contiguous device tensor; None for None."""
+def _dense(t, dtype, shape, dev, what):
+    """Address of a contiguous tensor on device `dev`; None for None."""
     if t is None:
         return None
-    _require(t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous(), what)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise OosError(OOS_EINVAL, what)
     return t.data_ptr()
 
 
-def _head_rows(t, dtype, n, heads, d, device, what):
+def _head_rows(t, dtype, n, heads, d, dev, what):
     """Address and token stride of rows [n, heads, d] whose heads are contiguous."""
-    _require(t.dtype is dtype and t.shape == (n, heads, d) and t.device == device, what)
+    if t.dtype is not dtype or t.shape != (n, heads, d) or t.get_device() != dev:
+        raise OosError(OOS_EINVAL, what)
     s0, s1, s2 = t.stride()
-    _require((s2 == 1 or d == 1) and (s1 == d or heads == 1), what)
+    if (s2 != 1 and d != 1) or (s1 != d and heads != 1):
+        raise OosError(OOS_EINVAL, what)
     return t.data_ptr(), s0 if n > 1 else heads * d
 
 
 def _here(t, what):
     """The device of `t`, which must be the current one: the library launches there."""
-    dev = t.device
-    _require(dev.type == "cuda" and dev.index == torch.cuda.current_device(), what)
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise OosError(OOS_EINVAL, what)
     return dev
+
+
+def _raw_stream(stream, dev):
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_current_stream(dev) if _raw_current_stream else torch.cuda.current_stream().cuda_stream
 
 
 class PagedCache:
@@ -384,8 +397,9 @@ class PagedCache:
         _require(v.dtype is k.dtype and v.shape == k.shape and v.is_contiguous() and v.device == k.device,
                  "PagedCache: v")
         self.k, self.v = k, v
-        self.device = k.device
+        self.dev = k.get_device()
         n_pages, page_size, nkv, d = k.shape
+        self.heads, self.d = nkv, d
         self.c = OosPagedCache(_DTYPES[k.dtype], nkv, d, page_size, n_pages, k.data_ptr(), v.data_ptr())
         self.ref = ctypes.byref(self.c)
 
@@ -402,9 +416,8 @@ class Batch:
     def __init__(self, q_start, seq_len, block_table, n_tokens):
         _require(block_table.dim() == 2, "Batch: block_table")
         B, width = block_table.shape
-        dev = block_table.device
-        _require(dev.type == "cuda", "Batch: block_table")
-        self.device = dev
+        dev = self.dev = block_table.get_device()
+        _require(dev >= 0, "Batch: block_table")
         self.q_start, self.seq_len, self.block_table, self.n_tokens = q_start, seq_len, block_table, int(n_tokens)
         i32 = torch.int32
         self.c = OosBatch(B, self.n_tokens, width, _dense(q_start, i32, (B + 1,), dev, "Batch: q_start"),
@@ -415,48 +428,42 @@ class Batch:
 
 def oos_qk_norm_rope(q, k, q_norm, k_norm, eps, rope, positions, q_out, k_out, stream=None):
     """q [n, nq, d] and k [n, nkv, d] (either None), rows any stride apart; q_out / k_out may be q / k."""
-    x = q if q is not None else k
+    x = k if q is None else q
     _require(x is not None and x.dim() == 3 and x.dtype in _DTYPES, "oos_qk_norm_rope: q, k")
     dt, dev = x.dtype, _here(x, "oos_qk_norm_rope: device")
     n, _, d = x.shape
-    args = []
-    heads = [0, 0]
-    outs = []
-    for i, (a, o, name) in enumerate(((q, q_out, "q"), (k, k_out, "k"))):
-        if a is None:
-            args += [None, 0]
-            outs += [None, 0]
-            continue
-        _require(a.dim() == 3 and o is not None, "oos_qk_norm_rope: " + name)
-        heads[i] = a.shape[1]
-        args += _head_rows(a, dt, n, heads[i], d, dev, "oos_qk_norm_rope: " + name)
-        outs += _head_rows(o, dt, n, heads[i], d, dev, "oos_qk_norm_rope: %s_out" % name)
-    _check(lib().oos_qk_norm_rope(_DTYPES[dt], n, heads[0], heads[1], d, *args,
-                                  _dense(q_norm, dt, (d,), dev, "oos_qk_norm_rope: q_norm"),
-                                  _dense(k_norm, dt, (d,), dev, "oos_qk_norm_rope: k_norm"), eps,
-                                  None if rope is None else ctypes.byref(rope),
-                                  _dense(positions, torch.int32, (n,), dev, "oos_qk_norm_rope: positions"), *outs,
-                                  _raw_stream(stream)), "oos_qk_norm_rope")
-
-
-def _raw_stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    qp = kp = qop = kop = None
+    nq = nkv = qs = ks = qos = kos = 0
+    if q is not None:
+        _require(q_out is not None, "oos_qk_norm_rope: q_out")
+        nq = q.shape[1]
+        qp, qs = _head_rows(q, dt, n, nq, d, dev, "oos_qk_norm_rope: q")
+        qop, qos = _head_rows(q_out, dt, n, nq, d, dev, "oos_qk_norm_rope: q_out")
+    if k is not None:
+        _require(k_out is not None and k.dim() == 3, "oos_qk_norm_rope: k, k_out")
+        nkv = k.shape[1]
+        kp, ks = _head_rows(k, dt, n, nkv, d, dev, "oos_qk_norm_rope: k")
+        kop, kos = _head_rows(k_out, dt, n, nkv, d, dev, "oos_qk_norm_rope: k_out")
+    code = (_lib or lib()).oos_qk_norm_rope(
+        _DTYPES[dt], n, nq, nkv, d, qp, qs, kp, ks, _dense(q_norm, dt, (d,), dev, "oos_qk_norm_rope: q_norm"),
+        _dense(k_norm, dt, (d,), dev, "oos_qk_norm_rope: k_norm"), eps, rope,
+        _dense(positions, _I32, (n,), dev, "oos_qk_norm_rope: positions"), qop, qos, kop, kos, _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, "oos_qk_norm_rope")
 
 
 def oos_paged_append(cache, batch, k, v, k_norm, eps, rope, positions, out_status, stream=None):
     """k, v: [batch.n_tokens, nkv, d] rows, any stride apart; positions: int32 [n_tokens]; out_status: int32 [1]."""
-    _require(k.dtype in _DTYPES, "oos_paged_append: k")
-    dt, dev, n = k.dtype, _here(k, "oos_paged_append: device"), batch.n_tokens
-    nkv, d = cache.c.n_kv_heads, cache.c.head_dim
-    _require(cache.device == dev and batch.device == dev, "oos_paged_append: device")
+    dt, dev, n, nkv, d = k.dtype, _here(k, "oos_paged_append: device"), batch.n_tokens, cache.heads, cache.d
+    _require(dt in _DTYPES and cache.dev == dev and batch.dev == dev, "oos_paged_append: k, device")
     kp, ks = _head_rows(k, dt, n, nkv, d, dev, "oos_paged_append: k")
     vp, vs = _head_rows(v, dt, n, nkv, d, dev, "oos_paged_append: v")
-    _check(lib().oos_paged_append(cache.ref, batch.ref, _DTYPES[dt], kp, ks, vp, vs,
-                                  _dense(k_norm, dt, (d,), dev, "oos_paged_append: k_norm"), eps,
-                                  None if rope is None else ctypes.byref(rope),
-                                  _dense(positions, torch.int32, (n,), dev, "oos_paged_append: positions"),
-                                  _dense(out_status, torch.int32, (1,), dev, "oos_paged_append: out_status"),
-                                  _raw_stream(stream)), "oos_paged_append")
+    code = (_lib or lib()).oos_paged_append(
+        cache.ref, batch.ref, _DTYPES[dt], kp, ks, vp, vs, _dense(k_norm, dt, (d,), dev, "oos_paged_append: k_norm"),
+        eps, rope, _dense(positions, _I32, (n,), dev, "oos_paged_append: positions"),
+        _dense(out_status, _I32, (1,), dev, "oos_paged_append: out_status"), _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, "oos_paged_append")
 
 
 def oos_shared_prefix_attention_workspace_bytes(q, prefix_len, cache, batch):
@@ -468,28 +475,29 @@ def oos_shared_prefix_attention(q, prefix_k, prefix_v, prefix_len, cache, batch,
     """q, out: [batch.n_tokens, nq, d] rows, any stride apart; prefix_k / prefix_v: one layer of a KVCache
     ([capacity, nkv, d], capacity >= prefix_len; None with prefix_len 0); tree_parent: int32 [n_tokens] or None;
     workspace: uint8; out_status: int32 [1]."""
-    name = "oos_shared_prefix_attention"
-    _require(q.dim() == 3 and q.dtype in _DTYPES, name + ": q")
-    dt, dev, n = q.dtype, _here(q, name + ": device"), batch.n_tokens
-    nkv, d = cache.c.n_kv_heads, cache.c.head_dim
-    _require(cache.device == dev and batch.device == dev and workspace.device == dev, name + ": device")
-    nq = q.shape[1]
-    qp, qs = _head_rows(q, dt, n, nq, d, dev, name + ": q")
-    op, os_ = _head_rows(out, dt, n, nq, d, dev, name + ": out")
+    _require(q.dim() == 3 and q.dtype in _DTYPES, "oos_shared_prefix_attention: q")
+    dt, dev, n = q.dtype, _here(q, "oos_shared_prefix_attention: device"), batch.n_tokens
+    nkv, d, nq = cache.heads, cache.d, q.shape[1]
+    _require(cache.dev == dev and batch.dev == dev and workspace.get_device() == dev and workspace.is_contiguous(),
+             "oos_shared_prefix_attention: device, workspace")
+    qp, qs = _head_rows(q, dt, n, nq, d, dev, "oos_shared_prefix_attention: q")
+    op, os_ = _head_rows(out, dt, n, nq, d, dev, "oos_shared_prefix_attention: out")
     pk = pv = None
     if prefix_len > 0:
-        _require(prefix_k is not None and prefix_v is not None and prefix_k.dim() == 3, name + ": prefix_k, prefix_v")
+        _require(prefix_k is not None and prefix_v is not None, "oos_shared_prefix_attention: prefix_k, prefix_v")
         shape = prefix_k.shape
-        _require(shape[0] >= prefix_len and shape[1] == nkv and shape[2] == d, name + ": prefix_k")
-        pk = _dense(prefix_k, cache.k.dtype, shape, dev, name + ": prefix_k")
-        pv = _dense(prefix_v, cache.k.dtype, shape, dev, name + ": prefix_v")
-    _require(workspace.is_contiguous(), name + ": workspace")
-    _check(lib().oos_shared_prefix_attention(_DTYPES[dt], nq, qp, qs, pk, pv, prefix_len, cache.ref, batch.ref,
-                                             _dense(tree_parent, torch.int32, (n,), dev, name + ": tree_parent"),
-                                             scale, op, os_, workspace.data_ptr(),
-                                             workspace.numel() * workspace.element_size(),
-                                             _dense(out_status, torch.int32, (1,), dev, name + ": out_status"),
-                                             _raw_stream(stream)), name)
+        _require(len(shape) == 3 and shape[0] >= prefix_len and shape[1] == nkv and shape[2] == d,
+                 "oos_shared_prefix_attention: prefix_k")
+        kv = cache.k.dtype
+        pk = _dense(prefix_k, kv, shape, dev, "oos_shared_prefix_attention: prefix_k")
+        pv = _dense(prefix_v, kv, shape, dev, "oos_shared_prefix_attention: prefix_v")
+    code = (_lib or lib()).oos_shared_prefix_attention(
+        _DTYPES[dt], nq, qp, qs, pk, pv, prefix_len, cache.ref, batch.ref,
+        _dense(tree_parent, _I32, (n,), dev, "oos_shared_prefix_attention: tree_parent"), scale, op, os_,
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _dense(out_status, _I32, (1,), dev, "oos_shared_prefix_attention: out_status"), _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, "oos_shared_prefix_attention")
 
 
 class VerifyOutputs:

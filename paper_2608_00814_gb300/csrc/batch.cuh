@@ -2,6 +2,8 @@
 // step's ragged rows, and the host's checks of both.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 #include "internal.h"
 
@@ -31,8 +33,11 @@ struct BatchView {
 bool rope_ok(const oos_rope_config* r);
 bool pages_ok(const oos_paged_cache* c);
 bool batch_ok(const oos_batch* b);
-// false: a rate is not a number
-void rope_turns(const oos_rope_config& r, int d, RopeTurns* out);
+const RopeTurns& rope_turns(const oos_rope_config& r, int d);
+int device_sms();   // of the current device, 0 without one
+// Once per kernel and device: its shared memory (and, of a kernel that splits its
+// registers, that it was compiled for as many as the split takes).  ready: a bit per device
+cudaError_t kernel_ready(std::atomic<uint64_t>& ready, const void* kernel, int smem, int regs = 0);
 inline int dtype_size(int dtype) { return dtype == OOS_DTYPE_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype >= OOS_DTYPE_F32 && dtype <= OOS_DTYPE_F16; }
 inline bool head_dim_ok(int d) { return d >= 2 && d <= kMaxHeadDim && d % 2 == 0; }

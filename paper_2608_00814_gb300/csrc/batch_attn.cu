@@ -252,11 +252,23 @@ struct BatchAttnPlan {
   size_t ml_off, bytes;
 };
 
-static int device_sms() {
+int device_sms() {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return 0;
   return n;
+}
+
+cudaError_t kernel_ready(std::atomic<uint64_t>& ready, const void* kernel, int smem, int regs) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (ready.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  if (regs) e = check_launch_regs(kernel, regs);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) ready.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, const oos_batch& b, BatchAttnPlan* p) {
@@ -292,8 +304,10 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
 template <typename TQ, typename TK, int RT, int VEC>
 static cudaError_t launch_rows(const BatchAttnArgs& a, int blocks, cudaStream_t st) {
   const int ld = ((a.pages.d + 3) & ~3) + 4;
-  const size_t smem = ((RT + 2 * kRowKeys) * ld + RT * (kRowKeys + 4)) * 4;
-  cudaError_t e = cudaFuncSetAttribute(k_attn_rows<TQ, TK, RT, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  auto smem_of = [](int ld_) { return ((RT + 2 * kRowKeys) * ld_ + RT * (kRowKeys + 4)) * 4; };
+  const size_t smem = smem_of(ld);
+  static std::atomic<uint64_t> ready{0};
+  cudaError_t e = kernel_ready(ready, (const void*)k_attn_rows<TQ, TK, RT, VEC>, smem_of(kMaxHeadDim + 4));
   if (e != cudaSuccess) return e;
   e = launch(false, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
   if (e != cudaSuccess) return e;

@@ -860,8 +860,9 @@ PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys
   return p;
 }
 
-static cudaError_t launch_pages(const void* kernel, int smem, const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+static cudaError_t launch_pages(std::atomic<uint64_t>& ready, const void* kernel, int smem, const BatchAttnArgs& a,
+                                const PagesPlan& p, cudaStream_t st) {
+  const cudaError_t e = kernel_ready(ready, kernel, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(p.tiles * p.splits), a.pages.nkv);
@@ -888,9 +889,10 @@ static cudaError_t launch_pages(const void* kernel, int smem, const BatchAttnArg
 
 template <typename TQ, bool F16>
 static cudaError_t launch_pages_of(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
-  if (p.tile_rows == 8) return launch_pages((const void*)k_attn_pages<TQ, F16, 1>, pg_smem(narrow_stages(1)), a, p, st);
-  if (p.tile_rows == 16) return launch_pages((const void*)k_attn_pages<TQ, F16, 2>, pg_smem(narrow_stages(2)), a, p, st);
-  return launch_pages((const void*)k_attn_pages_wide<TQ, F16>, pg_smem(kWideStages), a, p, st);
+  static std::atomic<uint64_t> ready[3] = {};
+  if (p.tile_rows == 8) return launch_pages(ready[0], (const void*)k_attn_pages<TQ, F16, 1>, pg_smem(narrow_stages(1)), a, p, st);
+  if (p.tile_rows == 16) return launch_pages(ready[1], (const void*)k_attn_pages<TQ, F16, 2>, pg_smem(narrow_stages(2)), a, p, st);
+  return launch_pages(ready[2], (const void*)k_attn_pages_wide<TQ, F16>, pg_smem(kWideStages), a, p, st);
 }
 
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st) {

@@ -421,9 +421,8 @@ __global__ void __launch_bounds__(kPxThreads, 1) k_attn_prefix(const __grid_cons
 template <typename TQ, bool F16>
 static cudaError_t launch_prefix(const PrefixArgs& p, dim3 grid, cudaStream_t st) {
   // the register split must not ask for more than the block is launched with
-  cudaError_t e = check_launch_regs((const void*)k_attn_prefix<TQ, F16>, kPxRegsLaunch);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(k_attn_prefix<TQ, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPxSmem);
+  static std::atomic<uint64_t> ready{0};
+  const cudaError_t e = kernel_ready(ready, (const void*)k_attn_prefix<TQ, F16>, kPxSmem, kPxRegsLaunch);
   return e == cudaSuccess ? launch(false, k_attn_prefix<TQ, F16>, grid, dim3(kPxThreads), kPxSmem, st, p) : e;
 }
 

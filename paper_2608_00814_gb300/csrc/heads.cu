@@ -15,6 +15,7 @@
 // eighth of a turn.  A warp forms them once per token and keeps them over its
 // heads: at a warp per head they were the kernel's largest cost.
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
 
@@ -178,14 +179,24 @@ bool rope_ok(const oos_rope_config* r) {
   return r->factor <= 1.f || (r->low_freq_factor > 0.f && r->high_freq_factor > r->low_freq_factor && r->orig_max_pos >= 1);
 }
 
-void rope_turns(const oos_rope_config& r, int d, RopeTurns* out) {
+// A layer's calls come with one configuration: its table of powers is kept per thread.
+const RopeTurns& rope_turns(const oos_rope_config& r, int d) {
+  static thread_local struct {
+    oos_rope_config r;
+    int d = 0;
+    RopeTurns turns;
+  } last;
+  if (last.d == d && memcmp(&last.r, &r, sizeof(r)) == 0) return last.turns;
   for (int m = 0; m < kMaxHeadDim / 2; ++m) {
-    out->f[m] = 0;
+    last.turns.f[m] = 0;
     if (m >= d / 2) continue;
     const double f = rope_rate(r.theta, m, d, r.factor, r.low_freq_factor, r.high_freq_factor, r.orig_max_pos);
     const double t = f / (2.0 * M_PI);
-    out->f[m] = (unsigned long long)ldexp(t - floor(t), 64);   // t - floor(t) <= 1 - 2^-53
+    last.turns.f[m] = (unsigned long long)ldexp(t - floor(t), 64);   // t - floor(t) <= 1 - 2^-53
   }
+  last.r = r;
+  last.d = d;
+  return last.turns;
 }
 
 bool pages_ok(const oos_paged_cache* c) {
@@ -224,10 +235,8 @@ static cudaError_t launch_heads(HeadArgs& a, const RopeTurns& rope, cudaStream_t
   const int chunks = w ? a.d2 / V : a.d2;
   a.lanes = std::min(32, pow2_at_least(chunks));
   const bool two = chunks > a.lanes;
-  int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
   // A token's heads go to as many warps as it takes to give every SM 16, so that a
   // few tokens are spread out while many share the angles over all their heads.
   const int total = a.heads[0] + a.heads[1], per_warp = 32 / a.lanes;
@@ -286,8 +295,8 @@ int oos_qk_norm_rope(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_h
   a.out_stride[1] = k_out_stride;
   a.positions = rope ? positions : nullptr;
   a.eps = eps;
-  RopeTurns turns = {};
-  if (rope) rope_turns(*rope, head_dim, &turns);
+  static const RopeTurns none = {};
+  const RopeTurns& turns = rope ? rope_turns(*rope, head_dim) : none;
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = dtype == OOS_DTYPE_F32    ? launch_heads<float, float, false>(a, turns, st)
                         : dtype == OOS_DTYPE_BF16 ? launch_heads<__nv_bfloat16, __nv_bfloat16, false>(a, turns, st)
@@ -320,8 +329,8 @@ int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32
   a.pages = view_of(*cache);
   a.batch = view_of(*batch);
   a.status = out_status;
-  RopeTurns turns = {};
-  if (rope) rope_turns(*rope, cache->head_dim, &turns);
+  static const RopeTurns none = {};
+  const RopeTurns& turns = rope ? rope_turns(*rope, cache->head_dim) : none;
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = dtype == OOS_DTYPE_F32    ? launch_append<float>(cache->dtype, a, turns, st)
                         : dtype == OOS_DTYPE_BF16 ? launch_append<__nv_bfloat16>(cache->dtype, a, turns, st)
