@@ -12,8 +12,8 @@
 // modulo 2^64 it is the angle's fraction of a turn to 2^-33 at position 2^31 (the
 // rate's own rounding to 53 bits), by integer products alone.  The nearest
 // quarter turn comes off exactly, so the fp32 sine and cosine see at most an
-// eighth of a turn.  A warp forms them once per token and keeps them over its
-// heads: at a warp per head they were the kernel's largest cost.
+// eighth of a turn.  A warp forms each of a token's angles once, dealt over its lanes,
+// hands them round by shuffles and keeps them over its heads.
 #include <math.h>
 #include <string.h>
 
@@ -23,12 +23,12 @@
 
 namespace oos {
 
-constexpr int kHeadWarps = 4;   // warps per block
+constexpr int kHeadWarps = 4;      // tokens per block, a warp each
+constexpr int kMaxSlices = 1024;   // warps a token's heads are dealt to (times 2^20 heads below 2^31)
 
 struct HeadArgs {
-  int n, d, d2, lanes;            // tokens, head size and half of it, lanes per head (a power of two)
+  int n, d, d2;                   // tokens, head size and half of it
   int heads[2];                   // q and k heads (append: 0 and the K heads)
-  int slices;                     // warps that share a token's heads
   const void* in[2];
   long long in_stride[2];         // elements
   const void* gain[2];
@@ -57,14 +57,57 @@ OOS_DEV void turn(unsigned long long rate, int pos, float& c, float& s) {
 }
 
 // T: elements of the inputs and gains, O: of the outputs.  VEC: values per access.
-// NC: chunks of half a head per lane.  APPEND: in[1] goes to the pages' K, v to
-// their V.
-template <typename T, typename O, int VEC, int NC, bool APPEND>
-__global__ void __launch_bounds__(kHeadWarps * 32) k_heads(const HeadArgs a, const __grid_constant__ RopeTurns rope) {
-  const long long w = (long long)blockIdx.x * kHeadWarps + (threadIdx.x >> 5);
+// LANES: lanes per head, NC: chunks of half a head per lane.  APPEND: in[1] goes to
+// the pages' K, v to their V.
+template <typename T, typename O, int VEC, int LANES, int NC, bool APPEND>
+__global__ void __launch_bounds__(kHeadWarps * 32, 4) k_heads(const HeadArgs a, const __grid_constant__ RopeTurns rope) {
   const int lane = threadIdx.x & 31;
-  const int t = (int)(w / a.slices), slice = (int)(w % a.slices);
+  const long long t = (long long)blockIdx.x * kHeadWarps + (threadIdx.x >> 5);
+  const int slice = blockIdx.y, slices = gridDim.y;
   if (t >= a.n) return;
+  constexpr int GROUPS = 32 / LANES;   // heads of the warp at once
+  // Heads in flight per lane, and so registers, against warps: 4 without V (15001 tokens
+  // of 40 binary16 heads: 49 us, 92 % of the copy's rate; 2: 60), 2 with it (12600 tokens
+  // of 8 heads: 25.5 us, 4: 32).
+  constexpr int U = NC * VEC > 8 ? 1 : APPEND ? 2 : 4;
+  const int sub = lane % LANES, group = lane / LANES;
+  const int pos = a.positions ? a.positions[t] : 0;
+  // heads [h0, h1) of this warp, counted over q's and k's
+  const int total = a.heads[0] + a.heads[1];
+  const int h0 = (int)((unsigned)(total * slice) / slices), h1 = (int)((unsigned)(total * (slice + 1)) / slices);
+  auto first = [&](int side) { return max(0, h0 - (side ? a.heads[0] : 0)); };
+  auto past = [&](int side) { return min(a.heads[side], h1 - (side ? a.heads[0] : 0)); };
+  Vec<T, VEC> x[U][NC][2];
+  auto load = [&](int side, int h) {
+    const T* in = (const T*)a.in[side] + t * a.in_stride[side];
+    const int hi = past(side);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int hh = h + u * GROUPS + group, m = (c * LANES + sub) * VEC;
+        const T* p = in + (long long)hh * a.d + m;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          x[u][c][half] = Vec<T, VEC>();
+          if (hh < hi && m < a.d2) x[u][c][half] = *reinterpret_cast<const Vec<T, VEC>*>(p + half * a.d2);
+        }
+      }
+  };
+  // the first heads' loads go out before everything that waits: an appended row's lookups
+  // follow each other through four of them
+  const int side0 = APPEND || h0 >= a.heads[0] ? 1 : 0;
+  load(side0, first(side0));
+  Vec<T, VEC> v[4];
+  const T* vin = nullptr;
+  int v_chunks = 0;
+  if (APPEND) {
+    vin = (const T*)a.v + t * a.v_stride + (long long)first(1) * a.d;
+    v_chunks = max(0, past(1) - first(1)) * a.d / VEC;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (lane + 32 * u < v_chunks) v[u] = *reinterpret_cast<const Vec<T, VEC>*>(vin + (lane + 32 * u) * VEC);
+  }
   // where an appended row goes (the whole warp; a row without a place is left out)
   long long slot = 0;
   if (APPEND) {
@@ -72,103 +115,109 @@ __global__ void __launch_bounds__(kHeadWarps * 32) k_heads(const HeadArgs a, con
     const int seq = warp_count_le(b.n_seqs, [&](int i) { return (long long)b.q_start[i]; }, t);
     if (seq >= b.n_seqs) return;                       // behind the last sequence
     const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1];
-    slot = t < q0 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, b.seq_len[seq] - (q1 - t));
+    slot = t < q0 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, b.seq_len[seq] - (q1 - (int)t));
     if (slot < 0) {
       if (lane == 0) *a.status = OOS_EBATCH;
       return;
     }
   }
-  const int sub = lane & (a.lanes - 1), group = lane / a.lanes, groups = 32 / a.lanes;
-  float cs[NC][VEC], sn[NC][VEC];
+  // a lane's pairs, counted over its chunks: (c * LANES + sub) * VEC + i, p = c * VEC + i
+  float cs[NC * VEC], sn[NC * VEC];
   if (a.positions) {
-    const int pos = a.positions[t];
+    constexpr int MINE = (NC * VEC + GROUPS - 1) / GROUPS;   // group g forms pairs p = g, g + GROUPS, ..
+    float mc[MINE], ms[MINE];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int m = (c * a.lanes + sub) * VEC + i;
-        if (m < a.d2) turn(rope.f[m], pos, cs[c][i], sn[c][i]);
-      }
-  }
-  // heads [h0, h1) of this warp, counted over q's and k's
-  const int total = a.heads[0] + a.heads[1];
-  const int h0 = (int)((long long)total * slice / a.slices), h1 = (int)((long long)total * (slice + 1) / a.slices);
-#pragma unroll 1
-  for (int side = APPEND ? 1 : 0; side < 2; ++side) {
-    const int lo = max(0, h0 - (side ? a.heads[0] : 0)), hi = min(a.heads[side], h1 - (side ? a.heads[0] : 0));
-    const T* in = (const T*)a.in[side] + (long long)t * a.in_stride[side];
-    O* out = APPEND ? (O*)a.pages.k + slot * a.pages.nkv * a.d : (O*)a.out[side] + (long long)t * a.out_stride[side];
-    const T* gain = (const T*)a.gain[side];
-    float g[NC][2][VEC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int m = (c * a.lanes + sub) * VEC;
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) g[c][half][i] = gain && m < a.d2 ? to_f32(gain[half * a.d2 + m + i]) : 1.f;
+    for (int k = 0; k < MINE; ++k) {
+      const int p = k * GROUPS + group, m = (p / VEC * LANES + sub) * VEC + p % VEC;
+      mc[k] = 1.f;
+      ms[k] = 0.f;
+      if (p < NC * VEC && m < a.d2) turn(rope.f[m], pos, mc[k], ms[k]);
     }
-    constexpr int U = NC * VEC > 8 ? 1 : 2;   // heads in flight per lane
+#pragma unroll
+    for (int p = 0; p < NC * VEC; ++p) {
+      cs[p] = __shfl_sync(0xffffffffu, mc[p / GROUPS], p % GROUPS * LANES + sub);
+      sn[p] = __shfl_sync(0xffffffffu, ms[p / GROUPS], p % GROUPS * LANES + sub);
+    }
+  }
+  bool loaded = true;
 #pragma unroll 1
-    for (int h = lo; h < hi; h += U * groups) {
-      float x[U][NC][2][VEC];
+  for (int side = side0; side < 2; ++side) {
+    const int lo = first(side), hi = past(side);
+    if (lo >= hi) continue;
+    O* out = APPEND ? (O*)a.pages.k + slot * a.pages.nkv * a.d : (O*)a.out[side] + t * a.out_stride[side];
+    const T* gain = (const T*)a.gain[side];
+    Vec<T, VEC> g[NC][2];
+    if (gain) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int c = 0; c < NC; ++c) {
+        const int m = (c * LANES + sub) * VEC;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int hh = h + u * groups + group, m = (c * a.lanes + sub) * VEC;
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (hh < hi && m < a.d2) load_vec<T, VEC>(in + (long long)hh * a.d + half * a.d2 + m, x[u][c][half]);
-            else
-#pragma unroll
-              for (int i = 0; i < VEC; ++i) x[u][c][half][i] = 0.f;
-          }
-        }
+          for (int i = 0; i < VEC; ++i)   // element by element: a gain may start anywhere
+            if (m < a.d2) g[c][half].v[i] = gain[half * a.d2 + m + i];
+      }
+    }
+#pragma unroll 1
+    for (int h = lo; h < hi; h += U * GROUPS) {
+      if (!loaded) load(side, h);
+      loaded = false;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (h + u * GROUPS >= hi) break;   // warp-uniform
+        float r = 1.f;
         if (gain) {
           float ss = 0.f;
 #pragma unroll
           for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) ss += x[u][c][0][i] * x[u][c][0][i] + x[u][c][1][i] * x[u][c][1][i];
-          for (int o = a.lanes >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float r = rsqrtf(ss / (float)a.d + a.eps);
+            for (int i = 0; i < VEC; ++i) {
+              const float lo_ = to_f32(x[u][c][0].v[i]), hi_ = to_f32(x[u][c][1].v[i]);
+              ss += lo_ * lo_ + hi_ * hi_;
+            }
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-              for (int i = 0; i < VEC; ++i) x[u][c][half][i] = x[u][c][half][i] * r * g[c][half][i];
+          for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          r = rsqrtf(ss / (float)a.d + a.eps);
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const int hh = h + u * groups + group, m = (c * a.lanes + sub) * VEC;
-          if (a.positions) {
+          const int hh = h + u * GROUPS + group, m = (c * LANES + sub) * VEC;
+          float y[2][VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              const float lo_ = x[u][c][0][i], hi_ = x[u][c][1][i];
-              x[u][c][0][i] = lo_ * cs[c][i] - hi_ * sn[c][i];
-              x[u][c][1][i] = hi_ * cs[c][i] + lo_ * sn[c][i];
+          for (int i = 0; i < VEC; ++i) {
+            float lo_ = to_f32(x[u][c][0].v[i]), hi_ = to_f32(x[u][c][1].v[i]);
+            if (gain) {
+              lo_ = lo_ * r * to_f32(g[c][0].v[i]);
+              hi_ = hi_ * r * to_f32(g[c][1].v[i]);
             }
+            const int p = c * VEC + i;
+            y[0][i] = a.positions ? lo_ * cs[p] - hi_ * sn[p] : lo_;
+            y[1][i] = a.positions ? hi_ * cs[p] + lo_ * sn[p] : hi_;
           }
           if (hh < hi && m < a.d2) {
-            store_vec<O, VEC>(out + (long long)hh * a.d + m, x[u][c][0]);
-            store_vec<O, VEC>(out + (long long)hh * a.d + a.d2 + m, x[u][c][1]);
+            store_vec<O, VEC>(out + (long long)hh * a.d + m, y[0]);
+            store_vec<O, VEC>(out + (long long)hh * a.d + a.d2 + m, y[1]);
           }
         }
       }
     }
-    if (APPEND) {   // the same heads of V
-      const T* vin = (const T*)a.v + (long long)t * a.v_stride;
-      O* vout = (O*)a.pages.v + slot * a.pages.nkv * a.d;
-      const int chunks = (hi - lo) * a.d / VEC;
-#pragma unroll 4
-      for (int i = lane; i < chunks; i += 32) {
-        float x[VEC];
-        load_vec<T, VEC>(vin + (long long)lo * a.d + i * VEC, x);
-        store_vec<O, VEC>(vout + (long long)lo * a.d + i * VEC, x);
+  }
+  if (APPEND) {   // the same heads of V, four accesses in flight
+    O* vout = (O*)a.pages.v + slot * a.pages.nkv * a.d + (long long)first(1) * a.d;
+#pragma unroll 1
+    for (int i0 = lane; i0 < v_chunks; i0 += 4 * 32) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + 32 * u >= v_chunks) continue;
+        if (i0 != lane) v[u] = *reinterpret_cast<const Vec<T, VEC>*>(vin + (i0 + 32 * u) * VEC);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + 32 * u >= v_chunks) continue;
+        float y[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[i] = to_f32(v[u].v[i]);
+        store_vec<O, VEC>(vout + (i0 + 32 * u) * VEC, y);
       }
     }
   }
@@ -222,32 +271,30 @@ static bool wide(const HeadArgs& a, int es, int vec, int out_es) {
   return ok;
 }
 
-static int pow2_at_least(int x) {
-  int p = 1;
-  while (p < x) p *= 2;
-  return p;
+template <typename T, typename O, int VEC, int LANES, int NC, bool APPEND>
+static cudaError_t launch_heads_of(HeadArgs& a, const RopeTurns& rope, cudaStream_t st) {
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  // A token's heads go to as many warps as it takes to give every SM 16, so that a
+  // few tokens are spread out while many share the angles over all their heads (2048
+  // tokens of 40 heads: 10.6 us, 11.4 with 32 warps, 13.9 with 48).
+  const int total = a.heads[0] + a.heads[1], most = (total * LANES + 31) / 32;
+  const int slices = (int)std::max(1ll, std::min<long long>(std::min(most, kMaxSlices), 16ll * sms / a.n));
+  const dim3 grid((unsigned)((a.n + (long long)kHeadWarps - 1) / kHeadWarps), slices);
+  return launch(false, k_heads<T, O, VEC, LANES, NC, APPEND>, grid, dim3(kHeadWarps * 32), 0, st, a, rope);
 }
 
 template <typename T, typename O, bool APPEND>
 static cudaError_t launch_heads(HeadArgs& a, const RopeTurns& rope, cudaStream_t st) {
-  constexpr int V = 16 / (int)sizeof(T);
-  const bool w = wide(a, sizeof(T), V, sizeof(O));
-  const int chunks = w ? a.d2 / V : a.d2;
-  a.lanes = std::min(32, pow2_at_least(chunks));
-  const bool two = chunks > a.lanes;
-  const int sms = device_sms();
-  if (sms <= 0) return cudaErrorInvalidDevice;
-  // A token's heads go to as many warps as it takes to give every SM 16, so that a
-  // few tokens are spread out while many share the angles over all their heads.
-  const int total = a.heads[0] + a.heads[1], per_warp = 32 / a.lanes;
-  const int most = (total + per_warp - 1) / per_warp;
-  a.slices = (int)std::max(1ll, std::min<long long>(most, 16ll * sms / a.n));
-  const long long warps = (long long)a.n * a.slices;
-  const dim3 grid((unsigned)((warps + kHeadWarps - 1) / kHeadWarps)), block(kHeadWarps * 32);
-  if (w && two) return cudaErrorInvalidValue;   // 64 values are at most 16 chunks of 4
-  if (w) return launch(false, k_heads<T, O, V, 1, APPEND>, grid, block, 0, st, a, rope);
-  if (two) return launch(false, k_heads<T, O, 1, 2, APPEND>, grid, block, 0, st, a, rope);
-  return launch(false, k_heads<T, O, 1, 1, APPEND>, grid, block, 0, st, a, rope);
+  constexpr int V = 16 / (int)sizeof(T);   // half a head is at most 8 chunks of 8 or 16 of 4
+  if (wide(a, sizeof(T), V, sizeof(O))) {
+    const int chunks = a.d2 / V;
+    if (chunks <= 4) return launch_heads_of<T, O, V, 4, 1, APPEND>(a, rope, st);
+    if (chunks <= 8) return launch_heads_of<T, O, V, 8, 1, APPEND>(a, rope, st);
+    return launch_heads_of<T, O, V, 16, 1, APPEND>(a, rope, st);
+  }
+  if (a.d2 > 32) return launch_heads_of<T, O, 1, 32, 2, APPEND>(a, rope, st);
+  return launch_heads_of<T, O, 1, 32, 1, APPEND>(a, rope, st);
 }
 
 template <typename T>
