@@ -40,6 +40,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   __shared__ TreeScratch s_tree;
   __shared__ long long s_at[kRowKeys];      // slot of each key in its buffer, -1: none
 
+  pdl_trigger();
   const int g = blockIdx.y;
   const bool prefix = (int)blockIdx.x < a.p_tiles * a.p_splits;
   const int local = prefix ? blockIdx.x : blockIdx.x - a.p_tiles * a.p_splits;
@@ -220,23 +221,37 @@ __global__ void __launch_bounds__(128) k_attn_join(const BatchAttnArgs a) {
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31, d = a.pages.d;
   const long long n_rows = (long long)a.batch.n_tokens * a.nq;
+  pdl_wait();
   if (row >= n_rows) return;
   const long long token = row / a.nq;
   if (token >= a.batch.q_start[a.batch.n_seqs] || token < a.batch.q_start[0]) return;   // padding
   const int parts = a.p_splits + a.s_splits;
   float2 ml = make_float2(-INFINITY, 0.f);
   if (lane < parts) ml = a.part_ml[lane * n_rows + row];
+  constexpr int U = 8;   // parts on their way at once
+  float v[U][4];
+  auto fetch = [&](int p0) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (p0 + i < parts && lane + 32 * c < d) v[i][c] = a.part_o[((p0 + i) * n_rows + row) * d + lane + 32 * c];
+  };
+  fetch(0);
   const float M = warp_max(ml.x);
   const float w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
   const float den = warp_sum(ml.x == -INFINITY ? 0.f : w * ml.y);
   T* out = (T*)a.out + token * a.out_stride + (row - token * a.nq) * d;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < parts; ++p) {
-    const float wp = __shfl_sync(0xffffffffu, w, p);
-    if (wp == 0.f) continue;   // a part without keys leaves its row unwritten
+  for (int p0 = 0; p0 < parts; p0 += U) {
+    if (p0 > 0) fetch(p0);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (lane + 32 * c < d) acc[c] += wp * a.part_o[(p * n_rows + row) * d + lane + 32 * c];
+    for (int i = 0; i < U; ++i) {
+      const float wp = __shfl_sync(0xffffffffu, w, (p0 + i) & 31);
+      if (p0 + i >= parts || wp == 0.f) continue;   // a part without keys leaves its row unwritten
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] += wp * v[i][c];
+    }
   }
 #pragma unroll
   for (int c = 0; c < 4; ++c)
@@ -288,10 +303,10 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
   p->p_tiles = prefix_len > 0 ? (int)((rows + p->rt - 1) / p->rt) : 0;
   p->s_tiles = (int)(b.n_seqs + rows / p->rt);
-  // enough blocks for four per SM, each with eight tiles of keys at least
+  // enough blocks for four per SM, each with two tiles of keys at least
   auto splits = [&](long long tiles, long long keys) {
     const long long want = tiles > 0 ? 4ll * sms / (tiles * c.n_kv_heads) : 1;
-    return (int)std::max(1ll, std::min({want, keys / (8 * kRowKeys), (long long)kMaxParts / 2}));
+    return (int)std::max(1ll, std::min({want, keys / (2 * kRowKeys), (long long)kMaxParts / 2}));
   };
   p->p_splits = prefix_len > 0 ? splits(p->p_tiles, prefix_len) : 0;
   p->s_splits = splits(p->s_tiles, most_keys);
@@ -312,7 +327,7 @@ static cudaError_t launch_rows(const BatchAttnArgs& a, int blocks, cudaStream_t 
   e = launch(false, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.batch.n_tokens * a.nq;
-  return launch(false, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);
+  return launch(true, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);
 }
 
 template <typename TQ, typename TK>
