@@ -18,7 +18,7 @@ OUT_DIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(OUT_DIR, "liboos.so")
 LIB_TIMELINE = os.path.join(OUT_DIR, "liboos_timeline.so")
 UNITS = ["oos_api.cu", "small.cu", "gemm.cu", "attn.cu", "prefill.cu", "f32.cu", "noalloc.cu", "hint.cu", "decode.cu",
-         "heads.cu", "batch_attn.cu", "batch_prefix.cu", "batch_pages.cu"]
+         "heads.cu", "batch_attn.cu", "batch_tiles.cu", "batch_pages.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -10,7 +10,7 @@
 // all; in the sequence's parts a tile holds rows of one sequence.
 //
 // k_attn_rows: CUDA cores, fp32 products, for every type and head size.  The 16-bit
-// types with heads of 128 take the tensor-core kernels of batch_prefix.cu and
+// types with heads of 128 take the tensor-core kernels of batch_tiles.cu and
 // batch_pages.cu.
 #include <math.h>
 
@@ -258,11 +258,31 @@ __global__ void __launch_bounds__(128) k_attn_join(const BatchAttnArgs a) {
     if (lane + 32 * c < d) out[lane + 32 * c] = from_f32<T>(den == 0.f ? 0.f : acc[c] / den);
 }
 
+// The same for the parts of the tensor-core kernels: rows by kv head, heads of 128
+template <typename T>
+__global__ void __launch_bounds__(256) k_attn_join_parts(const __grid_constant__ BatchAttnArgs a) {
+  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;   // of [kv head][token * group + head]
+  pdl_wait();
+  const int rows = a.batch.n_tokens * a.group;
+  if (row >= rows * a.pages.nkv) return;
+  const int g = row / rows, r = row - g * rows, token = r / a.group;
+  if (token >= a.batch.q_start[a.batch.n_seqs] || token < a.batch.q_start[0]) return;   // padding
+  const long long step = (long long)a.pages.nkv * rows * kPartLd;
+  const float* p = a.part_o + (long long)row * kPartLd;
+  join_rows<1, 8>(
+      0, 1, 0, 1, a.p_splits + a.s_splits,
+      [&](int, int i) { return *reinterpret_cast<const float2*>(p + i * step + 128); },
+      [&](int, int i) { return *reinterpret_cast<const float4*>(p + i * step + 4 * lane); },
+      [&](int, float4 o, float, float den) { store_row<T>(a, g, 0, r, weighted_mean(o, den)); });
+}
+
 // ---- host: how a call is cut up
 struct BatchAttnPlan {
   bool tc;             // tensor cores: 16-bit types with heads of 128
+  bool few;            // .. with few rows per sequence
   PrefixPlan prefix;
   PagesPlan pages;
+  SequencePlan sequence;
   int rt, p_tiles, p_splits, s_tiles, s_splits;   // CUDA cores
   size_t ml_off, bytes;
 };
@@ -294,10 +314,15 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, 1ll << 31);
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc) {
-    p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, sms) : PrefixPlan{0, 0};
-    p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
+    p->few = rows <= 16ll * b.n_seqs;
+    p->sequence = {false, 0, 1};
+    if (p->few) p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
+    else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, prefix_len, most_keys, sms);
+    p->prefix = prefix_len > 0 && !p->sequence.takes_prefix ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, sms)
+                                                            : PrefixPlan{0, 0, 0.0};
+    const int parts = p->prefix.splits + (p->sequence.splits > 1 ? p->sequence.splits : 0);
     p->ml_off = 0;
-    p->bytes = ((size_t)p->prefix.splits * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
+    p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
     return true;
   }
   p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
@@ -407,9 +432,16 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
   cudaError_t e;
   if (p.tc) {
     a.p_splits = p.prefix.splits;
-    a.s_splits = p.pages.splits;
-    e = prefix_len > 0 ? launch_prefix_tc(a, p.prefix, dtype, cache->dtype, st) : cudaSuccess;
-    if (e == cudaSuccess) e = launch_pages_tc(a, p.pages, dtype, cache->dtype, st);
+    a.s_splits = p.few ? p.pages.splits : p.sequence.splits;
+    e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, cache->dtype, st) : cudaSuccess;
+    if (e == cudaSuccess)
+      e = p.few ? launch_pages_tc(a, p.pages, dtype, cache->dtype, st)
+                : launch_sequence_tc(a, p.sequence, dtype, cache->dtype, st);
+    if (e == cudaSuccess && !p.few && a.s_splits > 1) {
+      const dim3 grid((unsigned)(((long long)batch->n_tokens * n_q_heads + 7) / 8));
+      e = dtype == OOS_DTYPE_BF16 ? launch(true, k_attn_join_parts<__nv_bfloat16>, grid, dim3(256), 0, st, a)
+                                  : launch(true, k_attn_join_parts<__half>, grid, dim3(256), 0, st, a);
+    }
   } else if (dtype == OOS_DTYPE_F32) {
     e = launch_batch_rows<float, float>(a, p, st);
   } else if (cache->dtype == OOS_DTYPE_BF16) {

@@ -1,4 +1,4 @@
-// Attention of a batch step: what its kernels share (batch_attn.cu, batch_prefix.cu,
+// Attention of a batch step: what its kernels share (batch_attn.cu, batch_tiles.cu,
 // batch_pages.cu).
 #pragma once
 
@@ -76,13 +76,16 @@ OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRow
 }
 
 // Ancestor sets of the sequence's rows, [row] -> 128 bits, itself included, by pointer
-// doubling in shared memory.  The whole block; n <= kMaxTreeRows.
+// doubling in shared memory: n <= kMaxTreeRows rows, threads tid of n_threads that meet
+// at sync().
 struct TreeScratch {
   unsigned long long anc[2][kMaxTreeRows][2];
   int up[2][kMaxTreeRows];
 };
-OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int n, TreeScratch* t))[2] {
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+template <typename SYNC>
+OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int n, TreeScratch* t, int tid, int n_threads,
+                                             SYNC sync))[2] {
+  for (int i = tid; i < n; i += n_threads) {
     int p = a.parent[q0 + i];
     if (p < -1 || p >= i) {
       *a.status = OOS_ETREE;
@@ -92,21 +95,31 @@ OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int
     t->anc[0][i][0] = i < 64 ? 1ull << i : 0ull;
     t->anc[0][i][1] = i < 64 ? 0ull : 1ull << (i - 64);
   }
-  __syncthreads();
+  sync();
   int cur = 0;
   for (int step = 1; step < n; step *= 2, cur ^= 1) {
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    for (int i = tid; i < n; i += n_threads) {
       const int p = t->up[cur][i];
       t->anc[cur ^ 1][i][0] = t->anc[cur][i][0] | (p >= 0 ? t->anc[cur][p][0] : 0ull);
       t->anc[cur ^ 1][i][1] = t->anc[cur][i][1] | (p >= 0 ? t->anc[cur][p][1] : 0ull);
       t->up[cur ^ 1][i] = p >= 0 ? t->up[cur][p] : -1;
     }
-    __syncthreads();
+    sync();
   }
   return t->anc[cur];
 }
+OOS_DEV const unsigned long long (*tree_sets(const BatchAttnArgs& a, int q0, int n, TreeScratch* t))[2] {   // the block
+  return tree_sets(a, q0, n, t, threadIdx.x, blockDim.x, [] { __syncthreads(); });
+}
 
-// ---- 16-bit types with heads of 128 (tensor cores)
+OOS_DEV void cp_async16(uint32_t dst, const void* src, bool ok) {   // zeros where not ok
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+OOS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+OOS_DEV void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 // Rows lo + warp, + n_warps, .. below hi, a warp per row and R rows at a time: part i
 // of row r has (m, l) = ml_of(r, i), its four columns of this lane v_of(r, i), i < parts
@@ -165,6 +178,26 @@ OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_o
   }
 }
 
+// Row `row` of the sequence that starts at token q0, kv head g: the lane's four columns
+template <typename TQ>
+OOS_DEV void store_row(const BatchAttnArgs& a, int g, int q0, int row, float4 o) {
+  const float v[4] = {o.x, o.y, o.z, o.w};
+  TQ* out = (TQ*)a.out + (long long)(q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * 128 +
+            4 * (threadIdx.x & 31);
+  if (((uintptr_t)out & 7) == 0) {
+    store_vec<TQ, 4>(out, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = from_f32<TQ>(v[e]);
+  }
+}
+
+// a row's sum over the sum of its weights; a row without keys: zeros
+OOS_DEV float4 weighted_mean(float4 o, float den) {
+  const float f = den == 0.f ? 0.f : 1.f / den;
+  return make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+}
+
 // bf16 queries of a binary16 cache: a power of two per row brings the largest element
 // to [1, 2), where binary16 holds bf16's 8 bits exactly (elements below 2^-14 of it
 // to 2^-25 of it, far below what their scores are rounded by); the power goes into
@@ -185,16 +218,24 @@ OOS_DEV uint32_t scaled_half2(uint32_t w, float f) {
 struct PrefixPlan {
   int splits;   // key ranges, a part each
   int pairs;    // pairs of 128-row tiles
+  double us;    // estimated
 };
 PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int n_sms);
 struct PagesPlan {
-  int tile_rows;   // of a block: 8 or 16 (decoding tokens), or 64
+  int tile_rows;   // of a block: 8 or 16
   int tiles, splits;
 };
+struct SequencePlan {
+  bool takes_prefix;   // in the same kernel
+  int tiles, splits;
+};
+SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_len, long long most_keys, int n_sms);
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
 // the prefix's parts of every row
 cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dtype, int kv_dtype, cudaStream_t st);
-// the sequences' own keys, joined with the prefix's p_splits parts into out
+// the sequences' own keys, joined with the prefix's p_splits parts into out; of
+// launch_sequence_tc with several splits, parts p_splits .. for launch_join_tc
+cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, int kv_dtype, cudaStream_t st);
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
 
 }  // namespace oos

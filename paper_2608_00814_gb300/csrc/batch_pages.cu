@@ -1,20 +1,20 @@
 // Attention of a batch step over the sequences' own pages, 16-bit types with heads of
-// 128, and the join with the prefix's part.
+// 128, where a sequence has few rows (a decoding token's group), and the join with the
+// prefix's parts.
 //
-// A block owns a tile of rows (token, head of one kv head's group) of one sequence and a
-// range of its keys; the blocks of the other ranges of the same rows are its cluster.
-// Pages are gathered by 16-byte asynchronous copies, a key row of 256 bytes by 16 lanes,
-// whatever the page size: keys that are not there arrive as zeros.  Products run on
-// mma.sync m16n8k16, operands by ldmatrix from rows whose 16-byte chunks are swizzled by
-// the key, S and O in registers.
-//   narrow  16 rows (a decoding token's group): the keys are dealt to the block's four
-//           warps in chunks of 16, each warp with a three-stage ring of its own, no
-//           block barrier before the end.  Bound by HBM.
-//   wide    64 rows (trees, prompts): 16 rows per warp, chunks of 64 keys shared by
-//           the block, so that a key is read once for 64 rows.
+// A block owns a tile of 8 or 16 rows (token, head of one kv head's group) of one
+// sequence and a range of its keys; the blocks of the other ranges of the same rows are
+// its cluster.  Pages are gathered by 16-byte asynchronous copies, a key row of 256 bytes
+// by 16 lanes, whatever the page size: keys that are not there arrive as zeros.  The
+// keys are dealt to the block's four warps in chunks of 16, each warp with a ring of its
+// own, no block barrier before the end; several blocks per SM cover each other's waits.
+// Products run on mma.sync m16n8k16, operands by ldmatrix from rows whose 16-byte chunks
+// are swizzled by the key.  Bound by HBM, and below about 300 keys by the lookups that
+// follow each other.
+//
 // Every row keeps its maximum, moved only when a chunk exceeds it by 2^8, and its sum in
-// fp32.  Weights enter P.V in the pages' type: binary16, or bf16 (narrow: as two bf16
-// halves, whose second product costs nothing beside the reads).
+// fp32.  Weights enter P.V as binary16, or as two bf16 halves, whose second product costs
+// nothing beside the reads.
 #include <math.h>
 
 #include <algorithm>
@@ -26,7 +26,6 @@
 namespace oos {
 
 constexpr int kPgWarps = 4;
-constexpr int kWideStages = 3;
 __host__ __device__ constexpr int narrow_stages(int nt) { return nt == 1 ? 2 : 3; }
 constexpr int kPgD = 128;
 constexpr int kPgRow = 2 * kPgD;                 // bytes of a key row
@@ -34,9 +33,6 @@ constexpr int kPgChunkBytes = 2 * 16 * kPgRow;   // 16 keys, K and V
 constexpr int pg_smem(int stages) { return stages * kPgWarps * kPgChunkBytes; }
 static_assert(kPgWarps * 8 * kPartLd * 4 <= pg_smem(2) && kPgWarps * 16 * kPartLd * 4 <= pg_smem(3), "staged rows over the rings");
 
-OOS_DEV void cp_async16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
 OOS_DEV void lds128(uint32_t addr, uint32_t (&w)[4]) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
 }
@@ -55,11 +51,6 @@ OOS_DEV uint32_t movmatrix_trans(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
-}
-OOS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-OOS_DEV void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 OOS_DEV void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -423,426 +414,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, NT == 1 ? 3 : 2) k_attn_pages(c
         const float* p = part(r, i) + 4 * lane;
         return i < own && S > 1 ? ld_cluster4(dsmem_addr(p, i / kPgWarps)) : *reinterpret_cast<const float4*>(p);
       },
-      [&](int r, float4 x, float, float den) {
-        const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
-        const float v[4] = {x.x * f, x.y * f, x.z * f, x.w * f};
-        const int row = t.r0 + r;
-        TQ* out = (TQ*)a.out + (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kPgD + 4 * lane;
-        if (((uintptr_t)out & 7) == 0) {
-          store_vec<TQ, 4>(out, v);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[e] = from_f32<TQ>(v[e]);
-        }
-      });
-  if (S > 1) {   // a peer may still read this block's rows
-    cluster_arrive_release();
-    cluster_wait_acquire();
-  }
-}
-
-template <typename TQ, bool F16>
-__global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages_wide(const __grid_constant__ BatchAttnArgs a) {
-  constexpr bool WIDE = true;
-  extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int ROWS = WIDE ? 64 : 16, KC = WIDE ? 64 : 16;   // rows of the block, keys a warp takes at once
-  constexpr int STAGES = kWideStages;
-  constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
-  __shared__ TreeScratch s_tree;
-  __shared__ uint32_t s_valid[STAGES][kPgWarps];           // keys of a chunk that are there
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = blockIdx.y, S = a.s_splits, split = blockIdx.x % S;
-  pdl_trigger();
-  TileRows t;
-  if (!sequence_tile(a, blockIdx.x / S, ROWS, &t)) {          // the whole cluster
-    if (blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();       // the grid must not end before the one it follows
-    return;
-  }
-  const unsigned long long (*anc)[2] = nullptr;
-  if (a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
-  const int last = (t.r0 + t.rows - 1) / a.group;
-  const int n_keys = anc ? t.len : max(0, min(t.len, t.first + last + 1));
-  const int units = (n_keys + 63) / 64;
-  const int k0 = (int)((long long)units * split / S) * 64;
-  const int k1 = min(n_keys, (int)((long long)units * (split + 1) / S) * 64);
-  const int n_chunks = max(0, k1 - k0 + 63) / 64;             // of 64 keys: one per warp each, or one for all
-
-  // ---- the first page lookups and the queries' loads go out together
-  const uint32_t ring = smem_addr(smem);
-  auto slot_of = [&](int c) -> long long {   // lane & 15: a key of this warp's 16 in 64-key chunk c
-    const int key = k0 + c * 64 + warp * 16 + (lane & 15);
-    if (c >= n_chunks || key >= k1) return -1;
-    const long long at = page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
-    if (at < 0) *a.status = OOS_EBATCH;
-    return at;
-  };
-  long long slot[STAGES];   // of the chunks up to the next one to be copied
-#pragma unroll
-  for (int c = 0; c < STAGES; ++c) slot[c] = slot_of(c);
-  const int row0 = WIDE ? warp * 16 : 0;          // rows of the tile
-  const int rr[2] = {row0 + (lane >> 2), row0 + (lane >> 2) + 8};
-  int token[2];
-  uint32_t qf[8][4];   // A fragments of 16 rows, all of d
-  float sc[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = t.r0 + rr[h];
-    token[h] = row / a.group;
-    const bool on = rr[h] < t.rows;
-    const TQ* q = (const TQ*)a.q + (long long)(t.q0 + (on ? token[h] : 0)) * a.q_stride + (g * a.group + row % a.group) * kPgD;
-    const bool pairs = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 3) == 0;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(q) + kk * 16 + e * 8 + (lane & 3) * 2;
-        uint32_t x = 0;
-        if (on) x = pairs ? *reinterpret_cast<const uint32_t*>(p) : (uint32_t)p[0] | (uint32_t)p[1] << 16;
-        qf[kk][2 * e + h] = x;
-      }
-  }
-
-  // ---- copies
-  const long long key_bytes = (long long)a.pages.nkv * kPgRow;
-  const uint8_t* kg = a.pages.k + (long long)g * kPgRow + (lane & 15) * 16;
-  const uint8_t* vg = a.pages.v + (long long)g * kPgRow + (lane & 15) * 16;
-  auto copy = [&](int c, long long slot) {   // this warp's keys of chunk c
-    const int st = c % STAGES;
-    const uint32_t dst = ring + (st * kPgWarps + warp) * kPgChunkBytes;
-    if (c < n_chunks) {
-      const uint32_t valid = __ballot_sync(0xffffffffu, slot >= 0) & 0xffffu;
-      if (lane == 0) s_valid[st][warp] = valid;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = 2 * i + (lane >> 4);
-        const long long at = __shfl_sync(0xffffffffu, slot, key);
-        const uint32_t o = key * kPgRow + (((lane & 15) ^ (key & 7)) << 4);
-        const bool ok = at >= 0;
-        const long long off = ok ? at * key_bytes : 0;
-        cp_async16(dst + o, kg + off, ok);
-        cp_async16(dst + 16 * kPgRow + o, vg + off, ok);
-      }
-    }
-    cp_async_commit();
-  };
-#pragma unroll
-  for (int c = 0; c < STAGES - 1; ++c) copy(c, slot[c]);
-  long long next = slot[STAGES - 1];   // looked up a chunk ahead
-
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    sc[h] = a.scale_log2;
-    if constexpr (CONVERT) {
-      float mx = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(qf[kk][2 * e + h])), fabsf(bf16_hi(qf[kk][2 * e + h]))));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const int e2 = row_exponent(mx);
-      sc[h] *= exp2i(e2);
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) qf[kk][2 * e + h] = scaled_half2(qf[kk][2 * e + h], exp2i(-e2));
-    }
-  }
-  // first and last token of the warp's rows
-  const int tok_lo = (t.r0 + row0) / a.group, tok_hi = (t.r0 + min(row0 + 15, t.rows - 1)) / a.group;
-  unsigned long long an[2][2] = {};
-  if (anc) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (rr[h] < t.rows) {
-        an[h][0] = anc[token[h]][0];
-        an[h][1] = anc[token[h]][1];
-      }
-  }
-
-  float o[16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-
-  // ldmatrix rows of this lane: K, keys by d; V, transposed on the way
-  const uint32_t k_key = ((lane >> 4) << 3) + (lane & 7), k_chunk = (lane >> 3) & 1;
-  const uint32_t v_key = (((lane >> 3) & 1) << 3) + (lane & 7), v_chunk = lane >> 4;
-
-  for (int c = 0; c < n_chunks; ++c) {
-    cp_async_wait<STAGES - 2>();
-    if (WIDE) __syncthreads();   // every warp's keys are there, and the stage before is free
-    else __syncwarp();
-    const int st = c % STAGES;
-    copy(c + STAGES - 1, next);
-    next = slot_of(c + STAGES);
-    unsigned long long valid;
-    if (WIDE) {
-      valid = 0;
-#pragma unroll
-      for (int w = 0; w < kPgWarps; ++w) valid |= (unsigned long long)s_valid[st][w] << (16 * w);
-    } else {
-      valid = s_valid[st][warp];
-    }
-    const int key0 = k0 + c * 64 + (WIDE ? 0 : warp * 16);
-    // nothing there, no row of this warp, or no row that sees the first key (warp-uniform)
-    if (valid == 0 || row0 >= t.rows || (!anc && key0 > t.first + tok_hi)) continue;
-    const uint32_t buf = ring + (st * kPgWarps + (WIDE ? 0 : warp)) * kPgChunkBytes;
-    // keys 16 j .. of the chunk: K rows, then V rows, of the warp that copied them
-    float s[KC / 8][4];
-#pragma unroll
-    for (int i = 0; i < KC / 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-      for (int j = 0; j < KC / 16; ++j) {
-        uint32_t b[4];
-        ldsm4(buf + j * kPgChunkBytes + k_key * kPgRow + (((2 * kk + k_chunk) ^ (k_key & 7)) << 4), b);
-        mma16816<F16>(s[2 * j], qf[kk], b[0], b[1]);
-        mma16816<F16>(s[2 * j + 1], qf[kk], b[2], b[3]);
-      }
-    // keys of the chunk that each row sees
-    const int seen = t.first - key0;   // those before it are committed
-    const bool full = valid == (KC == 64 ? ~0ull : 0xffffull) && (anc ? seen : seen + tok_lo + 1) >= KC;
-    unsigned long long bits[2] = {~0ull, ~0ull};
-    if (!full) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int lead = max(0, min(64, anc ? seen : seen + token[h] + 1));
-        unsigned long long b = lead >= 64 ? ~0ull : (1ull << lead) - 1;
-        if (anc) {
-          unsigned long long lo, hi;
-          if (seen >= 0) shl128(an[h][0], an[h][1], min(seen, 128), lo, hi);
-          else shr128(an[h][0], an[h][1], min(-seen, 128), lo, hi);
-          b |= lo;
-        }
-        bits[h] = b & valid;
-      }
-#pragma unroll
-      for (int i = 0; i < KC / 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!((bits[e >> 1] >> (8 * i + (lane & 3) * 2 + (e & 1))) & 1)) s[i][e] = -INFINITY;
-    }
-    // A key that some of the rows do not see must not reach them through 0 times a v
-    // that is not finite: such a chunk (the last ones of a sequence only) is summed apart.
-    const bool apart = !full && chunk_not_finite<F16>(buf, KC / 16);
-    bool move = false;
-    float mn[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < KC / 8; ++i) mx = max_nan(mx, max_nan(s[i][2 * h], s[i][2 * h + 1]));
-      mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) * sc[h];
-      mn[h] = !(mx <= m[h] + 8.f) ? mx : m[h];   // a NaN moves it, and stays
-      move = move || mn[h] != m[h];
-    }
-    if (__any_sync(0xffffffffu, move)) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float f = m[h] == mn[h] ? 1.f : m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn[h]);
-        l[h] *= f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          o[i][2 * h] *= f;
-          o[i][2 * h + 1] *= f;
-        }
-        m[h] = mn[h];
-      }
-    }
-    // without a finite score yet every score is -inf, and gives 0
-    const float neg[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
-    uint32_t p[KC / 8][2], p_lo[KC / 8][2];
-#pragma unroll
-    for (int i = 0; i < KC / 8; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float p0 = ex2_approx(fmaf(s[i][2 * h], sc[h], neg[h])), p1 = ex2_approx(fmaf(s[i][2 * h + 1], sc[h], neg[h]));
-        s[i][2 * h] = p0;
-        s[i][2 * h + 1] = p1;
-        l[h] += p0 + p1;
-        if constexpr (F16) {
-          const __half2 v = __floats2half2_rn(p0, p1);
-          p[i][h] = *reinterpret_cast<const uint32_t*>(&v);
-        } else {
-          const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
-          p[i][h] = *reinterpret_cast<const uint32_t*>(&v);
-          if constexpr (!WIDE) {
-            const __nv_bfloat162 r = __floats2bfloat162_rn(p0 - __low2float(v), p1 - __high2float(v));
-            p_lo[i][h] = *reinterpret_cast<const uint32_t*>(&r);
-          }
-        }
-      }
-    if (apart) {
-#pragma unroll
-      for (int i = 0; i < KC / 8; ++i)
-#pragma unroll 1
-        for (int j = 0; j < 8; ++j) {
-          const int key = 8 * i + j;
-          float pj[2];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float mine = j & 1 ? s[i][2 * h + 1] : s[i][2 * h];
-            pj[h] = __shfl_sync(0xffffffffu, mine, (lane & ~3) | (j >> 1));
-          }
-          const uint32_t vrow = buf + (key >> 4) * kPgChunkBytes + (16 + (key & 15)) * kPgRow + (lane & 3) * 4;
-#pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const uint32_t w = lds32(vrow + ((c ^ (key & 7)) << 4));
-            const float v0 = F16 ? __low2float(*reinterpret_cast<const __half2*>(&w)) : bf16_lo(w);
-            const float v1 = F16 ? __high2float(*reinterpret_cast<const __half2*>(&w)) : bf16_hi(w);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if ((bits[h] >> key) & 1) {
-                o[c][2 * h] += pj[h] * v0;
-                o[c][2 * h + 1] += pj[h] * v1;
-              }
-          }
-        }
-      continue;
-    }
-#pragma unroll
-    for (int j = 0; j < KC / 16; ++j) {
-      const uint32_t pa[4] = {p[2 * j][0], p[2 * j][1], p[2 * j + 1][0], p[2 * j + 1][1]};
-#pragma unroll
-      for (int dn = 0; dn < 8; ++dn) {
-        uint32_t b[4];
-        ldsm4_trans(buf + j * kPgChunkBytes + (16 + v_key) * kPgRow + (((2 * dn + v_chunk) ^ (v_key & 7)) << 4), b);
-        mma16816<F16>(o[2 * dn], pa, b[0], b[1]);
-        mma16816<F16>(o[2 * dn + 1], pa, b[2], b[3]);
-        if constexpr (!F16 && !WIDE) {
-          const uint32_t pl[4] = {p_lo[2 * j][0], p_lo[2 * j][1], p_lo[2 * j + 1][0], p_lo[2 * j + 1][1]};
-          mma16816<F16>(o[2 * dn], pl, b[0], b[1]);
-          mma16816<F16>(o[2 * dn + 1], pl, b[2], b[3]);
-        }
-      }
-    }
-  }
-  cp_async_wait<0>();
-  __syncthreads();
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-  }
-  const int n_pre = a.p_splits;   // the prefix's parts
-  const long long part_rows = (long long)a.batch.n_tokens * a.group;
-  // the prefix's row of tile row r, its first part; part_step floats to the next
-  auto prefix_row = [&](int r) {
-    return a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0 + r) * kPartLd;
-  };
-  const long long part_step = (long long)a.pages.nkv * part_rows * kPartLd;
-  auto out_row = [&](int r) {
-    const int row = t.r0 + r;
-    return (TQ*)a.out + (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kPgD;
-  };
-
-  if (WIDE && S == 1) {
-    // ---- join in registers: a warp has all of its rows' own keys
-    pdl_wait();   // the prefix's parts
-    if (row0 >= t.rows) return;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float* pr = prefix_row(min(rr[h], t.rows - 1));
-      float top = m[h];
-      for (int i = 0; i < n_pre; ++i) top = fmaxf(top, pr[i * part_step + kPgD]);
-      float w = m[h] == -INFINITY ? 0.f : exp2f(m[h] - top);
-      l[h] *= w;
-#pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        o[c][2 * h] *= w;
-        o[c][2 * h + 1] *= w;
-      }
-      for (int i = 0; i < n_pre; ++i) {
-        const float2 ml = *reinterpret_cast<const float2*>(pr + i * part_step + kPgD);
-        float2 v[16];
-#pragma unroll
-        for (int c = 0; c < 16; ++c) v[c] = *reinterpret_cast<const float2*>(pr + i * part_step + 8 * c + (lane & 3) * 2);
-        w = ml.x == -INFINITY ? 0.f : exp2f(ml.x - top);
-        if (w != 0.f) {
-          l[h] += w * ml.y;
-#pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            o[c][2 * h] += w * v[c].x;
-            o[c][2 * h + 1] += w * v[c].y;
-          }
-        }
-      }
-      const float f = l[h] == 0.f ? 0.f : 1.f / l[h];   // a row without keys: zeros
-      // through this warp's stage, for whole-row stores
-      TQ* srow = reinterpret_cast<TQ*>(smem + (warp * 16 + (lane >> 2) + 8 * h) * (2 * kPgD + 16));
-#pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        const float v[2] = {o[c][2 * h] * f, o[c][2 * h + 1] * f};
-        store_vec<TQ, 2>(srow + 8 * c + (lane & 3) * 2, v);
-      }
-    }
-    __syncwarp();
-    const bool vec = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * 2)) & 15) == 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = 2 * i + (lane >> 4);
-      if (row0 + r >= t.rows) continue;
-      const Vec<TQ, 8> v = *reinterpret_cast<const Vec<TQ, 8>*>(smem + (warp * 16 + r) * (2 * kPgD + 16) + (lane & 15) * 16);
-      TQ* out = out_row(row0 + r) + (lane & 15) * 8;
-      if (vec) {
-        *reinterpret_cast<Vec<TQ, 8>*>(out) = v;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = v.v[e];
-      }
-    }
-    return;
-  }
-
-  // ---- join through shared memory: O rows with (m, l), staged over the rings, of every
-  // warp that had keys of the row (narrow: four) and of every block of the cluster,
-  // and the prefix's parts; at most 32
-  float* stage = reinterpret_cast<float*>(smem);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float* row = stage + (size_t)(warp * 16 + (lane >> 2) + 8 * h) * kPartLd;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) *reinterpret_cast<float2*>(row + 8 * i + (lane & 3) * 2) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
-    if ((lane & 3) == 0) *reinterpret_cast<float2*>(row + kPgD) = make_float2(m[h], l[h]);
-  }
-  pdl_wait();   // the prefix's parts
-  __syncthreads();
-  if (S > 1) {
-    cluster_arrive_release();
-    cluster_wait_acquire();
-  }
-  constexpr int LOCAL = WIDE ? 1 : kPgWarps;
-  const int own = LOCAL * S;
-  auto staged = [&](int r, int i) { return stage + ((WIDE ? 0 : i % LOCAL) * 16 + r) * kPartLd; };
-  join_rows<WIDE ? 4 : 1, WIDE ? 2 : 20>(
-      t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + n_pre,
-      [&](int r, int i) {
-        if (i >= own) return *reinterpret_cast<const float2*>(prefix_row(r) + (i - own) * part_step + kPgD);
-        const float* p = staged(r, i) + kPgD;
-        return S > 1 ? ld_cluster2(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float2*>(p);
-      },
-      [&](int r, int i) {
-        if (i >= own) return *reinterpret_cast<const float4*>(prefix_row(r) + (i - own) * part_step + 4 * lane);
-        const float* p = staged(r, i) + 4 * lane;
-        return S > 1 ? ld_cluster4(dsmem_addr(p, i / LOCAL)) : *reinterpret_cast<const float4*>(p);
-      },
-      [&](int r, float4 x, float, float den) {
-        const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
-        const float v[4] = {x.x * f, x.y * f, x.z * f, x.w * f};
-        TQ* out = out_row(r) + 4 * lane;
-        if (((uintptr_t)out & 7) == 0) {
-          store_vec<TQ, 4>(out, v);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[e] = from_f32<TQ>(v[e]);
-        }
-      });
+      [&](int r, float4 x, float, float den) { store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(x, den)); });
   if (S > 1) {   // a peer may still read this block's rows
     cluster_arrive_release();
     cluster_wait_acquire();
@@ -851,7 +423,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, 2) k_attn_pages_wide(const __gr
 
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms) {
   PagesPlan p;
-  p.tile_rows = rows <= 8ll * n_seqs ? 8 : rows <= 16ll * n_seqs ? 16 : 64;
+  p.tile_rows = rows <= 8ll * n_seqs ? 8 : 16;
   p.tiles = (int)(n_seqs + rows / p.tile_rows);
   // blocks for every SM twice, each with 128 keys at least; a cluster holds 4 ranges
   // (their parts and the prefix's fit the join's 32 lanes)
@@ -889,10 +461,9 @@ static cudaError_t launch_pages(std::atomic<uint64_t>& ready, const void* kernel
 
 template <typename TQ, bool F16>
 static cudaError_t launch_pages_of(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
-  static std::atomic<uint64_t> ready[3] = {};
+  static std::atomic<uint64_t> ready[2] = {};
   if (p.tile_rows == 8) return launch_pages(ready[0], (const void*)k_attn_pages<TQ, F16, 1>, pg_smem(narrow_stages(1)), a, p, st);
-  if (p.tile_rows == 16) return launch_pages(ready[1], (const void*)k_attn_pages<TQ, F16, 2>, pg_smem(narrow_stages(2)), a, p, st);
-  return launch_pages(ready[2], (const void*)k_attn_pages_wide<TQ, F16>, pg_smem(kWideStages), a, p, st);
+  return launch_pages(ready[1], (const void*)k_attn_pages<TQ, F16, 2>, pg_smem(narrow_stages(2)), a, p, st);
 }
 
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st) {

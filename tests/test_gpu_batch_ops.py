@@ -298,6 +298,36 @@ def test_attention_many_rows_long_prefix(dtype, kv):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("shape", ["decode", "ragged", "tree"])
+def test_attention_repeats_bit_for_bit(dtype, kv, shape):
+    """Passes over cold and warm caches, next to another stream's traffic: a copy that is read before it has
+    landed shows as a difference."""
+    counts = {"decode": [1] * 40, "ragged": [100, 300, 17, 64, 33], "tree": [64, 128, 30, 90]}[shape]
+    lens = [c + 37 * (i + 1) % 400 for i, c in enumerate(counts)]
+    d = 64 if kv is F32 else 128
+    parent = [j - 1 if j % 3 else max(-1, j - 3) for c in counts for j in range(c)] if shape == "tree" else None
+    par = torch.tensor(parent, dtype=torch.int32, device="cuda") if parent else None
+    for prefix in (0, 1300):
+        step = R.Step(counts, lens, 16, seed=7)
+        q, pk, pv, kp, vp = inputs(step, prefix, 8, 2, d, dtype, kv)
+        base, st = attend(step, q, pk, pv, prefix, kp, vp, par)
+        ref, mag, size = R.attention(step, q, pk[:prefix], pv[:prefix], kp, vp, 1 / math.sqrt(d), parent)
+        R.check_attention(base, ref, mag, size, prefix + max(lens), F32 if kv is F32 else kv, shape)
+        flush = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+        side = torch.cuda.Stream()
+        outs = []
+        for i in range(12):
+            flush.fill_(i)
+            if i >= 6:
+                with torch.cuda.stream(side):
+                    flush[:1 << 27].copy_(flush[1 << 27:])
+            outs.append(attend(step, q, pk, pv, prefix, kp, vp, par)[0])
+            side.synchronize()
+        torch.cuda.synchronize()
+        assert int(st) == 0 and all(torch.equal(base, o) for o in outs)
+
+
+@pytest.mark.parametrize("dtype, kv", TYPES)
 def test_attention_rows_any_stride(dtype, kv):
     """q a slice of a projection's rows, out a slice of wider rows that starts off 16-byte boundaries."""
     step = R.Step([2, 5], [30, 12], 16)
