@@ -311,7 +311,7 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   if (sms <= 0) return false;
   const int G = nq / c.n_kv_heads;
   const long long rows = (long long)b.n_tokens * G;
-  const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, 1ll << 31);
+  const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, kMaxKeys);
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc) {
     p->few = rows <= 16ll * b.n_seqs;
@@ -370,7 +370,7 @@ static cudaError_t launch_batch_rows(BatchAttnArgs& a, const BatchAttnPlan& p, c
 }
 
 static bool attn_shape_ok(int nq, int prefix_len, const oos_paged_cache* c, const oos_batch* b) {
-  if (!c || !b || nq < 1 || prefix_len < 0 || c->n_kv_heads < 1 || c->page_size < 1 || c->n_pages < 1) return false;
+  if (!c || !b || nq < 1 || prefix_len < 0 || prefix_len > kMaxKeys || c->n_kv_heads < 1 || c->page_size < 1 || c->n_pages < 1) return false;
   if (nq % c->n_kv_heads || c->n_kv_heads > 65535 || b->n_seqs < 1 || b->n_tokens < 0 || b->max_pages < 1) return false;
   return (long long)b->n_tokens * nq + b->n_seqs < (1ll << 31) / kMaxParts && nq <= (1 << 20);
 }

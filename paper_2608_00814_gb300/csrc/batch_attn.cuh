@@ -8,6 +8,7 @@ namespace oos {
 
 constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
 constexpr int kPartLd = 128 + 4;   // a row of a part: O, m, l, padded to 16 bytes
+constexpr int kMaxKeys = 0x7fffff00;   // of a prefix or a sequence: tiles of keys past the last still count in 32 bits
 
 struct BatchAttnArgs {
   PagesView pages;
@@ -55,8 +56,8 @@ OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRow
   const BatchView& b = a.batch;
   auto start = [&](int s) { return s + (long long)b.q_start[s] * a.group / tile_rows; };
   const int seq = warp_count_le(b.n_seqs - 1, start, i);
-  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = b.seq_len[seq];
-  const long long most = (long long)b.max_pages * a.pages.page_size;
+  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = max(0, b.seq_len[seq]);
+  const long long most = min((long long)b.max_pages * a.pages.page_size, (long long)kMaxKeys);
   bool ok = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1 && (!a.parent || q1 - q0 <= kMaxTreeRows);
   if (!ok || len < q1 - q0 || len > most) {
     if (threadIdx.x == 0) *a.status = ok || !a.parent ? OOS_EBATCH : OOS_ETREE;

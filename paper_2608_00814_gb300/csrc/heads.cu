@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kHeadWarps * 32, 4) k_heads(const HeadArgs a, 
     const int seq = warp_count_le(b.n_seqs, [&](int i) { return (long long)b.q_start[i]; }, t);
     if (seq >= b.n_seqs) return;                       // behind the last sequence
     const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1];
-    slot = t < q0 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, b.seq_len[seq] - (q1 - (int)t));
+    slot = t < q0 || t >= q1 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, b.seq_len[seq] - (q1 - (int)t));
     if (slot < 0) {
       if (lane == 0) *a.status = OOS_EBATCH;
       return;
@@ -252,7 +252,7 @@ bool pages_ok(const oos_paged_cache* c) {
   return c->n_kv_heads >= 1 && c->page_size >= 1 && c->n_pages >= 1 && c->k && c->v;
 }
 bool batch_ok(const oos_batch* b) {
-  return b->n_seqs >= 1 && b->n_tokens >= 0 && b->max_pages >= 1 && b->q_start && b->seq_len && b->block_table;
+  return b->n_seqs >= 1 && b->n_seqs <= (1 << 30) && b->n_tokens >= 0 && b->max_pages >= 1 && b->q_start && b->seq_len && b->block_table;
 }
 
 // Rows of the widest access: 16 bytes of T (and the same count of O) where half a

@@ -71,7 +71,7 @@ def append(L, c=None, b=None, dtype=B.OOS_DTYPE_BF16, k=P, ks=256, v=P, vs=256, 
 
 
 BAD_CACHES = [dict(nkv=0), dict(page=0), dict(n_pages=0), dict(k=NULL), dict(v=NULL)]
-BAD_BATCHES = [dict(n_seqs=0), dict(n_tokens=-1), dict(width=0), dict(q_start=NULL), dict(seq_len=NULL), dict(table=NULL)]
+BAD_BATCHES = [dict(n_seqs=0), dict(n_seqs=2 ** 31 - 1), dict(n_tokens=-1), dict(width=0), dict(q_start=NULL), dict(seq_len=NULL), dict(table=NULL)]
 
 
 @pytest.mark.parametrize("bad", [dict(k=NULL), dict(v=NULL), dict(ks=255), dict(vs=255), dict(eps=-1.0),
@@ -93,7 +93,7 @@ def attention(L, c=None, b=None, dtype=B.OOS_DTYPE_BF16, nq=4, q=P, qs=512, pk=P
                                          out, os_, ws, ws_bytes, status, NULL)
 
 
-@pytest.mark.parametrize("bad", [dict(nq=0), dict(nq=5), dict(prefix=-1), dict(pk=NULL), dict(pv=NULL), dict(q=NULL),
+@pytest.mark.parametrize("bad", [dict(nq=0), dict(nq=5), dict(prefix=-1), dict(prefix=2 ** 31 - 1), dict(pk=NULL), dict(pv=NULL), dict(q=NULL),
                                  dict(out=NULL), dict(qs=511), dict(os_=511), dict(scale=0.0), dict(scale=-1.0),
                                  dict(scale=float("nan")), dict(scale=float("inf")), dict(status=NULL),
                                  dict(pk=P + 8), dict(pv=P + 2), dict(c=cache(k=P + 8)), dict(c=cache(v=P + 4)),

@@ -180,6 +180,21 @@ def test_append_reports_rows_without_a_place():
         assert torch.equal(kp, want), what
 
 
+def test_append_offsets_out_of_order():
+    """A row that its sequence's offsets do not hold is left out and reported, whatever the search finds."""
+    k, v = randn(gen(1), 6, 1, 64, dtype=F32), randn(gen(2), 6, 1, 64, dtype=F32)
+    kp = torch.zeros(4, 16, 1, 64, device="cuda")
+    vp = torch.zeros_like(kp)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    # row 5 counts two offsets not above it, and so falls to sequence 2, whose only row is row 1
+    batch = B.Batch(torch.tensor([0, 9, 1, 2], **i32), torch.tensor([9, 1, 1], **i32),
+                    torch.tensor([[0], [1], [2]], **i32), 6)
+    st = status()
+    B.oos_paged_append(B.PagedCache(kp, vp), batch, k, v, None, 1e-6, None, None, st)
+    assert int(st) == B.OOS_EBATCH
+    assert bool((kp[2, 1:] == 0).all()) and bool((vp[2, 1:] == 0).all())
+
+
 def test_append_far_pages():
     """Positions past 2^31 elements of the pool."""
     nkv, d, page = 8, 128, 64
@@ -444,6 +459,15 @@ def test_attention_reports_bad_batches(dtype, kv):
     fine = torch.tensor([-1, -1, -1, -1], dtype=torch.int32, device="cuda")
     ref, st = attend(good, q, None, None, 0, kp, vp, parent=fine)
     assert int(st) == 0 and torch.equal(ref, out)
+    # a length of any value: only the extremes' own rows are affected
+    for n in (-1, -2 ** 31, 2 ** 31 - 1):
+        for parents in (None, fine):
+            step = R.Step([1, 2, 1], [40, 2, 30], page)
+            ref, st = attend(step, q, None, None, 0, kp, vp, parent=parents)
+            step.lens[1] = n
+            out, st = attend(step, q, None, None, 0, kp, vp, parent=parents)
+            assert int(st) == B.OOS_EBATCH
+            assert torch.equal(out[0], ref[0]) and torch.equal(out[3], ref[3])
     # offsets that decrease or pass the rows: reported, and the sequence in order keeps its result
     step = R.Step([1, 2, 1], [40, 2, 30], page)
     step.q_start = [0, 1, 9, 4]
