@@ -318,7 +318,7 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     p->sequence = {false, 0, 1};
     if (p->few) p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, prefix_len, most_keys, sms);
-    p->prefix = prefix_len > 0 && !p->sequence.takes_prefix ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, sms)
+    p->prefix = prefix_len > 0 && !p->sequence.takes_prefix ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->few ? p->pages.sms : 0, sms)
                                                             : PrefixPlan{0, 0, 0.0};
     const int parts = p->prefix.splits + (p->sequence.splits > 1 ? p->sequence.splits : 0);
     p->ml_off = 0;

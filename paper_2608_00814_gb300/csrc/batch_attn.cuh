@@ -221,10 +221,12 @@ struct PrefixPlan {
   int pairs;    // pairs of 128-row tiles
   double us;    // estimated
 };
-PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int n_sms);
+// own_sms: that the blocks of the sequences' own keys would fill, 0 where that is not known
+PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, int n_sms);
 struct PagesPlan {
   int tile_rows;   // of a block: 8 or 16
   int tiles, splits;
+  int sms;         // that its blocks fill at once, about
 };
 struct SequencePlan {
   bool takes_prefix;   // in the same kernel

@@ -27,6 +27,7 @@ namespace oos {
 
 constexpr int kPgWarps = 4;
 __host__ __device__ constexpr int narrow_stages(int nt) { return nt == 1 ? 2 : 3; }
+__host__ __device__ constexpr int pg_blocks(int nt) { return nt == 1 ? 3 : 2; }   // per SM
 constexpr int kPgD = 128;
 constexpr int kPgRow = 2 * kPgD;                 // bytes of a key row
 constexpr int kPgChunkBytes = 2 * 16 * kPgRow;   // 16 keys, K and V
@@ -98,7 +99,7 @@ OOS_DEV bool chunk_not_finite(uint32_t buf, int pieces) {
 // rows and NT * 8 query rows on its columns, so that a decoding token's group of up to 8
 // heads costs one product of 8 columns where rows of 16 would cost two.
 template <typename TQ, bool F16, int NT>
-__global__ void __launch_bounds__(kPgWarps * 32, NT == 1 ? 3 : 2) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
+__global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int ROWS = 8 * NT, STAGES = narrow_stages(NT);
   constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
@@ -429,6 +430,9 @@ PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys
   // (their parts and the prefix's fit the join's 32 lanes)
   const long long want = 4ll * n_sms / std::max(1ll, (long long)p.tiles * nkv);
   p.splits = (int)std::max(1ll, std::min({want, most_keys / 128, 4ll}));
+  const long long live = std::max((long long)n_seqs, (rows + p.tile_rows - 1) / p.tile_rows) * nkv * p.splits;
+  const int per_sm = pg_blocks(p.tile_rows / 8);
+  p.sms = (int)std::min<long long>(n_sms, (live + per_sm - 1) / per_sm);
   return p;
 }
 

@@ -726,20 +726,25 @@ constexpr double kTlTileUs = 0.83, kTlBlockUs = 8.0, kTlSeqBlockUs = 12.0;
 static double waves(long long blocks, int n_sms) { return (double)((blocks + n_sms - 1) / n_sms); }   // one block per SM
 
 // The count of key ranges with the shortest schedule: waves, each of a block's tiles and
-// its beginning and end, and the parts, written and read once at about 8 bytes per ps.
-PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int n_sms) {
+// its beginning and end, and the parts, written and read at about 3 bytes per ps together
+// (64 sequences of one token, 32 heads over 8192 keys: 11 ranges 50 us with the pages', 16
+// at 8 bytes per ps 53).  Where the pages' blocks, own_sms of them full, then fit beside
+// them, and the prefix's kernel is not estimated a quarter longer for it, fewer: the two
+// kernels run at once (8 sequences: 8 ranges 21 us, 10 or 16 27).
+PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, int n_sms) {
   PrefixPlan p;
   p.pairs = (int)((rows + 2 * kTlRows - 1) / (2 * kTlRows));
   p.splits = 1;
-  p.us = 0;
   const int tiles = (prefix_len + kTlKeys - 1) / kTlKeys;
-  const double tile = (rows > kTlRows ? 2 : 1) * kTlTileUs, part = 2.0 * rows * nkv * kPartLd * 4 / 8e6;
-  for (int s = 1; s <= kTlMaxSplits && s <= tiles; ++s) {
-    const double us = waves((long long)p.pairs * nkv * s, n_sms) * (tile * ((tiles + s - 1) / s) + kTlBlockUs) + part * s;
-    if (s > 1 && us >= p.us) continue;
-    p.us = us;
-    p.splits = s;
-  }
+  const double tile = (rows > kTlRows ? 2 : 1) * kTlTileUs, part = 2.0 * rows * nkv * kPartLd * 4 / 3e6;
+  auto us = [&](int s) {
+    return waves((long long)p.pairs * nkv * s, n_sms) * (tile * ((tiles + s - 1) / s) + kTlBlockUs) + part * s;
+  };
+  for (int s = 2; s <= kTlMaxSplits && s <= tiles; ++s)
+    if (us(s) < us(p.splits)) p.splits = s;
+  const int beside = (int)std::min<long long>(kTlMaxSplits, (n_sms - own_sms) / ((long long)p.pairs * nkv));
+  if (own_sms > 0 && beside >= 1 && beside < p.splits && us(beside) <= 1.25 * us(p.splits)) p.splits = beside;
+  p.us = us(p.splits);
   return p;
 }
 
@@ -769,7 +774,7 @@ SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_le
   const double with_prefix = schedule(pre + 2.0, pre + own, 0.0, &split_with);
   p.takes_prefix = false;
   if (pre > 0) {
-    const PrefixPlan apart = plan_prefix_tc(rows, nkv, prefix_len, n_sms);
+    const PrefixPlan apart = plan_prefix_tc(rows, nkv, prefix_len, 0, n_sms);
     p.takes_prefix = with_prefix <= apart.us + schedule(2.0, own, 2.0 * apart.splits, &split_own);
   }
   if (!p.takes_prefix) schedule((double)std::min(own, 8ll), own, 0.0, &split_own);
