@@ -221,7 +221,7 @@ struct PrefixPlan {
   int pairs;    // pairs of 128-row tiles
   double us;    // estimated
 };
-// own_sms: that the blocks of the sequences' own keys would fill, 0 where that is not known
+// own_sms: that the blocks of launch_pages_tc would fill, 0 where that kernel does not follow
 PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, int n_sms);
 struct PagesPlan {
   int tile_rows;   // of a block: 8 or 16

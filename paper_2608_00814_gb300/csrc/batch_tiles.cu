@@ -726,17 +726,18 @@ constexpr double kTlTileUs = 0.83, kTlBlockUs = 8.0, kTlSeqBlockUs = 12.0;
 static double waves(long long blocks, int n_sms) { return (double)((blocks + n_sms - 1) / n_sms); }   // one block per SM
 
 // The count of key ranges with the shortest schedule: waves, each of a block's tiles and
-// its beginning and end, and the parts, written and read at about 3 bytes per ps together
-// (64 sequences of one token, 32 heads over 8192 keys: 11 ranges 50 us with the pages', 16
-// at 8 bytes per ps 53).  Where the pages' blocks, own_sms of them full, then fit beside
-// them, and the prefix's kernel is not estimated a quarter longer for it, fewer: the two
-// kernels run at once (8 sequences: 8 ranges 21 us, 10 or 16 27).
+// its beginning and end, and the parts, written and read once at about 8 bytes per ps, or
+// 3 where the pages' kernel of few rows reads them (64 sequences of one token, 32 heads
+// over 8192 keys: 11 ranges 50 us with the pages', 16 by 8 bytes per ps 53).  Where that
+// kernel's blocks, own_sms full of them, then fit beside these, and these are not estimated
+// a quarter longer for it, fewer: the two run at once (8 sequences: 8 ranges 21 us, 10 or
+// 16 27).
 PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, int n_sms) {
   PrefixPlan p;
   p.pairs = (int)((rows + 2 * kTlRows - 1) / (2 * kTlRows));
   p.splits = 1;
   const int tiles = (prefix_len + kTlKeys - 1) / kTlKeys;
-  const double tile = (rows > kTlRows ? 2 : 1) * kTlTileUs, part = 2.0 * rows * nkv * kPartLd * 4 / 3e6;
+  const double tile = (rows > kTlRows ? 2 : 1) * kTlTileUs, part = 2.0 * rows * nkv * kPartLd * 4 / (own_sms > 0 ? 3e6 : 8e6);
   auto us = [&](int s) {
     return waves((long long)p.pairs * nkv * s, n_sms) * (tile * ((tiles + s - 1) / s) + kTlBlockUs) + part * s;
   };
