@@ -484,7 +484,7 @@ int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32
  *              OOS_ETIMEOUT when a pipeline wait exceeded 2 s (out is not valid).
  * Sums and softmax statistics are fp32.  scale > 0.  Pages and prefix of 16-bit
  * types start on 16-byte boundaries, and n_tokens * n_q_heads + n_seqs is below
- * 2^26 (OOS_EINVAL otherwise), as prefix_len is up to 2^31 - 256 and a sequence's
+ * 2^26 (OOS_EINVAL otherwise), as prefix_len is up to 2^31 - 4096 and a sequence's
  * length (OOS_EBATCH otherwise).  With OOS_EBATCH for a sequence's offsets, or
  * OOS_ETREE for more than 128 of its rows, its rows of out are not valid. */
 size_t oos_shared_prefix_attention_workspace_bytes(int32_t n_q_heads, int32_t prefix_len, const oos_paged_cache* cache,

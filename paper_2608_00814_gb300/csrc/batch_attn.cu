@@ -269,11 +269,36 @@ __global__ void __launch_bounds__(256) k_attn_join_parts(const __grid_constant__
   if (token >= a.batch.q_start[a.batch.n_seqs] || token < a.batch.q_start[0]) return;   // padding
   const long long step = (long long)a.pages.nkv * rows * kPartLd;
   const float* p = a.part_o + (long long)row * kPartLd;
-  join_rows<1, 8>(
-      0, 1, 0, 1, a.p_splits + a.s_splits,
-      [&](int, int i) { return *reinterpret_cast<const float2*>(p + i * step + 128); },
-      [&](int, int i) { return *reinterpret_cast<const float4*>(p + i * step + 4 * lane); },
-      [&](int, float4 o, float, float den) { store_row<T>(a, g, 0, r, weighted_mean(o, den)); });
+  const int parts = a.p_splits + a.s_splits;   // <= 32, a lane each
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < parts) ml = *reinterpret_cast<const float2*>(p + lane * step + 128);
+  constexpr int U = 8;   // parts on their way at once
+  float4 v[U];
+  auto fetch = [&](int p0) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (p0 + i < parts) v[i] = *reinterpret_cast<const float4*>(p + (p0 + i) * step + 4 * lane);
+  };
+  fetch(0);
+  const bool on = ml.x != -INFINITY;   // a NaN is, and reaches the sum
+  const float top = warp_max(ml.x);
+  const float w = on ? exp2f(ml.x - top) : 0.f;
+  const float den = warp_sum(on ? w * ml.y : 0.f);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int p0 = 0; p0 < parts; p0 += U) {
+    if (p0 > 0) fetch(p0);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const float wi = __shfl_sync(0xffffffffu, w, (p0 + i) & 31);
+      if (p0 + i >= parts || wi == 0.f) continue;   // a part without weight counts for nothing, whatever it holds
+      acc.x += wi * v[i].x;
+      acc.y += wi * v[i].y;
+      acc.z += wi * v[i].z;
+      acc.w += wi * v[i].w;
+    }
+  }
+  store_row<T>(a, g, 0, r, weighted_mean(acc, den));
 }
 
 // ---- host: how a call is cut up

@@ -7,8 +7,9 @@
 namespace oos {
 
 constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
+constexpr int kMaxPrefixParts = 16;   // of a row, of the tensor-core kernels
 constexpr int kPartLd = 128 + 4;   // a row of a part: O, m, l, padded to 16 bytes
-constexpr int kMaxKeys = 0x7fffff00;   // of a prefix or a sequence: tiles of keys past the last still count in 32 bits
+constexpr int kMaxKeys = 0x7ffff000;   // of a prefix or a sequence: tiles of keys past the last still count in 32 bits
 
 struct BatchAttnArgs {
   PagesView pages;
@@ -120,63 +121,6 @@ OOS_DEV void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memo
 template <int N>
 OOS_DEV void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-// Rows lo + warp, + n_warps, .. below hi, a warp per row and R rows at a time: part i
-// of row r has (m, l) = ml_of(r, i), its four columns of this lane v_of(r, i), i < parts
-// <= 32.  out(r, O, max m, weighted l) takes the sum.  The first UNROLL parts' columns
-// are on their way before the weights are known: one row and one part at a time, the
-// join waited 2 us a row.
-template <int R, int UNROLL, typename ML, typename V, typename OUT>
-OOS_DEV void join_rows(int lo, int hi, int warp, int n_warps, int parts, ML ml_of, V v_of, OUT out) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll 1
-  for (int r0 = lo + warp; r0 < hi; r0 += R * n_warps) {
-    float2 ml[R];
-    float w[R], top[R], den[R];
-    float4 acc[R], v[UNROLL][R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int r = r0 + k * n_warps;
-      ml[k] = make_float2(-INFINITY, 0.f);
-      if (r < hi && lane < parts) ml[k] = ml_of(r, lane);
-    }
-    auto fetch = [&](int i0) {
-#pragma unroll
-      for (int i = 0; i < UNROLL; ++i)
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-          if (i0 + i < parts) v[i][k] = v_of(min(r0 + k * n_warps, hi - 1), i0 + i);
-    };
-    fetch(0);
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const bool on = ml[k].x != -INFINITY;   // a NaN is, and reaches the sum
-      top[k] = warp_max(ml[k].x);
-      w[k] = on ? exp2f(ml[k].x - top[k]) : 0.f;
-      den[k] = warp_sum(on ? w[k] * ml[k].y : 0.f);
-      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-#pragma unroll 1
-    for (int i0 = 0; i0 < parts; i0 += UNROLL) {
-      if (i0 > 0) fetch(i0);
-#pragma unroll
-      for (int i = 0; i < UNROLL; ++i)
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-          const float wi = __shfl_sync(0xffffffffu, w[k], (i0 + i) & 31);
-          if (i0 + i < parts && wi != 0.f) {   // a part without weight counts for nothing, whatever it holds
-            acc[k].x += wi * v[i][k].x;
-            acc[k].y += wi * v[i][k].y;
-            acc[k].z += wi * v[i][k].z;
-            acc[k].w += wi * v[i][k].w;
-          }
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < R; ++k)
-      if (r0 + k * n_warps < hi) out(r0 + k * n_warps, acc[k], top[k], den[k]);
-  }
 }
 
 // Row `row` of the sequence that starts at token q0, kv head g: the lane's four columns

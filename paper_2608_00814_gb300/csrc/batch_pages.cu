@@ -9,8 +9,16 @@
 // keys are dealt to the block's four warps in chunks of 16, each warp with a ring of its
 // own, no block barrier before the end; several blocks per SM cover each other's waits.
 // Products run on mma.sync m16n8k16, operands by ldmatrix from rows whose 16-byte chunks
-// are swizzled by the key.  Bound by HBM, and below about 300 keys by the lookups that
-// follow each other.
+// are swizzled by the key.
+//
+// Long sequences are bound by HBM (16 of 2000 keys on average, 8 kv heads: 49 us with the
+// prefix's kernel beside it, the bytes take 26), short ones by what a block does once --
+// lookups that follow each other, query fragments, the join -- at the 12 warps per SM that
+// the registers leave (256 of 150 keys, 2048 blocks: 40 us for 23 us of bytes; 47 before
+// the join took own and prefix's parts apart and lookups lost their divisions).  Fewer
+// warps a block and more blocks (2 x 6, 3 x 4 per SM) took 45 and 41 us where 4 x 3 took
+// 34; blocks that stay and take chunk after chunk, their parts joined by a kernel of its
+// own, 40.
 //
 // Every row keeps its maximum, moved only when a chunk exceeds it by 2^8, and its sum in
 // fp32.  Weights enter P.V as binary16, or as two bf16 halves, whose second product costs
@@ -36,11 +44,6 @@ static_assert(kPgWarps * 8 * kPartLd * 4 <= pg_smem(2) && kPgWarps * 16 * kPartL
 
 OOS_DEV void lds128(uint32_t addr, uint32_t (&w)[4]) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr) : "memory");
-}
-OOS_DEV uint32_t lds32(uint32_t addr) {
-  uint32_t w;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(addr) : "memory");
-  return w;
 }
 OOS_DEV uint32_t lds16(uint32_t addr) {
   uint16_t w;
@@ -79,19 +82,18 @@ OOS_DEV void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// whether a value of the chunk's V is infinite or NaN (16-key pieces at buf)
+// whether a value of the V of the 16 keys at buf is infinite or NaN
 template <bool F16>
-OOS_DEV bool chunk_not_finite(uint32_t buf, int pieces) {
+OOS_DEV bool chunk_not_finite(uint32_t buf) {
   constexpr uint32_t kExp = F16 ? 0x7c007c00u : 0x7f807f80u;
   uint32_t bad = 0;
-  for (int j = 0; j < pieces; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint32_t w[4];
-      lds128(buf + j * kPgChunkBytes + 16 * kPgRow + (i * 32 + (threadIdx.x & 31)) * 16, w);
+  for (int i = 0; i < 8; ++i) {
+    uint32_t w[4];
+    lds128(buf + 16 * kPgRow + (i * 32 + (threadIdx.x & 31)) * 16, w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) bad |= __vcmpeq2(w[e] & kExp, kExp);
-    }
+    for (int e = 0; e < 4; ++e) bad |= __vcmpeq2(w[e] & kExp, kExp);
+  }
   return __any_sync(0xffffffffu, bad != 0);
 }
 
@@ -122,16 +124,29 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
   const int n_chunks = max(0, k1 - k0 + 63) / 64;             // of 64 keys, 16 per warp
 
   // ---- the first page lookups and the queries' loads go out together
-  auto slot_of = [&](int c) -> long long {   // lane & 15: a key of this warp's 16 in chunk c
-    const int key = k0 + c * 64 + warp * 16 + (lane & 15);
-    if (c >= n_chunks || key >= k1) return -1;
-    const long long at = page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
-    if (at < 0) *a.status = OOS_EBATCH;
+  int key = k0 + warp * 16 + (lane & 15);   // of this warp's 16 in the chunk that is looked up next
+  int col = key / a.pages.page_size, in_page = key - col * a.pages.page_size;
+  const int* table = a.batch.table + (size_t)t.seq * a.batch.max_pages;
+  const int cols = 64 / a.pages.page_size, rest = 64 - cols * a.pages.page_size;   // of a chunk
+  auto next_slot = [&]() {   // its place in the pages, -1: none
+    long long at = -1;
+    if (key < k1) {   // no further than the table
+      const int page = __ldg(table + col);
+      if (page >= 0 && page < a.pages.n_pages) at = (long long)page * a.pages.page_size + in_page;
+      else *a.status = OOS_EBATCH;
+    }
+    key += 64;
+    col += cols;
+    in_page += rest;
+    if (in_page >= a.pages.page_size) {
+      in_page -= a.pages.page_size;
+      ++col;
+    }
     return at;
   };
   long long slot[STAGES];
 #pragma unroll
-  for (int c = 0; c < STAGES; ++c) slot[c] = slot_of(c);
+  for (int c = 0; c < STAGES; ++c) slot[c] = next_slot();
   // B fragments of the query rows, all of d: column lane / 4 of each 8 rows
   uint32_t qf[8][NT][2];
 #pragma unroll
@@ -245,7 +260,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
     for (int i = 0; i + 2 < STAGES; ++i) valid[i] = valid[i + 1];
     copy(c + STAGES - 1, next);
     valid[STAGES - 2] = __ballot_sync(0xffffffffu, next >= 0) & 0xffffu;
-    next = slot_of(c + STAGES);
+    next = next_slot();
     const int key0 = k0 + c * 64 + warp * 16;
     // nothing there, or no row that sees the first key (warp-uniform)
     if (there == 0 || (!anc && key0 > t.first + tok_hi)) continue;
@@ -285,7 +300,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
       }
     // A key that some of the rows do not see must not reach them through 0 times a v
     // that is not finite: such a chunk (the last ones of a sequence only) is summed apart.
-    const bool apart = !full && chunk_not_finite<F16>(buf, 1);
+    // One token's rows see all keys that are there, unless a tree hides its siblings.
+    const bool apart = !full && (anc || tok_lo != tok_hi) && chunk_not_finite<F16>(buf);
     bool move = false;
     float mn[NT][2];
 #pragma unroll
@@ -401,21 +417,53 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
   }
   const int own = kPgWarps * S;
   const long long part_rows = (long long)a.batch.n_tokens * a.group, part_step = (long long)a.pages.nkv * part_rows * kPartLd;
-  auto part = [&](int r, int i) {   // part i of row r: a staged one (its address in this block), or the prefix's
-    return i < own ? stage + ((i % kPgWarps) * ROWS + r) * kPartLd
-                   : a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0 + r) * kPartLd + (i - own) * part_step;
-  };
-  join_rows<1, 20>(
-      t.rows * split / S, t.rows * (split + 1) / S, warp, kPgWarps, own + a.p_splits,
-      [&](int r, int i) {
-        const float* p = part(r, i) + kPgD;
-        return i < own && S > 1 ? ld_cluster2(dsmem_addr(p, i / kPgWarps)) : *reinterpret_cast<const float2*>(p);
-      },
-      [&](int r, int i) {
-        const float* p = part(r, i) + 4 * lane;
-        return i < own && S > 1 ? ld_cluster4(dsmem_addr(p, i / kPgWarps)) : *reinterpret_cast<const float4*>(p);
-      },
-      [&](int r, float4 x, float, float den) { store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(x, den)); });
+  const float* pre = a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0) * kPartLd;
+#pragma unroll 1
+  for (int r = t.rows * split / S + warp; r < t.rows * (split + 1) / S; r += kPgWarps) {
+    // a lane per part; the prefix's columns are on their way before the weights are known
+    constexpr int U = 16;
+    static_assert(U >= kMaxPrefixParts, "all of them");
+    const float* mine = stage + (lane % kPgWarps * ROWS + r) * kPartLd + kPgD;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < own) ml = S > 1 ? ld_cluster2(dsmem_addr(mine, lane / kPgWarps)) : *reinterpret_cast<const float2*>(mine);
+    else if (lane < own + a.p_splits) ml = *reinterpret_cast<const float2*>(pre + (lane - own) * part_step + r * kPartLd + kPgD);
+    float4 v[U];
+    if (a.p_splits > 0) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (i < a.p_splits) v[i] = *reinterpret_cast<const float4*>(pre + i * part_step + r * kPartLd + 4 * lane);
+    }
+    const bool on = ml.x != -INFINITY;   // a NaN is, and reaches the sum
+    const float top = warp_max(ml.x);
+    const float w = on ? exp2f(ml.x - top) : 0.f;
+    const float den = warp_sum(on ? w * ml.y : 0.f);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](int i, const float4& x) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      if (wi == 0.f) return;   // a part without weight counts for nothing, whatever it holds
+      acc.x += wi * x.x;
+      acc.y += wi * x.y;
+      acc.z += wi * x.z;
+      acc.w += wi * x.w;
+    };
+#pragma unroll 1
+    for (int s = 0; s < S; ++s) {
+      float4 x[kPgWarps];
+#pragma unroll
+      for (int i = 0; i < kPgWarps; ++i) {
+        const float* p = stage + (i * ROWS + r) * kPartLd + 4 * lane;
+        x[i] = S > 1 ? ld_cluster4(dsmem_addr(p, s)) : *reinterpret_cast<const float4*>(p);
+      }
+#pragma unroll
+      for (int i = 0; i < kPgWarps; ++i) add(s * kPgWarps + i, x[i]);
+    }
+    if (a.p_splits > 0) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (i < a.p_splits) add(own + i, v[i]);
+    }
+    store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(acc, den));
+  }
   if (S > 1) {   // a peer may still read this block's rows
     cluster_arrive_release();
     cluster_wait_acquire();

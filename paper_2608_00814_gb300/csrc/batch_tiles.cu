@@ -58,7 +58,7 @@ constexpr int kTlSmem = kTlOffBar + 320 + 1024;           // + alignment slack
 constexpr int kTlThreads = 384;
 constexpr int kTlSoft0 = 4;                               // softmax warps 4..7 and 8..11
 constexpr int kTlRegsIo = 88, kTlRegsSoft = 208, kTlRegsLaunch = 168;
-constexpr int kTlMaxSplits = 16;
+constexpr int kTlMaxSplits = kMaxPrefixParts;
 static_assert(128 * kTlRegsIo + (kTlThreads - 128) * kTlRegsSoft <= kTlThreads * kTlRegsLaunch, "register split");
 static_assert(2 * kTlRows * ((kPartLd + kTlMaxSplits + 2) * 4 + 8) <= kTlOffQ, "staged rows and their weights over the ring");
 static_assert(kTlSmem <= 227 * 1024, "shared memory per block");
