@@ -40,6 +40,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   __shared__ TreeScratch s_tree;
   __shared__ long long s_at[kRowKeys];      // slot of each key in its buffer, -1: none
 
+  pdl_wait();
   pdl_trigger();
   const int g = blockIdx.y;
   const bool prefix = (int)blockIdx.x < a.p_tiles * a.p_splits;
@@ -222,6 +223,7 @@ __global__ void __launch_bounds__(128) k_attn_join(const BatchAttnArgs a) {
   const int lane = threadIdx.x & 31, d = a.pages.d;
   const long long n_rows = (long long)a.batch.n_tokens * a.nq;
   pdl_wait();
+  pdl_trigger();
   if (row >= n_rows) return;
   const long long token = row / a.nq;
   if (token >= a.batch.q_start[a.batch.n_seqs] || token < a.batch.q_start[0]) return;   // padding
@@ -263,6 +265,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_attn_join_parts(const __grid_constant__ BatchAttnArgs a) {
   const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;   // of [kv head][token * group + head]
   pdl_wait();
+  pdl_trigger();
   const int rows = a.batch.n_tokens * a.group;
   if (row >= rows * a.pages.nkv) return;
   const int g = row / rows, r = row - g * rows, token = r / a.group;
@@ -374,7 +377,7 @@ static cudaError_t launch_rows(const BatchAttnArgs& a, int blocks, cudaStream_t 
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = kernel_ready(ready, (const void*)k_attn_rows<TQ, TK, RT, VEC>, smem_of(kMaxHeadDim + 4));
   if (e != cudaSuccess) return e;
-  e = launch(false, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
+  e = launch(true, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.batch.n_tokens * a.nq;
   return launch(true, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);

@@ -108,6 +108,9 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
   __shared__ TreeScratch s_tree;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = blockIdx.y, S = a.s_splits, split = blockIdx.x % S;
+  // behind the prefix's kernel, which has waited for what the caller wrote before it
+  // triggers, only the join waits
+  if (a.p_splits == 0) pdl_wait();
   pdl_trigger();
   TileRows t;
   if (!sequence_tile(a, blockIdx.x / S, ROWS, &t)) {          // the whole cluster
@@ -501,10 +504,8 @@ static cudaError_t launch_pages(std::atomic<uint64_t>& ready, const void* kernel
     attr[n].val.clusterDim.y = 1;
     attr[n++].val.clusterDim.z = 1;
   }
-  if (a.prefix_len > 0) {   // starts while the prefix's kernel drains, and waits for it before the join
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
+  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // starts while the prefix's kernel drains
+  attr[n++].val.programmaticStreamSerializationAllowed = 1;
   lc.attrs = attr;
   lc.numAttrs = n;
   void* args[1] = {const_cast<BatchAttnArgs*>(&a)};

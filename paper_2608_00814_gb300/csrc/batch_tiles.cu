@@ -159,7 +159,10 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
   int32_t* status = a.status;
   const int S = SEQ ? a.s_splits : a.p_splits, split = blockIdx.x % S, pair = blockIdx.x / S, g = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_trigger();
+  // behind the prefix's kernel, which has waited for what the caller wrote before it
+  // triggers, only the end waits for the prefix's parts
+  if (SEQ && a.p_splits == 0) pdl_wait();
+  if (SEQ) pdl_trigger();
   TileRows t = {};
   if constexpr (SEQ) {
     if (!sequence_tile(a, pair, 2 * kTlRows, &t)) {
@@ -204,6 +207,10 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (!SEQ) {   // the kernel before ran under the set-up
+    pdl_wait();
+    pdl_trigger();
+  }
   const uint32_t tmem = *tmem_slot;
   float* stage = reinterpret_cast<float*>(sm);
 
@@ -713,11 +720,11 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
 
 // ---- host
 template <typename TQ, bool F16, bool SEQ>
-static cudaError_t launch_tiles(const TileArgs& p, dim3 grid, bool follows, cudaStream_t st) {
+static cudaError_t launch_tiles(const TileArgs& p, dim3 grid, cudaStream_t st) {
   // the register split must not ask for more than the block is launched with
   static std::atomic<uint64_t> ready{0};
   const cudaError_t e = kernel_ready(ready, (const void*)k_attn_tiles<TQ, F16, SEQ>, kTlSmem, kTlRegsLaunch);
-  return e == cudaSuccess ? launch(follows, k_attn_tiles<TQ, F16, SEQ>, grid, dim3(kTlThreads), kTlSmem, st, p) : e;
+  return e == cudaSuccess ? launch(true, k_attn_tiles<TQ, F16, SEQ>, grid, dim3(kTlThreads), kTlSmem, st, p) : e;
 }
 
 // us: a row tile's work on a key tile, and a block's beginning and end (with pages: the
@@ -798,9 +805,9 @@ cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& plan, int
   const bool f16 = kv_dtype == OOS_DTYPE_F16;
   if (!encode_prefix(a, f16, &p)) return cudaErrorInvalidValue;
   const dim3 grid((unsigned)(plan.pairs * plan.splits), a.pages.nkv);
-  if (!f16) return launch_tiles<__nv_bfloat16, false, false>(p, grid, false, st);
-  if (dtype == OOS_DTYPE_BF16) return launch_tiles<__nv_bfloat16, true, false>(p, grid, false, st);
-  return launch_tiles<__half, true, false>(p, grid, false, st);
+  if (!f16) return launch_tiles<__nv_bfloat16, false, false>(p, grid, st);
+  if (dtype == OOS_DTYPE_BF16) return launch_tiles<__nv_bfloat16, true, false>(p, grid, st);
+  return launch_tiles<__half, true, false>(p, grid, st);
 }
 
 cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& plan, int dtype, int kv_dtype, cudaStream_t st) {
@@ -808,12 +815,12 @@ cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& plan,
   memset(&p, 0, sizeof(p));
   p.a = a;
   p.part0 = a.p_splits;
-  const bool f16 = kv_dtype == OOS_DTYPE_F16, follows = a.p_splits > 0;
+  const bool f16 = kv_dtype == OOS_DTYPE_F16;
   if (a.prefix_len > 0 && plan.takes_prefix && !encode_prefix(a, f16, &p)) return cudaErrorInvalidValue;
   const dim3 grid((unsigned)(plan.tiles * plan.splits), a.pages.nkv);
-  if (!f16) return launch_tiles<__nv_bfloat16, false, true>(p, grid, follows, st);
-  if (dtype == OOS_DTYPE_BF16) return launch_tiles<__nv_bfloat16, true, true>(p, grid, follows, st);
-  return launch_tiles<__half, true, true>(p, grid, follows, st);
+  if (!f16) return launch_tiles<__nv_bfloat16, false, true>(p, grid, st);
+  if (dtype == OOS_DTYPE_BF16) return launch_tiles<__nv_bfloat16, true, true>(p, grid, st);
+  return launch_tiles<__half, true, true>(p, grid, st);
 }
 
 }  // namespace oos

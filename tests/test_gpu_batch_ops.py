@@ -583,6 +583,69 @@ def test_three_steps_of_a_layer(dtype, kv):
         assert torch.equal(out[:step.n], first[:step.n])
 
 
+@pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("prefix", [0, 700])
+@pytest.mark.parametrize("counts", [[1] * 9, [40, 0, 7, 90]])
+def test_calls_that_follow_each_other(dtype, kv, prefix, counts):
+    """Layers whose queries are the layer's before, over the same pages, workspace and rows, with torch's kernels
+    and fills between them: the same bits whether each call is waited for, none is, or a graph with a second
+    stream in it runs them."""
+    nq, nkv, d, page, layers = 8, 2, 128, 16, 6
+    step = R.Step(counts, [c + 150 + 11 * i for i, c in enumerate(counts)], page, pad=1)
+    g = gen(5)
+    pk, pv = [randn(g, prefix + 1, nkv, d, dtype=kv) for _ in range(2)]
+    pages = [randn(g, step.n_pages, page, nkv, d, dtype=kv) for _ in range(2)]
+    start = randn(g, step.rows, nq + 2 * nkv, d, dtype=dtype)
+    gain, pos = 1 + randn(g, d, dtype=dtype, std=0.1), torch.arange(step.rows, dtype=torch.int32, device="cuda")
+    rope, batch, st = B.OosRopeConfig(1e6), step.device(B), status()
+    kp, vp, rows = torch.empty_like(pages[0]), torch.empty_like(pages[1]), torch.empty_like(start)
+    q, out = [torch.empty(step.rows, nq, d, dtype=dtype, device="cuda") for _ in range(2)]
+    outs = torch.empty(layers, step.rows, nq, d, dtype=dtype, device="cuda")
+    cache = B.PagedCache(kp, vp)
+    ws = torch.empty(B.oos_shared_prefix_attention_workspace_bytes(q, prefix, cache, batch), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+
+    def run(after):
+        kp.copy_(pages[0]), vp.copy_(pages[1]), rows.copy_(start)
+        for i in range(layers):
+            fork, join = torch.cuda.Event(), torch.cuda.Event()
+            out.zero_()
+            fork.record()
+            with torch.cuda.stream(side):
+                side.wait_event(fork)
+                rows[:, nq:].mul_(-1)
+                join.record()
+            after()
+            B.oos_qk_norm_rope(rows[:, :nq], None, gain, None, 1e-6, rope, pos, q, None)
+            after()
+            torch.cuda.current_stream().wait_event(join)
+            B.oos_paged_append(cache, batch, rows[:, nq:nq + nkv], rows[:, nq + nkv:], gain, 1e-6, rope, pos, st)
+            after()
+            B.oos_shared_prefix_attention(q, pk, pv, prefix, cache, batch, None, 1 / math.sqrt(d), out, ws, st)
+            after()
+            rows[:, :nq].copy_(out)
+            outs[i].copy_(out)
+            after()
+
+    run(torch.cuda.synchronize)
+    want = outs.clone()
+    assert int(st) == 0 and not torch.equal(want[0], want[1])
+    for _ in range(3):
+        outs.zero_()
+        run(lambda: None)
+        torch.cuda.synchronize()
+        assert torch.equal(outs, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(lambda: None)
+    for _ in range(3):
+        outs.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs, want)
+    assert int(st) == 0
+
+
 def test_two_calls_at_once():
     """Calls on two streams with workspaces of their own do not disturb each other."""
     step = R.Step([1] * 20, list(range(1, 400, 20)), 16)
