@@ -342,7 +342,12 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, kMaxKeys);
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc) {
-    p->few = rows <= 16ll * b.n_seqs;
+    // Tiles of 16 rows that read their sequence's pages again (from L2), or tiles of up to
+    // 256 that are mostly empty.  Trees of 4 rows a node, 8 kv heads, 2048 prefix keys: 24
+    // rows on average 72 us against 100 (64 sequences), 34 against 38 (16); 48 rows 41
+    // against 40 (16 sequences; over 8192 keys 93 against 103), 16 against 24 (2), but 111
+    // against 91 (64); 96 rows 32 against 26 (4).
+    p->few = rows <= 32ll * b.n_seqs || (rows <= 64ll * b.n_seqs && rows / 16 * c.n_kv_heads <= 4ll * sms);
     p->sequence = {false, 0, 1};
     if (p->few) p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, prefix_len, most_keys, sms);

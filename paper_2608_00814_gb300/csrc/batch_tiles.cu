@@ -756,7 +756,7 @@ PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, 
   return p;
 }
 
-// Sequences of more than 16 rows on average.  They take the prefix along where that is
+// Sequences of many rows.  They take the prefix along where that is
 // estimated shorter than a kernel for it and its parts (two tiles of own keys assumed: the
 // lengths are on the device).
 SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_len, long long most_keys, int n_sms) {
