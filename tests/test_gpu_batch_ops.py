@@ -307,6 +307,17 @@ def test_attention_long_prefix_few_rows(dtype, kv):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES[1:])
+@pytest.mark.parametrize("n_seqs, most", [(64, 9), (3, 16), (16, 16)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_attention_several_tiles_of_few_rows(dtype, kv, n_seqs, most, tree):
+    """Sequences of one to `most` tokens of five heads a group: a few 16-row tiles each, or one large one."""
+    rng = np.random.RandomState(n_seqs)
+    counts = [int(c) for c in rng.randint(1, most + 1, n_seqs)]
+    parent = [-1 if j == 0 else int(rng.randint(-1, j)) for c in counts for j in range(c)] if tree else None
+    run_case(counts, [c + int(rng.randint(0, 300)) for c in counts], 16, 1, 100, 10, 2, 128, dtype, kv, parent=parent)
+
+
+@pytest.mark.parametrize("dtype, kv", TYPES[1:])
 def test_attention_many_rows_long_prefix(dtype, kv):
     """Several row tiles and several splits of the prefix; scores far enough apart that maxima move."""
     run_case([90, 1, 200, 77], [90, 300, 210, 500], 16, 1, 1501, 8, 2, 128, dtype, kv, std=6.0)
@@ -343,9 +354,10 @@ def test_attention_repeats_bit_for_bit(dtype, kv, shape):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES)
-def test_attention_rows_any_stride(dtype, kv):
+@pytest.mark.parametrize("counts, lens", [([2, 5], [30, 12]), ([70, 130], [90, 150])])
+def test_attention_rows_any_stride(dtype, kv, counts, lens):
     """q a slice of a projection's rows, out a slice of wider rows that starts off 16-byte boundaries."""
-    step = R.Step([2, 5], [30, 12], 16)
+    step = R.Step(counts, lens, 16)
     q, pk, pv, kp, vp = inputs(step, 40, 8, 2, 128, dtype, kv)
     wide_q = torch.zeros(step.rows, 12, 128, dtype=dtype, device="cuda")
     wide_q[:, 1:9] = q
@@ -365,9 +377,10 @@ def test_attention_rows_any_stride(dtype, kv):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES)
-def test_attention_large_and_special_scores(dtype, kv):
+@pytest.mark.parametrize("last", [3, 150])
+def test_attention_large_and_special_scores(dtype, kv, last):
     """Rows whose scores are huge in either direction; a NaN key that is seen makes its rows NaN, and only those."""
-    step = R.Step([1, 1, 3], [40, 3, 20], 16)
+    step = R.Step([1, 1, last], [40, 3, 17 + last], 16)
     q, pk, pv, kp, vp = inputs(step, 130, 4, 2, 128, dtype, kv, std=60.0)
     out, _ = attend(step, q, pk, pv, 130, kp, vp)
     ref, mag, size = R.attention(step, q, pk[:130], pv[:130], kp, vp, 1 / math.sqrt(128))
@@ -376,7 +389,7 @@ def test_attention_large_and_special_scores(dtype, kv):
     kp[p, e, 1, 5] = math.nan
     out2, _ = attend(step, q, pk, pv, 130, kp, vp)
     nan = torch.isnan(out2).any(-1).cpu()
-    want = torch.zeros(5, 4, dtype=torch.bool)
+    want = torch.zeros(2 + last, 4, dtype=torch.bool)
     want[1, 2:] = True
     assert torch.equal(nan, want)
 
@@ -384,16 +397,18 @@ def test_attention_large_and_special_scores(dtype, kv):
 @pytest.mark.parametrize("dtype, kv", TYPES)
 @pytest.mark.parametrize("tree", [False, True])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
-def test_attention_masked_places_hold_anything(dtype, kv, tree, value):
+@pytest.mark.parametrize("counts, lens, nodes", [([3, 1, 90, 30], [3, 20, 200, 31], (2, 40, 7)),
+                                                 ([3, 1, 9, 5], [3, 20, 200, 31], (2, 4, 3))])
+def test_attention_masked_places_hold_anything(dtype, kv, tree, value, counts, lens, nodes):
     """A v or k that is not finite at one of the step's own positions reaches the rows that see it, and no other."""
-    counts, lens = [3, 1, 90, 30], [3, 20, 200, 31]
     step = R.Step(counts, lens, 16)
-    parent = [j - 1 for j in range(3)] + [-1] + [-1 if j == 0 else j // 2 for j in range(90)] + [-1] * 30 if tree else None
+    parent = ([j - 1 for j in range(3)] + [-1] + [-1 if j == 0 else j // 2 for j in range(counts[2])] + [-1] * counts[3]
+              if tree else None)
     par = torch.tensor(parent, dtype=torch.int32, device="cuda") if tree else None
     q, pk, pv, kp, vp = inputs(step, 50, 6, 2, 128, dtype, kv)
     base, _ = attend(step, q, pk, pv, 50, kp, vp, par)
     sees = torch.zeros(step.n, dtype=torch.bool)
-    for b, node in ((0, 2), (2, 40), (3, 7)):
+    for b, node in zip((0, 2, 3), nodes):
         lo, c, n = step.q_start[b], counts[b], lens[b]
         p, e = step.where(b, n - c + node)
         vp[p, e, 1, 3] = value
@@ -411,9 +426,10 @@ def test_attention_masked_places_hold_anything(dtype, kv, tree, value):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES[1:])
-def test_attention_queries_of_any_size(dtype, kv):
+@pytest.mark.parametrize("counts", [[1, 1, 40], [70, 1, 90]])
+def test_attention_queries_of_any_size(dtype, kv, counts):
     """Queries far above and below one: with binary16 pages they must neither overflow nor vanish."""
-    step = R.Step([1, 1, 40], [40, 3, 60], 16)
+    step = R.Step(counts, [39 + counts[0], 3, 20 + counts[2]], 16)
     top = 2.0 ** 15 if dtype is F16 else 2.0 ** 60
     for factor in (top, 2.0 ** -13 if dtype is F16 else 2.0 ** -60):
         q, pk, pv, kp, vp = inputs(step, 200, 4, 2, 128, dtype, kv, std=0.3)
@@ -421,7 +437,7 @@ def test_attention_queries_of_any_size(dtype, kv):
         scale = 1 / math.sqrt(128) / factor
         out, _ = attend(step, q, pk, pv, 200, kp, vp, scale=scale)
         ref, mag, size = R.attention(step, q, pk[:200], pv[:200], kp, vp, scale)
-        R.check_attention(out, ref, mag, size, 260, kv, factor)
+        R.check_attention(out, ref, mag, size, 200 + max(step.lens), kv, factor)
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES)
