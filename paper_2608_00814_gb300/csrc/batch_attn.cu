@@ -27,6 +27,11 @@ constexpr int kMaxParts = 32;      // parts of a row (a lane each in the join)
 // RT rows x 32 keys per step, 128 threads: thread (r, c) of 16 x 8 has RT / 16 rows and
 // keys c, c + 8, c + 16, c + 24 of S, and four columns in 32 of O.  The eight threads of
 // a row share its statistics by shuffles.
+//
+// Bound by latency: lookups, loads, products, statistics and products of a tile follow each
+// other at 4 blocks per SM (40 sequences of up to 3 rows, 6 heads of 128, 900 + up to 300
+// keys: 82 us, issue slots 39 % used, shared memory 40 %).  So a tile's places are looked up
+// under the tile before, and the keys dealt to as many blocks as help.
 template <typename TQ, typename TK, int RT, int VEC>
 __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a) {
   extern __shared__ __align__(16) float sm[];
@@ -38,7 +43,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   float* s_p = s_v + kRowKeys * ld;         // [RT][36]
   constexpr int ldp = kRowKeys + 4;
   __shared__ TreeScratch s_tree;
-  __shared__ long long s_at[kRowKeys];      // slot of each key in its buffer, -1: none
+  __shared__ long long s_at[2][kRowKeys];   // slot of each key in its buffer, -1: none; of two tiles in turn
 
   pdl_wait();
   pdl_trigger();
@@ -88,18 +93,20 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
       for (int e = 0; e < 4; ++e) o[r][c][e] = 0.f;
   }
   const long long heads_d = (long long)a.pages.nkv * d;
-  for (int key0 = k0; key0 < k1; key0 += kRowKeys) {
-    __syncthreads();   // the tile before is read
-    if (tid < kRowKeys) {
-      const int key = key0 + tid;
-      long long at = -1;
-      if (key < k1) {
-        at = prefix ? key : page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
-        if (at < 0) *a.status = OOS_EBATCH;
-      }
-      s_at[tid] = at;
+  auto look_up = [&](int key0) {   // the places of a tile's keys, while the tile before is worked on
+    if (tid >= kRowKeys) return;
+    const int key = key0 + tid;
+    long long at = -1;
+    if (key < k1) {
+      at = prefix ? key : page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
+      if (at < 0) *a.status = OOS_EBATCH;
     }
-    __syncthreads();
+    s_at[(key0 - k0) / kRowKeys & 1][tid] = at;
+  };
+  look_up(k0);
+  for (int key0 = k0; key0 < k1; key0 += kRowKeys) {
+    __syncthreads();   // the tile before is read, this one's places are known
+    const long long* at_of = s_at[(key0 - k0) / kRowKeys & 1];
     const TK* kb = (const TK*)(prefix ? a.pk : a.pages.k);
     const TK* vb = (const TK*)(prefix ? a.pv : a.pages.v);
     const int chunks = (ld - 4) / VEC;
@@ -108,8 +115,8 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
       float kv[VEC], vv[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) kv[e] = vv[e] = 0.f;   // keys that are not there must not reach a sum
-      if (s_at[key] >= 0 && c < d) {
-        const long long off = s_at[key] * heads_d + (long long)g * d + c;
+      if (at_of[key] >= 0 && c < d) {
+        const long long off = at_of[key] * heads_d + (long long)g * d + c;
         load_vec<TK, VEC>(kb + off, kv);
         load_vec<TK, VEC>(vb + off, vv);
       }
@@ -119,6 +126,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
         s_v[key * ld + c + e] = vv[e];
       }
     }
+    look_up(key0 + kRowKeys);
     __syncthreads();
     float s[RPT][4];
     bool see[RPT][4];
@@ -145,7 +153,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = key0 + tc + 8 * j, own = key - t.first;
-        bool ok = s_at[tc + 8 * j] >= 0;
+        bool ok = at_of[tc + 8 * j] >= 0;
         if (!prefix && own >= 0)
           ok = ok && (anc ? token < t.n && own < kMaxTreeRows && ((anc[token][own >> 6] >> (own & 63)) & 1) : own <= token);
         see[r][j] = ok;
@@ -174,7 +182,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
         for (int e = 0; e < 4; ++e) o[r][c][e] *= f;
     }
     __syncwarp();   // a row's weights are written and read by the same eight lanes
-#pragma unroll 2
+#pragma unroll 8
     for (int key = 0; key < kRowKeys; ++key) {
       float p[RPT];
 #pragma unroll
@@ -361,10 +369,11 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
   p->p_tiles = prefix_len > 0 ? (int)((rows + p->rt - 1) / p->rt) : 0;
   p->s_tiles = (int)(b.n_seqs + rows / p->rt);
-  // enough blocks for four per SM, each with two tiles of keys at least
+  // enough blocks for four per SM, each with a tile of keys at least (a tile is a chain of
+  // some 4 us: one request of 1 token over 130 keys 10.8 us, with two tiles a block 17.9)
   auto splits = [&](long long tiles, long long keys) {
     const long long want = tiles > 0 ? 4ll * sms / (tiles * c.n_kv_heads) : 1;
-    return (int)std::max(1ll, std::min({want, keys / (2 * kRowKeys), (long long)kMaxParts / 2}));
+    return (int)std::max(1ll, std::min({want, keys / kRowKeys, (long long)kMaxParts / 2}));
   };
   p->p_splits = prefix_len > 0 ? splits(p->p_tiles, prefix_len) : 0;
   p->s_splits = splits(p->s_tiles, most_keys);
