@@ -361,7 +361,18 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, prefix_len, most_keys, sms);
     p->prefix = prefix_len > 0 && !p->sequence.takes_prefix ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->few ? p->pages.sms : 0, sms)
                                                             : PrefixPlan{0, 0, 0.0};
-    const int parts = p->prefix.splits + (p->sequence.splits > 1 ? p->sequence.splits : 0);
+    // Blocks of few rows that join with the prefix's parts hold their place until those
+    // are there.  Where the prefix's last wave leaves SMs free for long -- as much as the
+    // chip does in 9 us -- they leave a part of their own and go on, for one more kernel.
+    // 256 sequences, 32768 prefix keys (20 us): 130 us against 142; 64 trees of 6 nodes, 2048
+    // keys: 66 against 72; 200 sequences of 64 heads, 16000 keys (9.6): 123 against 130; but
+    // 64 of 40 heads, 3000 keys (7.4): 56.5 against 55, 40 over 30000 keys (6.3): 53 against 48.
+    if (p->few && p->prefix.splits > 0) {
+      const long long blocks = (long long)p->prefix.pairs * c.n_kv_heads * p->prefix.splits, waves = (blocks + sms - 1) / sms;
+      const long long left = waves * sms - blocks;   // SMs, in the last wave
+      p->pages.part = p->pages.sms > left && p->prefix.us * (double)left / (double)(waves * sms) > 9.0;
+    }
+    const int parts = p->prefix.splits + (p->few ? (int)p->pages.part : p->sequence.splits > 1 ? p->sequence.splits : 0);
     p->ml_off = 0;
     p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
     return true;
@@ -475,11 +486,13 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
   if (p.tc) {
     a.p_splits = p.prefix.splits;
     a.s_splits = p.few ? p.pages.splits : p.sequence.splits;
+    a.own_part = p.few && p.pages.part;
     e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, cache->dtype, st) : cudaSuccess;
     if (e == cudaSuccess)
       e = p.few ? launch_pages_tc(a, p.pages, dtype, cache->dtype, st)
                 : launch_sequence_tc(a, p.sequence, dtype, cache->dtype, st);
-    if (e == cudaSuccess && !p.few && a.s_splits > 1) {
+    if (p.few) a.s_splits = p.pages.part;   // for the join
+    if (e == cudaSuccess && (p.few ? p.pages.part : a.s_splits > 1)) {
       const dim3 grid((unsigned)(((long long)batch->n_tokens * n_q_heads + 7) / 8));
       e = dtype == OOS_DTYPE_BF16 ? launch(true, k_attn_join_parts<__nv_bfloat16>, grid, dim3(256), 0, st, a)
                                   : launch(true, k_attn_join_parts<__half>, grid, dim3(256), 0, st, a);

@@ -30,6 +30,7 @@ struct BatchAttnArgs {
   float* part_o;
   float2* part_ml;
   int p_tiles, p_splits, s_tiles, s_splits;
+  bool own_part;   // few rows on tensor cores: own keys leave part p_splits for the join
   int32_t* status;
 };
 
@@ -171,6 +172,7 @@ struct PagesPlan {
   int tile_rows;   // of a block: 8 or 16
   int tiles, splits;
   int sms;         // that its blocks fill at once, about
+  bool part;       // leaves a part for a join
 };
 struct SequencePlan {
   bool takes_prefix;   // in the same kernel
@@ -180,8 +182,8 @@ SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_le
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
 // the prefix's parts of every row
 cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dtype, int kv_dtype, cudaStream_t st);
-// the sequences' own keys, joined with the prefix's p_splits parts into out; of
-// launch_sequence_tc with several splits, parts p_splits .. for launch_join_tc
+// the sequences' own keys, joined with the prefix's p_splits parts into out; with several
+// splits of launch_sequence_tc, or own_part, left as parts p_splits .. for k_attn_join_parts
 cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, int kv_dtype, cudaStream_t st);
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
 

@@ -412,7 +412,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
         for (int h = 0; h < 2; ++h) row[16 * i + 8 * h + (lane >> 2)] = o[i][n][2 * h + e];
       if (lane < 4) *reinterpret_cast<float2*>(row + kPgD) = make_float2(m[n][e], l[n][e]);
     }
-  pdl_wait();   // the prefix's parts
+  const int pre_parts = a.own_part ? 0 : a.p_splits;
+  if (!a.own_part) pdl_wait();   // the prefix's parts
   __syncthreads();
   if (S > 1) {
     cluster_arrive_release();
@@ -429,12 +430,12 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
     const float* mine = stage + (lane % kPgWarps * ROWS + r) * kPartLd + kPgD;
     float2 ml = make_float2(-INFINITY, 0.f);
     if (lane < own) ml = S > 1 ? ld_cluster2(dsmem_addr(mine, lane / kPgWarps)) : *reinterpret_cast<const float2*>(mine);
-    else if (lane < own + a.p_splits) ml = *reinterpret_cast<const float2*>(pre + (lane - own) * part_step + r * kPartLd + kPgD);
+    else if (lane < own + pre_parts) ml = *reinterpret_cast<const float2*>(pre + (lane - own) * part_step + r * kPartLd + kPgD);
     float4 v[U];
-    if (a.p_splits > 0) {
+    if (pre_parts > 0) {
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (i < a.p_splits) v[i] = *reinterpret_cast<const float4*>(pre + i * part_step + r * kPartLd + 4 * lane);
+        if (i < pre_parts) v[i] = *reinterpret_cast<const float4*>(pre + i * part_step + r * kPartLd + 4 * lane);
     }
     const bool on = ml.x != -INFINITY;   // a NaN is, and reaches the sum
     const float top = warp_max(ml.x);
@@ -460,17 +461,24 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
 #pragma unroll
       for (int i = 0; i < kPgWarps; ++i) add(s * kPgWarps + i, x[i]);
     }
-    if (a.p_splits > 0) {
+    if (pre_parts > 0) {
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (i < a.p_splits) add(own + i, v[i]);
+        if (i < pre_parts) add(own + i, v[i]);
     }
-    store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(acc, den));
+    if (a.own_part) {
+      float* to = a.part_o + a.p_splits * part_step + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0 + r) * kPartLd;
+      *reinterpret_cast<float4*>(to + 4 * lane) = acc;
+      if (lane == 0) *reinterpret_cast<float2*>(to + kPgD) = make_float2(top, den);
+    } else {
+      store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(acc, den));
+    }
   }
   if (S > 1) {   // a peer may still read this block's rows
     cluster_arrive_release();
     cluster_wait_acquire();
   }
+  if (a.own_part && blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();   // a kernel that waits for this one counts on the prefix's
 }
 
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms) {
@@ -484,6 +492,7 @@ PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys
   const long long live = std::max((long long)n_seqs, (rows + p.tile_rows - 1) / p.tile_rows) * nkv * p.splits;
   const int per_sm = pg_blocks(p.tile_rows / 8);
   p.sms = (int)std::min<long long>(n_sms, (live + per_sm - 1) / per_sm);
+  p.part = false;
   return p;
 }
 

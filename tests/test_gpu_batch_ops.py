@@ -318,6 +318,14 @@ def test_attention_several_tiles_of_few_rows(dtype, kv, n_seqs, most, tree):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES[1:])
+@pytest.mark.parametrize("most", [1, 2])
+def test_attention_pages_beside_a_long_prefix(dtype, kv, most):
+    """The prefix's kernel leaves SMs free for long, and the sequences' own keys leave parts for a join."""
+    counts = [1 + i % most for i in range(100)]
+    run_case(counts, [c + 4 * i % 400 for i, c in enumerate(counts)], 16, 2, 20000, 8, 1, 128, dtype, kv)
+
+
+@pytest.mark.parametrize("dtype, kv", TYPES[1:])
 def test_attention_many_rows_long_prefix(dtype, kv):
     """Several row tiles and several splits of the prefix; scores far enough apart that maxima move."""
     run_case([90, 1, 200, 77], [90, 300, 210, 500], 16, 1, 1501, 8, 2, 128, dtype, kv, std=6.0)
