@@ -24,18 +24,20 @@ constexpr int kRowKeys = 32;       // keys per tile
 constexpr int kRowThreads = 128;
 constexpr int kMaxParts = 32;      // parts of a row (a lane each in the join)
 
-// RT rows x 32 keys per step, 128 threads: thread (r, c) of 16 x 8 has RT / 16 rows and
-// keys c, c + 8, c + 16, c + 24 of S, and four columns in 32 of O.  The eight threads of
-// a row share its statistics by shuffles.
+// RT rows x 32 keys per step, 128 threads: thread (r, c) of 16 x 8 (of 4 x 32 with 4 rows)
+// has RT / 16 rows (one) and keys c, c + 8, c + 16, c + 24 (c) of S, and four columns in
+// 32 (in 128) of O.  The threads of a row share its statistics by shuffles.
 //
 // Bound by latency: lookups, loads, products, statistics and products of a tile follow each
-// other at 4 blocks per SM (40 sequences of up to 3 rows, 6 heads of 128, 900 + up to 300
-// keys: 82 us, issue slots 39 % used, shared memory 40 %).  So a tile's places are looked up
-// under the tile before, and the keys dealt to as many blocks as help.
+// other (40 sequences of up to 3 rows, 6 heads of 128, 900 + up to 300 keys, 16-row tiles:
+// 82 us, issue slots 39 % used, shared memory 40 %).  So a tile's places are looked up under
+// the tile before, the keys are dealt to as many blocks as help, and sequences of few rows
+// have tiles of 4 or 8, more of whose blocks fit on an SM (the same: 61 us).
 template <typename TQ, typename TK, int RT, int VEC>
-__global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a) {
+__global__ void __launch_bounds__(kRowThreads, RT == 64 ? 3 : RT == 16 ? 4 : 6) k_attn_rows(const BatchAttnArgs a) {
   extern __shared__ __align__(16) float sm[];
-  constexpr int RPT = RT / 16;
+  constexpr int GROUPS = RT < 16 ? RT : 16, RPT = RT / GROUPS, TPR = kRowThreads / GROUPS;   // TPR: threads of a row
+  constexpr int KPT = kRowKeys / TPR, CPT = kMaxHeadDim / (4 * TPR);                         // keys, column quads of a thread
   const int d = a.pages.d, ld = ((d + 3) & ~3) + 4, tid = threadIdx.x;
   float* s_q = sm;                          // [RT][ld]
   float* s_k = s_q + RT * ld;               // [32][ld]
@@ -45,7 +47,9 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
   __shared__ TreeScratch s_tree;
   __shared__ long long s_at[2][kRowKeys];   // slot of each key in its buffer, -1: none; of two tiles in turn
 
-  pdl_wait();
+  // behind the prefix's launch, which has waited for what the caller wrote before it
+  // triggers, only the end waits
+  if (!a.own_part) pdl_wait();
   pdl_trigger();
   const int g = blockIdx.y;
   const bool prefix = (int)blockIdx.x < a.p_tiles * a.p_splits;
@@ -61,6 +65,7 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     t.rows = min(RT, a.batch.n_tokens * a.group - t.r0);
     t.first = t.len = a.prefix_len;
   } else if (!sequence_tile(a, tile, RT, &t)) {
+    if (a.own_part && blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();   // the join counts on the prefix's launch, too
     return;
   }
   const unsigned long long (*anc)[2] = nullptr;
@@ -81,14 +86,14 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     }
     s_q[r * ld + c] = v;
   }
-  const int tr = tid >> 3, tc = tid & 7;
-  float o[RPT][4][4], m[RPT], l[RPT];
+  const int tr = tid / TPR, tc = tid % TPR;
+  float o[RPT][CPT][4], m[RPT], l[RPT];
 #pragma unroll
   for (int r = 0; r < RPT; ++r) {
     m[r] = -INFINITY;
     l[r] = 0.f;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < CPT; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[r][c][e] = 0.f;
   }
@@ -128,21 +133,21 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     }
     look_up(key0 + kRowKeys);
     __syncthreads();
-    float s[RPT][4];
-    bool see[RPT][4];
+    float s[RPT][KPT];
+    bool see[RPT][KPT];
 #pragma unroll
     for (int r = 0; r < RPT; ++r)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[r][j] = 0.f;
+      for (int j = 0; j < KPT; ++j) s[r][j] = 0.f;
     for (int c = 0; c < ld - 4; c += 4) {
-      float4 kk[4];
+      float4 kk[KPT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) kk[j] = *reinterpret_cast<const float4*>(s_k + (tc + 8 * j) * ld + c);
+      for (int j = 0; j < KPT; ++j) kk[j] = *reinterpret_cast<const float4*>(s_k + (tc + TPR * j) * ld + c);
 #pragma unroll
       for (int r = 0; r < RPT; ++r) {
         const float4 qq = *reinterpret_cast<const float4*>(s_q + (tr * RPT + r) * ld + c);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < KPT; ++j)
           s[r][j] += qq.x * kk[j].x + qq.y * kk[j].y + qq.z * kk[j].z + qq.w * kk[j].w;
       }
     }
@@ -151,9 +156,9 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
       const int token = (t.r0 + tr * RPT + r) / a.group;
       float mx = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = key0 + tc + 8 * j, own = key - t.first;
-        bool ok = at_of[tc + 8 * j] >= 0;
+      for (int j = 0; j < KPT; ++j) {
+        const int key = key0 + tc + TPR * j, own = key - t.first;
+        bool ok = at_of[tc + TPR * j] >= 0;
         if (!prefix && own >= 0)
           ok = ok && (anc ? token < t.n && own < kMaxTreeRows && ((anc[token][own >> 6] >> (own & 63)) & 1) : own <= token);
         see[r][j] = ok;
@@ -161,35 +166,35 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
         mx = max_nan(mx, s[r][j]);
       }
 #pragma unroll
-      for (int x = 1; x < 8; x *= 2) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+      for (int x = 1; x < TPR; x *= 2) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
       const float mn = max_nan(m[r], mx);
       const bool live = mn != -INFINITY;
       const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mn);
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < KPT; ++j) {
         const float p = live ? exp2f(s[r][j] - mn) : 0.f;
         sum += p;
-        s_p[(tr * RPT + r) * ldp + tc + 8 * j] = see[r][j] ? p : -1.f;   // negative: not seen
+        s_p[(tr * RPT + r) * ldp + tc + TPR * j] = see[r][j] ? p : -1.f;   // negative: not seen
       }
 #pragma unroll
-      for (int x = 1; x < 8; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      for (int x = 1; x < TPR; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
       l[r] = l[r] * f + sum;
       m[r] = mn;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < CPT; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[r][c][e] *= f;
     }
-    __syncwarp();   // a row's weights are written and read by the same eight lanes
+    __syncwarp();   // a row's weights are written and read by the same lanes
 #pragma unroll 8
     for (int key = 0; key < kRowKeys; ++key) {
       float p[RPT];
 #pragma unroll
       for (int r = 0; r < RPT; ++r) p[r] = s_p[(tr * RPT + r) * ldp + key];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int col = tc * 4 + 32 * c;
+      for (int c = 0; c < CPT; ++c) {
+        const int col = tc * 4 + 4 * TPR * c;
         if (col >= d) continue;
         const float4 v = *reinterpret_cast<const float4*>(s_v + key * ld + col);
 #pragma unroll
@@ -214,13 +219,14 @@ __global__ void __launch_bounds__(kRowThreads) k_attn_rows(const BatchAttnArgs a
     const long long at = part * n_rows + (long long)(t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
     if (tc == 0) a.part_ml[at] = make_float2(m[r], l[r]);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < CPT; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int col = tc * 4 + 32 * c + e;
+        const int col = tc * 4 + 4 * TPR * c + e;
         if (col < d) a.part_o[at * d + col] = o[r][c][e];
       }
   }
+  if (a.own_part && blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();
 }
 
 // A warp per row adds its parts up: weights 2^(m - max m), the sum divided by the
@@ -319,7 +325,7 @@ struct BatchAttnPlan {
   PrefixPlan prefix;
   PagesPlan pages;
   SequencePlan sequence;
-  int rt, p_tiles, p_splits, s_tiles, s_splits;   // CUDA cores
+  int p_rt, rt, p_tiles, p_splits, s_tiles, s_splits;   // CUDA cores: rows of a tile over the prefix, over own keys
   size_t ml_off, bytes;
 };
 
@@ -377,17 +383,24 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
     return true;
   }
-  p->rt = rows <= 16ll * b.n_seqs ? 16 : 64;
-  p->p_tiles = prefix_len > 0 ? (int)((rows + p->rt - 1) / p->rt) : 0;
+  // One request of 1 token, 9 heads, 2000 keys: 22.8 us with 4 rows, 22.6 with 16; 30 of up to
+  // 2 tokens, 9 heads: 42 and 63; 50 of 1 token, 8 heads on one: 46 with 8 rows, 47 with 16.
+  p->rt = rows <= 4ll * b.n_seqs ? 4 : rows <= 8ll * b.n_seqs ? 8 : rows <= 16ll * b.n_seqs ? 16 : 64;
+  p->p_rt = rows > p->rt ? std::max(p->rt, 16) : p->rt;   // the prefix's tiles hold rows of all sequences
+  p->p_tiles = prefix_len > 0 ? (int)((rows + p->p_rt - 1) / p->p_rt) : 0;
   p->s_tiles = (int)(b.n_seqs + rows / p->rt);
-  // enough blocks for four per SM, each with a tile of keys at least (a tile is a chain of
-  // some 4 us: one request of 1 token over 130 keys 10.8 us, with two tiles a block 17.9)
-  auto splits = [&](long long tiles, long long keys) {
-    const long long want = tiles > 0 ? 4ll * sms / (tiles * c.n_kv_heads) : 1;
+  // Enough blocks for four per SM, or twelve small ones (84 sequences of 3 rows over 580 keys
+  // on average: 64 us; with 8: 78, with 4 of 16 rows 152), each with a tile of keys at least
+  // (a tile is a chain of some 4 us: one request of 1 token over 130 keys 10.8 us, with two
+  // tiles a block 17.9).
+  auto splits = [&](long long tiles, int rt, long long keys) {
+    const long long want = (rt < 16 ? 12ll : 4ll) * sms / std::max(1ll, tiles * c.n_kv_heads);
     return (int)std::max(1ll, std::min({want, keys / kRowKeys, (long long)kMaxParts / 2}));
   };
-  p->p_splits = prefix_len > 0 ? splits(p->p_tiles, prefix_len) : 0;
-  p->s_splits = splits(p->s_tiles, most_keys);
+  p->p_splits = prefix_len > 0 ? splits(p->p_tiles, p->p_rt, prefix_len) : 0;
+  // tiles that have rows, about
+  const long long live = std::max((long long)b.n_seqs, (rows + p->rt - 1) / p->rt);
+  p->s_splits = splits(live, p->rt, most_keys);
   const size_t n = (size_t)(p->p_splits + p->s_splits) * b.n_tokens * nq;
   p->ml_off = (n * c.head_dim * 4 + 255) / 256 * 256;
   p->bytes = p->ml_off + (n * 8 + 255) / 256 * 256;
@@ -395,17 +408,23 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
 }
 
 template <typename TQ, typename TK, int RT, int VEC>
-static cudaError_t launch_rows(const BatchAttnArgs& a, int blocks, cudaStream_t st) {
+static cudaError_t launch_rows_of(const BatchAttnArgs& a, cudaStream_t st) {
   const int ld = ((a.pages.d + 3) & ~3) + 4;
   auto smem_of = [](int ld_) { return ((RT + 2 * kRowKeys) * ld_ + RT * (kRowKeys + 4)) * 4; };
   const size_t smem = smem_of(ld);
   static std::atomic<uint64_t> ready{0};
   cudaError_t e = kernel_ready(ready, (const void*)k_attn_rows<TQ, TK, RT, VEC>, smem_of(kMaxHeadDim + 4));
   if (e != cudaSuccess) return e;
-  e = launch(true, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
-  if (e != cudaSuccess) return e;
-  const long long rows = (long long)a.batch.n_tokens * a.nq;
-  return launch(true, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);
+  const int blocks = a.p_tiles * a.p_splits + a.s_tiles * a.s_splits;
+  return launch(true, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
+}
+
+template <typename TQ, typename TK>
+static cudaError_t launch_rows(const BatchAttnArgs& a, int rt, bool vec, cudaStream_t st) {
+  if (rt == 4) return vec ? launch_rows_of<TQ, TK, 4, 4>(a, st) : launch_rows_of<TQ, TK, 4, 1>(a, st);
+  if (rt == 8) return vec ? launch_rows_of<TQ, TK, 8, 4>(a, st) : launch_rows_of<TQ, TK, 8, 1>(a, st);
+  if (rt == 16) return vec ? launch_rows_of<TQ, TK, 16, 4>(a, st) : launch_rows_of<TQ, TK, 16, 1>(a, st);
+  return vec ? launch_rows_of<TQ, TK, 64, 4>(a, st) : launch_rows_of<TQ, TK, 64, 1>(a, st);
 }
 
 template <typename TQ, typename TK>
@@ -414,12 +433,21 @@ static cudaError_t launch_batch_rows(BatchAttnArgs& a, const BatchAttnPlan& p, c
   a.p_splits = p.p_splits;
   a.s_tiles = p.s_tiles;
   a.s_splits = p.s_splits;
-  const int blocks = a.p_tiles * a.p_splits + a.s_tiles * a.s_splits;
   // rows of whole aligned 4-element groups, else one element at a time
   const uintptr_t any = (uintptr_t)a.pages.k | (uintptr_t)a.pages.v | (uintptr_t)a.pk | (uintptr_t)a.pv;
   const bool vec = a.pages.d % 4 == 0 && any % (4 * sizeof(TK)) == 0;
-  if (p.rt == 16) return vec ? launch_rows<TQ, TK, 16, 4>(a, blocks, st) : launch_rows<TQ, TK, 16, 1>(a, blocks, st);
-  return vec ? launch_rows<TQ, TK, 64, 4>(a, blocks, st) : launch_rows<TQ, TK, 64, 1>(a, blocks, st);
+  cudaError_t e = cudaSuccess;
+  if (p.p_tiles > 0 && p.p_rt != p.rt) {   // the prefix's blocks in a launch of their own
+    a.s_tiles = 0;
+    e = launch_rows<TQ, TK>(a, p.p_rt, vec, st);
+    a.s_tiles = p.s_tiles;
+    a.p_tiles = 0;
+    a.own_part = true;
+  }
+  if (e == cudaSuccess) e = launch_rows<TQ, TK>(a, p.rt, vec, st);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)a.batch.n_tokens * a.nq;
+  return launch(true, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);
 }
 
 static bool attn_shape_ok(int nq, int prefix_len, const oos_paged_cache* c, const oos_batch* b) {

@@ -30,7 +30,7 @@ struct BatchAttnArgs {
   float* part_o;
   float2* part_ml;
   int p_tiles, p_splits, s_tiles, s_splits;
-  bool own_part;   // few rows on tensor cores: own keys leave part p_splits for the join
+  bool own_part;   // own keys in a launch behind the prefix's leave their parts for the join
   int32_t* status;
 };
 

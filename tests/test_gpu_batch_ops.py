@@ -406,11 +406,12 @@ def test_attention_large_and_special_scores(dtype, kv, last):
 @pytest.mark.parametrize("tree", [False, True])
 @pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("counts, lens, nodes", [([3, 1, 90, 30], [3, 20, 200, 31], (2, 40, 7)),
-                                                 ([3, 1, 9, 5], [3, 20, 200, 31], (2, 4, 3))])
+                                                 ([3, 1, 9, 5], [3, 20, 200, 31], (2, 4, 3)),
+                                                 ([2, 1, 3, 1], [9, 20, 200, 31], (1, 1, 0))])
 def test_attention_masked_places_hold_anything(dtype, kv, tree, value, counts, lens, nodes):
     """A v or k that is not finite at one of the step's own positions reaches the rows that see it, and no other."""
     step = R.Step(counts, lens, 16)
-    parent = ([j - 1 for j in range(3)] + [-1] + [-1 if j == 0 else j // 2 for j in range(counts[2])] + [-1] * counts[3]
+    parent = ([j - 1 for j in range(counts[0])] + [-1] + [-1 if j == 0 else j // 2 for j in range(counts[2])] + [-1] * counts[3]
               if tree else None)
     par = torch.tensor(parent, dtype=torch.int32, device="cuda") if tree else None
     q, pk, pv, kp, vp = inputs(step, 50, 6, 2, 128, dtype, kv)
