@@ -21,8 +21,8 @@
 // own, 40.
 //
 // Every row keeps its maximum, moved only when a chunk exceeds it by 2^8, and its sum in
-// fp32.  Weights enter P.V as binary16, or as two bf16 halves, whose second product costs
-// nothing beside the reads.
+// fp32.  Weights enter P.V as binary16 (2^-11), or as two bf16 halves (2^-16 together, where
+// one bf16 would round to 2^-9), whose second product costs nothing beside the reads.
 #include <math.h>
 
 #include <algorithm>
@@ -356,8 +356,12 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
           const __half2 v = __floats2half2_rn(p0, p1);
           pf[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&v));
         } else {
-          const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
-          const __nv_bfloat162 r = __floats2bfloat162_rn(p0 - __low2float(v), p1 - __high2float(v));
+          // the upper half cut off, and a lower one that is positive where the weight is: an
+          // infinite v stays infinite under both (of a NaN weight the lower one is NaN)
+          const float h0 = __uint_as_float(__float_as_uint(p0) & 0xffff0000u);
+          const float h1 = __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
+          const __nv_bfloat162 v = __floats2bfloat162_rn(h0, h1);
+          const __nv_bfloat162 r = __floats2bfloat162_rn(fmaxf(p0 - h0, p0 * 0x1p-60f), fmaxf(p1 - h1, p1 * 0x1p-60f));
           pf[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&v));
           pl[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&r));
         }

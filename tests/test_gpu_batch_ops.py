@@ -434,6 +434,25 @@ def test_attention_masked_places_hold_anything(dtype, kv, tree, value, counts, l
     assert float((got - want)[same].abs().max()) <= 0.05 * float(want[same].abs().max())
 
 
+@pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("counts", [[1, 1, 1], [1, 90, 60]])
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+def test_attention_infinite_values_stay_infinite(dtype, kv, counts, value):
+    """An infinite v long before the step, where no row's weight vanishes: infinite in all rows, not NaN."""
+    step = R.Step(counts, [40, 130, 90], 16)
+    q, pk, pv, kp, vp = inputs(step, 50, 6, 2, 128, dtype, kv, std=0.2)
+    p, e = step.where(0, 3)
+    vp[p, e, 1, 3] = value
+    pv[7, 0, 5] = value
+    out, st = attend(step, q, pk, pv, 50, kp, vp)
+    assert int(st) == 0
+    want = torch.isfinite(out)
+    assert bool((out[:counts[0], 3:, 3] == value).all()) and bool((out[:step.n, :3, 5] == value).all())
+    want[:counts[0], 3:, 3] = True
+    want[:step.n, :3, 5] = True
+    assert bool(want[:step.n].all())
+
+
 @pytest.mark.parametrize("dtype, kv", TYPES[1:])
 @pytest.mark.parametrize("counts", [[1, 1, 40], [70, 1, 90]])
 def test_attention_queries_of_any_size(dtype, kv, counts):
