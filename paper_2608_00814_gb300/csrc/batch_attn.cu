@@ -386,7 +386,10 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   // One request of 1 token, 9 heads, 2000 keys: 22.8 us with 4 rows, 22.6 with 16; 30 of up to
   // 2 tokens, 9 heads: 42 and 63; 50 of 1 token, 8 heads on one: 46 with 8 rows, 47 with 16.
   p->rt = rows <= 4ll * b.n_seqs ? 4 : rows <= 8ll * b.n_seqs ? 8 : rows <= 16ll * b.n_seqs ? 16 : 64;
-  p->p_rt = rows > p->rt ? std::max(p->rt, 16) : p->rt;   // the prefix's tiles hold rows of all sequences
+  // The prefix's tiles hold rows of all sequences: 16 where there are many, in a launch of
+  // their own, which few rows do not pay for (10 rows over a few keys 11 us a call against
+  // 13.8; 8 rows over 1500: 21 against 28).
+  p->p_rt = rows > 8ll * p->rt ? std::max(p->rt, 16) : p->rt;
   p->p_tiles = prefix_len > 0 ? (int)((rows + p->p_rt - 1) / p->p_rt) : 0;
   p->s_tiles = (int)(b.n_seqs + rows / p->rt);
   // Enough blocks for four per SM, or twelve small ones (84 sequences of 3 rows over 580 keys
