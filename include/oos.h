@@ -380,7 +380,8 @@ int oos_set_wait_limit(oos_model* m, uint64_t limit_ns, void* stream);
  * each request adds lives in pages of its own.  One step of a layer is: project
  * q, k, v (the caller's product), oos_qk_norm_rope on q, oos_paged_append of k
  * and v, oos_shared_prefix_attention.  All three are stream-ordered, allocate
- * nothing, keep nothing between calls and may be captured into a CUDA graph;
+ * nothing, keep nothing between calls but the rotation rates of a thread's last
+ * configuration, compared by value, and may be captured into a CUDA graph;
  * calls may overlap on the GPU as long as no call writes what another uses.
  *
  * Element types are OOS_DTYPE_F32, _BF16 and _F16; head_dim is even, 2..128

@@ -295,6 +295,15 @@ def test_attention_head_sizes(dtype, kv, d):
 
 
 @pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("d", [66, 96])
+@pytest.mark.parametrize("most", [1, 2])
+def test_attention_many_sequences_of_few_rows(dtype, kv, d, most):
+    """Small tiles over the own keys, larger ones over the prefix."""
+    counts = [1 + i % most for i in range(40)]
+    run_case(counts, [c + 13 * i % 120 for i, c in enumerate(counts)], 16, 2, 150, 9, 3, d, dtype, kv, seed=d)
+
+
+@pytest.mark.parametrize("dtype, kv", TYPES)
 def test_attention_many_sequences(dtype, kv):
     """More sequences than one round of the search takes, one wide group of heads."""
     counts = [(i * 7) % 3 for i in range(1100)]
