@@ -473,7 +473,9 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
     if (a.own_part) {
       float* to = a.part_o + a.p_splits * part_step + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0 + r) * kPartLd;
       *reinterpret_cast<float4*>(to + 4 * lane) = acc;
-      if (lane == 0) *reinterpret_cast<float2*>(to + kPgD) = make_float2(top, den);
+      // the maximum over the parts passes a NaN by, the sum does not: stored with a maximum of
+      // -inf it would read as a part without keys
+      if (lane == 0) *reinterpret_cast<float2*>(to + kPgD) = make_float2(den == den ? top : den, den);
     } else {
       store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(acc, den));
     }
