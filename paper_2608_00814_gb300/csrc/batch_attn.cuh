@@ -9,6 +9,10 @@ namespace oos {
 constexpr int kMaxTreeRows = 128;  // rows of a sequence with a tree
 constexpr int kMaxPrefixParts = 16;   // of a row, of the tensor-core kernels
 constexpr int kPartLd = 128 + 4;   // a row of a part: O, m, l, padded to 16 bytes
+// Binary16 weights are 2^(score - maximum + 7): below 2^15 before a maximum moves (which takes
+// scores 2^8 above it), and normal numbers, rounded to 2^-11, down to 2^-21 of the largest;
+// below that to 2^-32 of the largest.
+constexpr float kHalfBias = 7.f;
 constexpr int kMaxKeys = 0x7ffff000;   // of a prefix or a sequence: tiles of keys past the last still count in 32 bits
 
 struct BatchAttnArgs {

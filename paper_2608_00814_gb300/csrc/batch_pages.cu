@@ -21,8 +21,9 @@
 // own, 40.
 //
 // Every row keeps its maximum, moved only when a chunk exceeds it by 2^8, and its sum in
-// fp32.  Weights enter P.V as binary16 (2^-11), or as two bf16 halves (2^-16 together, where
-// one bf16 would round to 2^-9), whose second product costs nothing beside the reads.
+// fp32.  Weights enter P.V as binary16 (2^-11, small ones see kHalfBias), or as two bf16 halves
+// (2^-16 together, where one bf16 would round to 2^-8), whose second product costs nothing
+// beside the reads.
 #include <math.h>
 
 #include <algorithm>
@@ -104,6 +105,7 @@ template <typename TQ, bool F16, int NT>
 __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(const __grid_constant__ BatchAttnArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int ROWS = 8 * NT, STAGES = narrow_stages(NT);
+  constexpr float kBias = F16 ? kHalfBias : 0.f;
   constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
   __shared__ TreeScratch s_tree;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -320,7 +322,7 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
         float mx = max_nan(s[n][e], s[n][2 + e]);
         mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
         mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 16)) * sc[n][e];
+        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 16)) * sc[n][e] - kBias;
         mn[n][e] = !(mx <= m[n][e] + 8.f) ? mx : m[n][e];   // a NaN moves it, and stays
         move = move || mn[n][e] != m[n][e];
       }

@@ -135,8 +135,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr bool CONVERT = F16 && std::is_same<TQ, __nv_bfloat16>::value;
-  // binary16 weights carry 2^4, so that fewer of the small ones fall below its range
-  constexpr float kBias = F16 ? 4.f : 0.f;
+  constexpr float kBias = F16 ? kHalfBias : 0.f;
   uint64_t* bar = reinterpret_cast<uint64_t*>(sm + kTlOffBar);
   uint64_t* kfull = bar;           // [3] transaction bytes
   uint64_t* kempty = bar + 3;      // [3] its score products done

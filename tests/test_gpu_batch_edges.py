@@ -7,7 +7,8 @@ import pytest
 import torch
 
 import batch_ref as R
-from test_gpu_batch_ops import TYPES, attend, inputs
+from paper_2608_00814_gb300 import binding as B
+from test_gpu_batch_ops import BF16, F16, F32, TYPES, attend, inputs, status
 
 pytestmark = pytest.mark.gpu
 
@@ -16,6 +17,52 @@ pytestmark = pytest.mark.gpu
 def _built():
     from paper_2608_00814_gb300 import _build
     _build.build()
+
+
+# ------------------------------------------------------------------ weights
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("far", [18.5, 20.5, 22.5])
+@pytest.mark.parametrize("where", ["prefix", "own, few rows", "own, many rows"])
+def test_attention_small_weights_of_binary16(dtype, far, where):
+    """One key in 16 has all the weight but a v of zero; what comes out is the others', each 2^-far of it.  A weight
+    is a binary16 number below the row's largest, which stands at 2^7 or above: half a step is 2^-11 of a weight, or
+    2^-25 / 2^7 = 2^-32 of the largest where it is subnormal.  A score of `far` from two fp32 roundings is off by
+    far 2^-23, the rest as in check_attention."""
+    n = 2048
+    i32 = dict(dtype=torch.int32, device="cuda")
+    heavy = torch.arange(n, device="cuda") % 16 == 0
+    k, v = torch.zeros(n, 2, 128, dtype=F16, device="cuda"), torch.full((n, 2, 128), 2.0 ** 14, dtype=F16, device="cuda")
+    k[heavy, :, 0], v[heavy] = 16.0, 0.0
+    seqs, rows = (5, 1) if where != "own, many rows" else (2, 100)
+    q = torch.zeros(seqs * rows, 8, 128, dtype=dtype, device="cuda")
+    q[:, :, 0] = 1
+    scale = far * math.log(2) / 16
+    q_start = torch.arange(seqs + 1, **i32) * rows
+    pk = pv = None
+    if where == "prefix":
+        pk, pv, prefix = k, v, n
+        # one own key of weight zero: -2^13 scale
+        kp = torch.zeros(1, 16, 2, 128, dtype=F16, device="cuda")
+        kp[..., 0] = -(2.0 ** 13)
+        vp, lens = torch.zeros_like(kp), 1
+    else:       # every sequence reads the same page; rows of the step see it whole but for their successors
+        prefix = 0
+        kp, vp, lens = k[None], v[None], n
+    batch = B.Batch(q_start, torch.full((seqs,), lens, **i32), torch.zeros(seqs, 1, **i32), seqs * rows)
+    cache, st, out = B.PagedCache(kp.contiguous(), vp.contiguous()), status(), torch.empty_like(q)
+    ws = torch.empty(B.oos_shared_prefix_attention_workspace_bytes(q, prefix, cache, batch), dtype=torch.uint8, device="cuda")
+    B.oos_shared_prefix_attention(q, pk, pv, prefix, cache, batch, None, scale, out, ws, st)
+    assert int(st) == 0
+    w = 2.0 ** -far
+    seen = torch.full((seqs * rows,), n)
+    if where != "prefix":
+        seen = (n - rows + 1 + torch.arange(rows)).repeat(seqs)
+    big = (seen + 15) // 16
+    want = ((seen - big) * w * 2.0 ** 14 / (big + (seen - big) * w))[:, None, None].double()
+    rel = R.U[dtype] + max(R.U[F16], 2.0 ** -32 / w) + far * 2.0 ** -23 + (4 * n + 64) * R.F32
+    got = out.double().cpu()
+    assert bool(((got - want).abs() <= rel * want).all()), float(((got - want).abs() / want).max() / rel)
 
 
 # ------------------------------------------------------------------ scores that are not finite
