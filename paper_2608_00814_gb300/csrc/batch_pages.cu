@@ -352,11 +352,11 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
         const float p0 = ex2_approx(fmaf(s[n][2 * h], sc[n][0], neg[0])), p1 = ex2_approx(fmaf(s[n][2 * h + 1], sc[n][1], neg[1]));
         s[n][2 * h] = p0;
         s[n][2 * h + 1] = p1;
-        l[n][0] += p0;
-        l[n][1] += p1;
-        if constexpr (F16) {
+        if constexpr (F16) {   // the sum is of the weights as they are multiplied
           const __half2 v = __floats2half2_rn(p0, p1);
           pf[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&v));
+          s[n][2 * h] = __low2float(v);
+          s[n][2 * h + 1] = __high2float(v);
         } else {
           // the upper half cut off, and a lower one that is positive where the weight is: an
           // infinite v stays infinite under both (of a NaN weight the lower one is NaN)
@@ -367,6 +367,8 @@ __global__ void __launch_bounds__(kPgWarps * 32, pg_blocks(NT)) k_attn_pages(con
           pf[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&v));
           pl[n][h] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&r));
         }
+        l[n][0] += s[n][2 * h];
+        l[n][1] += s[n][2 * h + 1];
       }
     }
     if (apart) {

@@ -23,8 +23,14 @@
 // P.V of the one before: 197.)
 //
 // P, 16-bit pairs in TMEM, is the A operand of P.V and is handed over in halves of 64
-// keys; the sum l is of the unrounded weights.  The running maximum moves only when a
-// tile exceeds it by 2^8 (the threads rescale their O rows in TMEM then).
+// keys.  A weight is rounded to the type of V, as the product's operands have one type: by
+// up to 2^-8 for bf16, as much as out itself is rounded by.  (A second bf16 half would need
+// another 128 columns of TMEM, all of which are taken, and half as much product again.)
+// The sum l is of the rounded weights, so that what a row's keys share comes out as it is: a
+// twentieth of the time (1024 rows of 8 heads over 32768 keys 126 us; 117 with the sum of the
+// weights before they are rounded, which is off by up to 2^-8 from those multiplied).
+// The running maximum moves only when a tile exceeds it by 2^8 (the threads rescale their O
+// rows in TMEM then).
 // Keys past the prefix's end arrive as zeros (the tensor map ends there), and so do those
 // without a page, so masking their scores is enough.  Pages are gathered by 16-byte
 // asynchronous copies into the layout TMA writes, whatever their size; the copying warp
@@ -122,6 +128,12 @@ OOS_DEV float2 add2(float2 a, float2 b) {
   float2 v;
   asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
   return v;
+}
+// s plus the two bf16 of w, in fp32
+OOS_DEV void add_bf16x2(float2& s, uint32_t w) {
+  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tadd.rn.f32.bf16 %0, x, %0;\n\tadd.rn.f32.bf16 %1, y, %1;\n\t}"
+      : "+f"(s.x), "+f"(s.y)
+      : "r"(w));
 }
 OOS_DEV float max3_nan(float a, float b, float c) {
   float r;
@@ -523,13 +535,14 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
           for (int i = 0; i < 32; i += 2) {
             float2 e = fma2(make_float2(sv[32 * c + i], sv[32 * c + i + 1]), sc2, neg2);
             e = make_float2(ex2_approx(e.x), ex2_approx(e.y));
-            ps[(i >> 1) & 1] = add2(ps[(i >> 1) & 1], e);
             if constexpr (F16) {
               const __half2 v = __floats2half2_rn(e.x, e.y);
               pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+              ps[(i >> 1) & 1] = add2(ps[(i >> 1) & 1], __half22float2(v));
             } else {
               const __nv_bfloat162 v = __floats2bfloat162_rn(e.x, e.y);
               pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
+              add_bf16x2(ps[(i >> 1) & 1], pk[i / 2]);
             }
           }
           tmem_st16u(tp + 16 * c, pk);

@@ -8,7 +8,7 @@ import torch
 
 import batch_ref as R
 from paper_2608_00814_gb300 import binding as B
-from test_gpu_batch_ops import BF16, F16, F32, TYPES, attend, inputs, status
+from test_gpu_batch_ops import BF16, F16, F32, TYPES, attend, gen, inputs, status
 
 pytestmark = pytest.mark.gpu
 
@@ -20,6 +20,48 @@ def _built():
 
 
 # ------------------------------------------------------------------ weights
+
+@pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("prefix", [0, 2048])
+@pytest.mark.parametrize("counts", [[1] * 40, [90, 200, 64, 140, 90, 200, 64, 140]])
+def test_attention_returns_a_constant_v(dtype, kv, prefix, counts):
+    """Where every key has the same v, out is that v: a row's weights, as they are multiplied, add up to the sum
+    that it is divided by.  v is a power of two, below which half a step is smallest: 2^-9 of the value for bf16 and
+    2^-12 for binary16.  Both sums are of the same positive numbers, at most `keys` of them and 64 in the joins, each
+    rounded or truncated to 2^-23 of it, but few of them count: one key in 128 (16 of own keys with few rows) has a
+    score 2^1 to 2^4 times, by row, the one before's and the others have none.  At most 64 count, so the sums are off
+    by 2^-23 (64 + 64) < 2^-12, and nothing but the value itself may come out (bf16 weights of two halves are off by
+    2^-16 at most besides)."""
+    apart = 16 if counts[0] == 1 else 128
+    step = R.Step(counts, [c + apart * (2 + i % 7) + 5 * i for i, c in enumerate(counts)], 16)
+    q, pk, pv, kp, vp = inputs(step, prefix, 8, 2, 128, dtype, kv)
+    q.zero_()
+    q[..., 0] = 1 + 3 * torch.rand(step.rows, 8, generator=gen(1), device="cuda")      # powers of two per step
+    q[..., 1] = 2.0 ** 12
+
+    def ramp(n, apart):
+        k = torch.zeros(n, 2, 128, device="cuda")
+        i = torch.arange(n, device="cuda")
+        k[..., 0] = (i // apart)[:, None]
+        k[..., 1] = -1.0 * (i % apart != apart - 1)[:, None]
+        return k.to(kv)
+
+    pk[:prefix] = ramp(prefix, 128)
+    for b, n in enumerate(step.lens):
+        own = ramp(n, apart)
+        if prefix:
+            own[..., 1] = -1
+        for s in range(n):
+            kp[step.where(b, s)] = own[s]
+    v = torch.tensor([1.0, -1.0, 2.0, 0.5], device="cuda", dtype=kv).repeat(32)
+    pv[:prefix], vp[:] = v, v
+    out, st = attend(step, q, pk, pv, prefix, kp, vp, scale=math.log(2))
+    assert int(st) == 0
+    if dtype is F32:      # rounded sums divided, without a type's rounding after it
+        assert float((out / v - 1).abs().max()) <= 128 * 2.0 ** -23
+    else:
+        assert torch.equal(out, v.to(dtype).expand_as(out))
+
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("far", [18.5, 20.5, 22.5])
