@@ -129,3 +129,29 @@ def test_attention_nan_key_beside_a_long_prefix(dtype, kv, own):
     assert int(st) == 0
     nan = torch.isnan(out).cpu()
     assert torch.equal(nan.all(-1).all(-1), want) and torch.equal(nan.any(-1).any(-1), want)
+
+
+# ------------------------------------------------------------------ what a status says
+
+@pytest.mark.parametrize("dtype, kv", TYPES)
+def test_attention_bad_offsets_with_trees(dtype, kv):
+    """Offsets out of range are a bad batch with a tree, too; more than 128 rows of a sequence with a tree are a
+    bad tree."""
+    good = R.Step([1, 2, 1], [40, 2, 30], 16)
+    q, _, _, kp, vp = inputs(good, 0, 4, 2, 128, dtype, kv)
+    parent = torch.tensor([-1, -1, 0, -1], dtype=torch.int32, device="cuda")
+    base, st = attend(good, q, None, None, 0, kp, vp, parent=parent)
+    assert int(st) == 0
+    for starts in ([0, 1, 9, 4], [0, 1, 3, 5], [0, 1, 0, 4], [0, 1, -3, 4]):
+        step = R.Step([1, 2, 1], [40, 2, 30], 16)
+        step.q_start = starts
+        for parents in (None, parent):
+            out, st = attend(step, q, None, None, 0, kp, vp, parent=parents)
+            assert int(st) == B.OOS_EBATCH, (starts, parents is None)
+        if starts[2] != 0:      # there sequence 2, from row 0 on, claims sequence 0's row as well
+            assert torch.equal(out[0], base[0])
+    big = R.Step([129], [140], 16)
+    q, _, _, kp, vp = inputs(big, 0, 4, 2, 128, dtype, kv)
+    chain = torch.arange(-1, 128, dtype=torch.int32, device="cuda")
+    _, st = attend(big, q, None, None, 0, kp, vp, parent=chain)
+    assert int(st) == B.OOS_ETREE
