@@ -62,11 +62,11 @@ OOS_DEV bool sequence_tile(const BatchAttnArgs& a, int i, int tile_rows, TileRow
   const BatchView& b = a.batch;
   auto start = [&](int s) { return s + (long long)b.q_start[s] * a.group / tile_rows; };
   const int seq = warp_count_le(b.n_seqs - 1, start, i);
-  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = max(0, b.seq_len[seq]);
+  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], given = b.seq_len[seq], len = max(0, given);
   const long long most = min((long long)b.max_pages * a.pages.page_size, (long long)kMaxKeys);
   const bool in_order = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1;
   const bool ok = in_order && (!a.parent || q1 - q0 <= kMaxTreeRows);
-  if (!ok || len < q1 - q0 || len > most) {
+  if (!ok || given < q1 - q0 || len > most) {
     if (threadIdx.x == 0) *a.status = in_order && !ok ? OOS_ETREE : OOS_EBATCH;
   }
   if (!ok || i < start(seq)) return false;

@@ -155,3 +155,17 @@ def test_attention_bad_offsets_with_trees(dtype, kv):
     chain = torch.arange(-1, 128, dtype=torch.int32, device="cuda")
     _, st = attend(big, q, None, None, 0, kp, vp, parent=chain)
     assert int(st) == B.OOS_ETREE
+
+
+@pytest.mark.parametrize("dtype, kv", TYPES)
+@pytest.mark.parametrize("counts", [[1, 0, 2], [70, 0, 90]])
+def test_attention_bad_length_of_a_waiting_sequence(dtype, kv, counts):
+    """A sequence without rows in the step: its length is checked all the same, the others keep their results."""
+    step = R.Step(counts, [counts[0] + 9, 5, counts[2]], 16)
+    q, _, _, kp, vp = inputs(step, 0, 4, 2, 128, dtype, kv)
+    base, st = attend(step, q, None, None, 0, kp, vp)
+    assert int(st) == 0
+    for n in (-1, -2 ** 31, 2 ** 31 - 1):
+        step.lens[1] = n
+        out, st = attend(step, q, None, None, 0, kp, vp)
+        assert int(st) == B.OOS_EBATCH and torch.equal(out, base), n
