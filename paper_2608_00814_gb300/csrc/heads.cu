@@ -24,7 +24,7 @@
 namespace oos {
 
 constexpr int kHeadWarps = 4;      // tokens per block, a warp each
-constexpr int kMaxSlices = 1024;   // warps a token's heads are dealt to (times 2^20 heads below 2^31)
+constexpr int kMaxSlices = 1024;   // warps a token's heads are dealt to
 
 struct HeadArgs {
   int n, d, d2;                   // tokens, head size and half of it
@@ -281,7 +281,8 @@ static cudaError_t launch_heads_of(HeadArgs& a, const RopeTurns& rope, cudaStrea
   // few tokens are spread out while many share the angles over all their heads (2048
   // tokens of 40 heads: 10.6 us, 11.4 with 32 warps, 13.9 with 48).
   const int total = a.heads[0] + a.heads[1], most = (total * LANES + 31) / 32;
-  const int slices = (int)std::max(1ll, std::min<long long>(std::min(most, kMaxSlices), 16ll * sms / a.n));
+  const int fit = 0x7fffffff / total;   // the kernel deals the heads by total * slices in 32 bits
+  const int slices = (int)std::max(1ll, std::min<long long>(std::min({most, kMaxSlices, fit}), 16ll * sms / a.n));
   const dim3 grid((unsigned)((a.n + (long long)kHeadWarps - 1) / kHeadWarps), slices);
   return launch(true, k_heads<T, O, VEC, LANES, NC, APPEND>, grid, dim3(kHeadWarps * 32), 0, st, a, rope);
 }

@@ -8,7 +8,7 @@ import torch
 
 import batch_ref as R
 from paper_2608_00814_gb300 import binding as B
-from test_gpu_batch_ops import BF16, F16, F32, TYPES, attend, gen, inputs, status
+from test_gpu_batch_ops import BF16, F16, F32, TYPES, attend, gen, inputs, randn, status
 
 pytestmark = pytest.mark.gpu
 
@@ -169,3 +169,20 @@ def test_attention_bad_length_of_a_waiting_sequence(dtype, kv, counts):
         step.lens[1] = n
         out, st = attend(step, q, None, None, 0, kp, vp)
         assert int(st) == B.OOS_EBATCH and torch.equal(out, base), n
+
+
+# ------------------------------------------------------------------ append
+
+@pytest.mark.parametrize("heads", [1 << 20, 1 << 22, 1 << 23])
+def test_append_of_many_heads(heads):
+    """As many heads of two elements as a call may have: all are appended."""
+    k, v = randn(gen(1), 1, heads, 2, dtype=BF16), randn(gen(2), 1, heads, 2, dtype=BF16)
+    kp = torch.full((2, 1, heads, 2), 7.0, dtype=BF16, device="cuda")
+    vp = torch.full_like(kp, 7.0)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    batch = B.Batch(torch.tensor([0, 1], **i32), torch.tensor([1], **i32), torch.tensor([[1]], **i32), 1)
+    st = status()
+    B.oos_paged_append(B.PagedCache(kp, vp), batch, k, v, None, 1e-6, None, None, st)
+    assert int(st) == 0
+    assert torch.equal(kp[1], k) and torch.equal(vp[1], v)
+    assert bool((kp[0] == 7.0).all()) and bool((vp[0] == 7.0).all())
