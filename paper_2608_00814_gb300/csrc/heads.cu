@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(kHeadWarps * 32, 4) k_heads(const HeadArgs a, 
     const int seq = warp_count_le(b.n_seqs, [&](int i) { return (long long)b.q_start[i]; }, t);
     if (seq >= b.n_seqs) return;                       // behind the last sequence
     const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1];
-    slot = t < q0 || t >= q1 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, b.seq_len[seq] - (q1 - (int)t));
+    const long long at = (long long)b.seq_len[seq] - (q1 - t);   // a length may be any 32 bits
+    slot = t < q0 || t >= q1 || at < 0 ? -1 : page_slot(b, a.pages.page_size, a.pages.n_pages, seq, (int)at);
     if (slot < 0) {
       if (lane == 0) *a.status = OOS_EBATCH;
       return;

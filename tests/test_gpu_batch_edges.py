@@ -186,3 +186,19 @@ def test_append_of_many_heads(heads):
     assert int(st) == 0
     assert torch.equal(kp[1], k) and torch.equal(vp[1], v)
     assert bool((kp[0] == 7.0).all()) and bool((vp[0] == 7.0).all())
+
+
+def test_append_of_a_length_below_every_row():
+    """A length so far below zero that a row's position would wrap to a large one: left out and reported, also where
+    the table reaches that far."""
+    page = 1 << 30
+    k, v = randn(gen(1), 2, 1, 2, dtype=BF16), randn(gen(2), 2, 1, 2, dtype=BF16)
+    kp = torch.zeros(1, page, 1, 2, dtype=BF16, device="cuda")
+    vp = torch.zeros_like(kp)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    for n in (-2 ** 31, -2 ** 31 + 1, -1, 0):
+        batch = B.Batch(torch.tensor([0, 2], **i32), torch.tensor([n], **i32), torch.tensor([[0, 0]], **i32), 2)
+        st = status()
+        B.oos_paged_append(B.PagedCache(kp, vp), batch, k, v, None, 1e-6, None, None, st)
+        assert int(st) == B.OOS_EBATCH
+        assert int(torch.count_nonzero(kp)) == 0 and int(torch.count_nonzero(vp)) == 0, n
