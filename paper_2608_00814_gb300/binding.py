@@ -348,6 +348,7 @@ def oos_status_string(code):
 
 _DTYPES = {torch.float32: OOS_DTYPE_F32, torch.bfloat16: OOS_DTYPE_BF16, torch.float16: OOS_DTYPE_F16}
 _I32 = torch.int32
+_MAX = 2 ** 31 - 1      # of a size: ctypes would cut a larger one to 32 bits
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # a tenth of current_stream()'s time
 
 
@@ -368,6 +369,8 @@ def _dense(t, dtype, shape, dev, what):
 def _head_rows(t, dtype, n, heads, d, dev, what):
     """Address and token stride of rows [n, heads, d] whose heads are contiguous."""
     if t.dtype is not dtype or t.shape != (n, heads, d) or t.get_device() != dev:
+        raise OosError(OOS_EINVAL, what)
+    if n > _MAX or heads > _MAX or d > _MAX:
         raise OosError(OOS_EINVAL, what)
     s0, s1, s2 = t.stride()
     if (s2 != 1 and d != 1) or (s1 != d and heads != 1):
@@ -399,6 +402,7 @@ class PagedCache:
         self.k, self.v = k, v
         self.dev = k.get_device()
         n_pages, page_size, nkv, d = k.shape
+        _require(max(k.shape) <= _MAX, "PagedCache: k")
         self.heads, self.d = nkv, d
         self.c = OosPagedCache(_DTYPES[k.dtype], nkv, d, page_size, n_pages, k.data_ptr(), v.data_ptr())
         self.ref = ctypes.byref(self.c)
@@ -417,7 +421,8 @@ class Batch:
         _require(block_table.dim() == 2, "Batch: block_table")
         B, width = block_table.shape
         dev = self.dev = block_table.get_device()
-        _require(dev >= 0, "Batch: block_table")
+        _require(dev >= 0 and max(B, width) <= _MAX, "Batch: block_table")
+        _require(0 <= n_tokens <= _MAX, "Batch: n_tokens")
         self.q_start, self.seq_len, self.block_table, self.n_tokens = q_start, seq_len, block_table, int(n_tokens)
         i32 = torch.int32
         self.c = OosBatch(B, self.n_tokens, width, _dense(q_start, i32, (B + 1,), dev, "Batch: q_start"),
@@ -467,6 +472,8 @@ def oos_paged_append(cache, batch, k, v, k_norm, eps, rope, positions, out_statu
 
 
 def oos_shared_prefix_attention_workspace_bytes(q, prefix_len, cache, batch):
+    if not 0 <= prefix_len <= _MAX or q.shape[1] > _MAX:
+        return 0
     return int(lib().oos_shared_prefix_attention_workspace_bytes(q.shape[1], prefix_len, cache.ref, batch.ref))
 
 
@@ -483,6 +490,7 @@ def oos_shared_prefix_attention(q, prefix_k, prefix_v, prefix_len, cache, batch,
     qp, qs = _head_rows(q, dt, n, nq, d, dev, "oos_shared_prefix_attention: q")
     op, os_ = _head_rows(out, dt, n, nq, d, dev, "oos_shared_prefix_attention: out")
     pk = pv = None
+    _require(0 <= prefix_len <= _MAX, "oos_shared_prefix_attention: prefix_len")
     if prefix_len > 0:
         _require(prefix_k is not None and prefix_v is not None, "oos_shared_prefix_attention: prefix_k, prefix_v")
         shape = prefix_k.shape

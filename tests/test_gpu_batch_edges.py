@@ -202,3 +202,39 @@ def test_append_of_a_length_below_every_row():
         B.oos_paged_append(B.PagedCache(kp, vp), batch, k, v, None, 1e-6, None, None, st)
         assert int(st) == B.OOS_EBATCH
         assert int(torch.count_nonzero(kp)) == 0 and int(torch.count_nonzero(vp)) == 0, n
+
+
+# ------------------------------------------------------------------ sizes past 32 bits
+
+def test_binding_refuses_sizes_past_32_bits():
+    """The library takes sizes of 32 bits: a larger one is refused, not cut to what is left of it."""
+    wide = 2 ** 32
+    x = torch.ones(wide + 3, 1, 2, dtype=BF16, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    for t in (x, x.view(1, wide + 3, 2), x.view(-1)[:wide + 4].view(1, 1, wide + 4)):
+        with pytest.raises(B.OosError) as e:
+            B.oos_qk_norm_rope(t, None, None, None, 1e-6, None, None, t, None)
+        assert e.value.code == B.OOS_EINVAL
+    assert int((x != 1).sum()) == 0
+    for shape in ((wide + 1, 1, 1, 2), (1, wide + 1, 1, 2)):
+        pages = x.view(-1)[:2 * (wide + 1)].view(shape)
+        with pytest.raises(B.OosError) as e:
+            B.PagedCache(pages, pages)
+        assert e.value.code == B.OOS_EINVAL
+    starts, lens, table = torch.tensor([0, 1], **i32), torch.tensor([1], **i32), torch.zeros(1, 1, **i32)
+    for n in (wide + 1, 2 ** 31, -wide + 1):
+        with pytest.raises(B.OosError) as e:
+            B.Batch(starts, lens, table, n)
+        assert e.value.code == B.OOS_EINVAL
+    cache, batch = B.PagedCache(x[:16].view(1, 16, 1, 2), x[16:32].view(1, 16, 1, 2)), B.Batch(starts, lens, table, 1)
+    q = torch.ones(1, 1, 2, dtype=BF16, device="cuda")
+    ws, st, out = torch.empty(1 << 20, dtype=torch.uint8, device="cuda"), status(), torch.zeros_like(q)
+    for prefix in (wide + 1, 2 ** 31, -wide + 1, -wide):
+        with pytest.raises(B.OosError) as e:
+            B.oos_shared_prefix_attention(q, x, x, prefix, cache, batch, None, 1.0, out, ws, st)
+        assert e.value.code == B.OOS_EINVAL
+        assert B.oos_shared_prefix_attention_workspace_bytes(q, prefix, cache, batch) == 0
+    many = x[:wide].view(1, wide, 2)
+    with pytest.raises(B.OosError):
+        B.oos_shared_prefix_attention(many, None, None, 0, cache, batch, None, 1.0, many, ws, st)
+    assert B.oos_shared_prefix_attention_workspace_bytes(many, 0, cache, batch) == 0
