@@ -107,6 +107,22 @@ def test_attention_small_weights_of_binary16(dtype, far, where):
     assert bool(((got - want).abs() <= rel * want).all()), float(((got - want).abs() / want).max() / rel)
 
 
+@pytest.mark.parametrize("counts, heads", [([1] * 6, 8), ([3, 1, 2], 4), ([2, 7], 8)])
+def test_attention_own_keys_in_two_bf16_halves(counts, heads):
+    """Few rows over bf16 pages without a prefix: weights are multiplied as two bf16 halves, 2^-16 of a weight
+    together, and not as one, 2^-8.  Other terms as in check_attention."""
+    step = R.Step(counts, [c + 40 + i for i, c in enumerate(counts)], 16)
+    q, pk, pv, kp, vp = inputs(step, 0, heads, 1, 128, BF16, BF16, std=0.1)
+    out, st = attend(step, q, None, None, 0, kp, vp)
+    assert int(st) == 0
+    ref, mag, size = R.attention(step, q, pk[:0], pv[:0], kp, vp, 1 / math.sqrt(128))
+    rel = 2.0 ** -16 + 2 * (131 * R.F32 * size + 4 * R.F32) + (4 * max(step.lens) + 64) * R.F32 + 256 * R.F32 * size
+    tol = R.U[BF16] * ref.abs() + rel * mag
+    assert bool(((out.double().cpu() - ref).abs() <= tol).all())
+    # a bound that one bf16 half would not keep
+    assert rel < 2.0 ** -12
+
+
 # ------------------------------------------------------------------ scores that are not finite
 
 @pytest.mark.parametrize("dtype, kv", TYPES[1:])
@@ -169,6 +185,19 @@ def test_attention_bad_length_of_a_waiting_sequence(dtype, kv, counts):
         step.lens[1] = n
         out, st = attend(step, q, None, None, 0, kp, vp)
         assert int(st) == B.OOS_EBATCH and torch.equal(out, base), n
+
+
+def test_attention_row_with_one_key():
+    """A length below the step's rows: the row that is left at position 0 sees that key alone, and gives its v."""
+    for dtype, kv in TYPES:
+        step = R.Step([1, 2, 1], [40, 2, 30], 16)
+        q, _, _, kp, vp = inputs(step, 0, 4, 2, 128, dtype, kv)
+        step.lens[1] = 1
+        out, st = attend(step, q, None, None, 0, kp, vp)
+        assert int(st) == B.OOS_EBATCH
+        p, e = step.where(1, 0)
+        assert torch.equal(out[2], vp[p, e].repeat_interleave(2, 0).to(dtype))
+        assert bool((out[1] == 0).all())
 
 
 # ------------------------------------------------------------------ append
