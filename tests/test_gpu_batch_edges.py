@@ -3,6 +3,7 @@ and scores lose digits, and calls over several steps."""
 
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -198,6 +199,33 @@ def test_attention_row_with_one_key():
         p, e = step.where(1, 0)
         assert torch.equal(out[2], vp[p, e].repeat_interleave(2, 0).to(dtype))
         assert bool((out[1] == 0).all())
+
+
+# ------------------------------------------------------------------ how a call is cut up
+
+@pytest.mark.parametrize("dtype, kv", TYPES[1:])
+@pytest.mark.parametrize("n_seqs, rows, heads, prefix, own, tree, parts", [(1, 16, 8, 0, 1100, True, 4), (1, 16, 16, 1000, 1100, True, 8),
+                                                                           (16, 33, 16, 9000, 1100, False, 6)])
+def test_attention_many_rows_over_long_own_keys(dtype, kv, n_seqs, rows, heads, prefix, own, tree, parts):
+    """Ranges of own keys as parts, with the prefix among them, and beside its parts of a launch of its own; `parts` is
+    what a GPU of 152 SMs cuts the call into.  Lengths differ, down to sequences whose later ranges hold no key."""
+    lens = [own - (own - rows) * i // n_seqs for i in range(n_seqs)]
+    nkv = heads // 8
+    step = R.Step([rows] * n_seqs, lens, 16, pad=1)
+    rng = np.random.RandomState(1)
+    parent = [-1 if j == 0 else int(rng.randint(-1, j)) for _ in range(n_seqs) for j in range(rows)] if tree else None
+    q, pk, pv, kp, vp = inputs(step, prefix, heads, nkv, 128, dtype, kv)
+    par = None if parent is None else torch.tensor(parent + [-1], dtype=torch.int32, device="cuda")
+    size = B.oos_shared_prefix_attention_workspace_bytes(q, prefix, B.PagedCache(kp, vp), step.device(B))
+    if torch.cuda.get_device_properties(0).multi_processor_count == 152:
+        assert size // (step.rows * heads * 132 * 4) == parts
+    out, st = attend(step, q, pk, pv, prefix, kp, vp, par)
+    assert int(st) == 0
+    ref, mag, top = R.attention(step, q, pk[:prefix], pv[:prefix], kp, vp, 1 / math.sqrt(128), parent)
+    R.check_attention(out[:step.n], ref, mag, top, prefix + own, kv)
+    assert bool((out[step.n:] == 7.0).all())
+    again, _ = attend(step, q, pk, pv, prefix, kp, vp, par)
+    assert torch.equal(out, again)
 
 
 # ------------------------------------------------------------------ append
