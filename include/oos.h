@@ -457,7 +457,14 @@ int oos_qk_norm_rope(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_h
  *                  when a row's sequence, position or page is out of range; the
  *                  row is then left out and the others are appended.
  * Two sequences whose tables name the same page must not append to the same
- * position of it.  Returns OOS_EINVAL, OOS_EUNSUPPORTED, OOS_ECUDA. */
+ * position of it.
+ * After a step with trees the accepted nodes lie among the others.  Before the
+ * next step append their rows of k and v again, as a batch of the accepted rows
+ * alone in the order of their path, with the positions they had and seq_len the
+ * positions before the step and the accepted ones: they then stand where later
+ * steps take committed positions to be (oos_kv_compact does it for a contiguous
+ * cache), and what lies behind them is overwritten before it is seen.
+ * Returns OOS_EINVAL, OOS_EUNSUPPORTED, OOS_ECUDA. */
 int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32_t dtype, const void* k,
                      int64_t k_stride, const void* v, int64_t v_stride, const void* k_norm, float eps,
                      const oos_rope_config* rope, const int32_t* positions, int32_t* out_status, void* stream);

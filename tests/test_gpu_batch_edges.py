@@ -295,3 +295,71 @@ def test_binding_refuses_sizes_past_32_bits():
     with pytest.raises(B.OosError):
         B.oos_shared_prefix_attention(many, None, None, 0, cache, batch, None, 1.0, many, ws, st)
     assert B.oos_shared_prefix_attention_workspace_bytes(many, 0, cache, batch) == 0
+
+
+# ------------------------------------------------------------------ steps with trees
+
+@pytest.mark.parametrize("dtype, kv", TYPES)
+def test_steps_with_trees_follow_each_other(dtype, kv):
+    """Three steps with trees.  After each, a path of every tree is accepted (none of one tree's) and its rows are
+    appended again, where the next step takes committed positions to be: the rows of all steps see the accepted
+    history and their own ancestors, as if K and V lay in order."""
+    nq, nkv, d, page, prefix = 8, 2, 128, 16, 70
+    g, rng, i32 = gen(4), np.random.RandomState(7), dict(dtype=torch.int32, device="cuda")
+    pk, pv = [randn(g, prefix, nkv, d, dtype=kv) for _ in range(2)]
+    gain, rope = 1 + randn(g, d, dtype=dtype, std=0.1), B.OosRopeConfig(1e6)
+    held = [0, 5, 33]                                  # committed positions behind the prefix
+    pool = R.Step([1] * 3, [128] * 3, page)
+    kp, vp = [randn(g, pool.n_pages, page, nkv, d, dtype=kv) for _ in range(2)]
+    hist = [[[t[pool.where(b, s)].clone() for s in range(n)] for b, n in enumerate(held)] for t in (kp, vp)]
+    cache, st = B.PagedCache(kp, vp), status()
+
+    def on_pool(counts, lens):
+        step = R.Step(counts, lens, page)
+        step.table, step.n_pages, step.width = pool.table, pool.n_pages, pool.width
+        return step
+
+    for t in range(3):
+        counts = [int(c) for c in rng.randint(1, 30, 3)]
+        trees = [[-1 if j == 0 else int(rng.randint(max(-1, j - 4), j)) for j in range(c)] for c in counts]
+        depth = [R.ancestors(p).sum(1).tolist() for p in trees]
+        step = on_pool(counts, [n + c for n, c in zip(held, counts)])
+        pos = torch.tensor([prefix + held[b] + x - 1 for b in range(3) for x in depth[b]], **i32)
+        rows = randn(g, step.n, nq + 2 * nkv, d, dtype=dtype)
+        k, v = rows[:, nq:nq + nkv].contiguous(), rows[:, nq + nkv:].contiguous()
+        q, out = [torch.empty(step.n, nq, d, dtype=dtype, device="cuda") for _ in range(2)]
+        parent = [p for x in trees for p in x]
+        batch = step.device(B)
+        ws = torch.empty(B.oos_shared_prefix_attention_workspace_bytes(q, prefix, cache, batch), dtype=torch.uint8, device="cuda")
+        B.oos_qk_norm_rope(rows[:, :nq], None, gain, None, 1e-6, rope, pos, q, None)
+        B.oos_paged_append(cache, batch, k, v, gain, 1e-6, rope, pos, st)
+        B.oos_shared_prefix_attention(q, pk, pv, prefix, cache, batch, torch.tensor(parent, **i32), 1 / math.sqrt(d), out, ws, st)
+        assert int(st) == 0
+        # the definition over pages in order: the history, then the step's K and V
+        flat = R.Step(counts, step.lens, page)
+        fk, fv = [torch.zeros(flat.n_pages, page, nkv, d, dtype=kv, device="cuda") for _ in range(2)]
+        for f, h, src in ((fk, hist[0], kp), (fv, hist[1], vp)):
+            for b in range(3):
+                for s in range(step.lens[b]):
+                    f[flat.where(b, s)] = h[b][s] if s < held[b] else src[step.where(b, s)]
+        ref, mag, size = R.attention(flat, q, pk, pv, fk, fv, 1 / math.sqrt(d), parent)
+        R.check_attention(out, ref, mag, size, prefix + max(step.lens), F32 if kv is F32 else kv, t)
+        # accept a path of each tree, none of one
+        path = []
+        for b, p in enumerate(trees):
+            j, nodes = int(rng.randint(len(p))) if b != t else -1, []
+            while j >= 0:
+                nodes.insert(0, j)
+                j = p[j]
+            path.append(nodes)
+        for i, src in ((0, kp), (1, vp)):
+            for b in range(3):
+                hist[i][b] += [src[step.where(b, held[b] + j)].clone() for j in path[b]]
+        taken = torch.tensor([step.q_start[b] + j for b in range(3) for j in path[b]], dtype=torch.long, device="cuda")
+        held = [n + len(x) for n, x in zip(held, path)]
+        again = on_pool([len(x) for x in path], held)
+        B.oos_paged_append(cache, again.device(B), k[taken], v[taken], gain, 1e-6, rope, pos[taken], st)
+        assert int(st) == 0
+        for i, src in ((0, kp), (1, vp)):
+            for b in range(3):
+                assert all(torch.equal(src[pool.where(b, s)], hist[i][b][s]) for s in range(held[b])), (t, b)
