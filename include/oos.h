@@ -438,8 +438,9 @@ typedef struct {
  *   positions      DEVICE int32[n], any values (not read when rope is NULL)
  *   q_out, k_out   DEVICE rows; either may be its input (same address and
  *                  stride), and must not overlap an input otherwise
- * Sums, angles and products are fp32 (the angle is reduced exactly, whatever the
- * position); the result is rounded once.  Returns OOS_EINVAL on a NULL or
+ * Sums, angles and products are fp32; rates are doubles, and the angle is reduced
+ * from them exactly (their rounding counts 2^-55 of a turn per position, 2^-24 at
+ * 2^31).  The result is rounded once.  Returns OOS_EINVAL on a NULL or
  * out-of-range argument, OOS_EUNSUPPORTED on the head size or a type. */
 int oos_qk_norm_rope(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* q,
                      int64_t q_stride, const void* k, int64_t k_stride, const void* q_norm, const void* k_norm,

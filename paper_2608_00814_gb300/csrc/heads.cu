@@ -9,8 +9,8 @@
 // norm is a few shuffles and nothing goes through shared memory.  Bound by HBM.
 //
 // Angles: rate_m / 2 pi is kept as a 64-bit fraction of a turn; times the position
-// modulo 2^64 it is the angle's fraction of a turn to 2^-33 at position 2^31 (the
-// rate's own rounding to 53 bits), by integer products alone.  The nearest
+// modulo 2^64 it is the angle's fraction of a turn by integer products alone, off by what
+// the rate is off as a double: 2^-55 of a turn per position, 2^-24 at 2^31.  The nearest
 // quarter turn comes off exactly, so the fp32 sine and cosine see at most an
 // eighth of a turn.  A warp forms each of a token's angles once, dealt over its lanes,
 // hands them round by shuffles and keeps them over its heads.

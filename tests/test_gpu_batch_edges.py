@@ -2,6 +2,7 @@
 and scores lose digits, and calls over several steps."""
 
 import math
+from decimal import Decimal, localcontext
 
 import numpy as np
 import pytest
@@ -226,6 +227,33 @@ def test_attention_many_rows_over_long_own_keys(dtype, kv, n_seqs, rows, heads, 
     assert bool((out[step.n:] == 7.0).all())
     again, _ = attend(step, q, pk, pv, prefix, kp, vp, par)
     assert torch.equal(out, again)
+
+
+# ------------------------------------------------------------------ angles
+
+@pytest.mark.parametrize("theta", [1e4, 5e5, 1e6])
+@pytest.mark.parametrize("d", [128, 66])
+def test_norm_rope_angles_against_exact_rates(theta, d):
+    """Rates theta^(-2m/d) to 50 digits: the angle is off by at most 2^-55 of a turn per position, which moves a
+    pair by 2 pi of that; the rest as in check_norm_rope."""
+    turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937511")
+    pos = [1, 1000003, 2 ** 24 + 1, 2 ** 31 - 1, -2 ** 31]
+    angle = torch.zeros(len(pos), d // 2, dtype=torch.float64)
+    with localcontext() as digits:
+        digits.prec = 50
+        for m in range(d // 2):
+            rate = (Decimal(theta).ln() * Decimal(-2 * m) / Decimal(d)).exp() / turn
+            for i, p in enumerate(pos):
+                angle[i, m] = float((p * rate) % 1 * turn)
+    x = randn(gen(3), len(pos), 2, d)
+    y = torch.empty_like(x)
+    B.oos_qk_norm_rope(x, None, None, None, 0.0, B.OosRopeConfig(theta), torch.tensor(pos, dtype=torch.int32, device="cuda"), y, None)
+    c, s, xd, h = torch.cos(angle)[:, None], torch.sin(angle)[:, None], x.double().cpu(), d // 2
+    ref = torch.cat((xd[..., :h] * c - xd[..., h:] * s, xd[..., h:] * c + xd[..., :h] * s), -1)
+    r = torch.hypot(xd[..., :h], xd[..., h:]).repeat(1, 1, 2)
+    far = torch.tensor(pos, dtype=torch.float64).abs()[:, None, None] * 2.0 ** -55 * 2 * math.pi
+    tol = R.F32 * ref.abs() + (32 * R.F32 + far) * r
+    assert bool(((y.double().cpu() - ref).abs() <= tol).all())
 
 
 # ------------------------------------------------------------------ append
