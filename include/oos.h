@@ -484,14 +484,18 @@ int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32
  * matter (NaN included).
  *   dtype      of q and out.  With pages of OOS_DTYPE_F32: F32; BF16: BF16; F16:
  *              BF16 or F16 (OOS_EUNSUPPORTED otherwise).
- *   q, out     DEVICE rows of n_q_heads heads (a multiple of n_kv_heads)
+ *   q, out     DEVICE rows of n_q_heads heads (a multiple of n_kv_heads); out
+ *              overlaps no other argument
  *   workspace  DEVICE, >= oos_shared_prefix_attention_workspace_bytes of the same
  *              sizes, 256-byte aligned; caller-owned scratch for the call
  *   out_status DEVICE int32[1], the caller's to clear: OOS_EBATCH when a
  *              sequence's offsets, length or page is out of range (positions
  *              without a page are then not seen), OOS_ETREE when a parent is,
  *              OOS_ETIMEOUT when a pipeline wait exceeded 2 s (out is not valid).
- * Sums and softmax statistics are fp32.  scale > 0.  Pages and prefix of 16-bit
+ * Sums and softmax statistics are fp32.  With 16-bit pages and heads of 128 the
+ * weights that v is multiplied by are rounded to the pages' type (to 2^-16 for own
+ * keys of few rows over bf16 pages), and their sum is what a row is divided by.
+ * scale > 0.  Pages and prefix of 16-bit
  * types start on 16-byte boundaries, and n_tokens * n_q_heads + n_seqs is below
  * 2^26 (OOS_EINVAL otherwise), as prefix_len is up to 2^31 - 4096 and a sequence's
  * length (OOS_EBATCH otherwise).  With OOS_EBATCH for a sequence's offsets, or

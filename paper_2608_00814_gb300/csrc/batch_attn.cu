@@ -358,9 +358,9 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   if (p->tc) {
     // Tiles of 16 rows that read their sequence's pages again (from L2), or tiles of up to
     // 256 that are mostly empty.  Trees of 4 rows a node, 8 kv heads, 2048 prefix keys: 24
-    // rows on average 72 us against 100 (64 sequences), 34 against 38 (16); 48 rows 41
-    // against 40 (16 sequences; over 8192 keys 93 against 103), 16 against 24 (2), but 111
-    // against 91 (64); 96 rows 32 against 26 (4).
+    // rows on average 67 us against 102 (64 sequences), 30 against 39 (16); 48 rows 42
+    // against 40 (16 sequences; over 8192 keys 95 against 106), 16 against 25 (2), but 100
+    // against 94 (64); 96 rows 28 against 27 (4).
     p->few = rows <= 32ll * b.n_seqs || (rows <= 64ll * b.n_seqs && rows / 16 * c.n_kv_heads <= 4ll * sms);
     p->sequence = {false, 0, 1};
     if (p->few) p->pages = plan_pages_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
@@ -370,9 +370,9 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     // Blocks of few rows that join with the prefix's parts hold their place until those
     // are there.  Where the prefix's last wave leaves SMs free for long -- as much as the
     // chip does in 9 us -- they leave a part of their own and go on, for one more kernel.
-    // 256 sequences, 32768 prefix keys (20 us): 130 us against 142; 64 trees of 6 nodes, 2048
-    // keys: 66 against 72; 200 sequences of 64 heads, 16000 keys (9.6): 123 against 130; but
-    // 64 of 40 heads, 3000 keys (7.4): 56.5 against 55, 40 over 30000 keys (6.3): 53 against 48.
+    // 256 sequences, 32768 prefix keys (20 us): 137 us against 148; 64 trees of 6 nodes, 2048
+    // keys: 67 against 73; 200 sequences of 64 heads, 16000 keys (9.6): 127 against 135; but
+    // 64 of 40 heads, 3000 keys (7.4): 56 against 55, 40 over 30000 keys (6.3): 54 against 49.
     if (p->few && p->prefix.splits > 0) {
       const long long blocks = (long long)p->prefix.pairs * c.n_kv_heads * p->prefix.splits, waves = (blocks + sms - 1) / sms;
       const long long left = waves * sms - blocks;   // SMs, in the last wave

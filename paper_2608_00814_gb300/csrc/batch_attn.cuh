@@ -165,7 +165,7 @@ OOS_DEV uint32_t scaled_half2(uint32_t w, float f) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// clusters of the prefix kernel: what a call is cut into
+// the prefix kernel's blocks: what a call is cut into
 struct PrefixPlan {
   int splits;   // key ranges, a part each
   int pairs;    // pairs of 128-row tiles

@@ -11,7 +11,7 @@
 // Products run on mma.sync m16n8k16, operands by ldmatrix from rows whose 16-byte chunks
 // are swizzled by the key.
 //
-// Long sequences are bound by HBM (16 of 2000 keys on average, 8 kv heads: 49 us with the
+// Long sequences are bound by HBM (16 of 2000 keys on average, 8 kv heads: 48 us with the
 // prefix's kernel beside it, the bytes take 26), short ones by what a block does once --
 // lookups that follow each other, query fragments, the join -- at the 12 warps per SM that
 // the registers leave (256 of 150 keys, 2048 blocks: 40 us for 23 us of bytes; 47 before

@@ -17,10 +17,10 @@
 // The streams share one score buffer, held only from a product's issue until the threads
 // have its row in registers, so that the next unit's scores run under this one's
 // exponentials and wait for no P.V; one thread issues the scores, one the P.V products,
-// and the tensor cores take them turn by turn.  (A buffer for each stream with P over it
-// makes a stream's scores, weights and P.V follow each other: 159 us against 145 for 1024
-// rows of 8 heads over 32768 keys.  One thread for both kinds, a unit's scores before the
-// P.V of the one before: 197.)
+// and the tensor cores take them turn by turn.  (1024 rows of 8 heads over 32768 keys, each
+// against the kernel of its day: a buffer for each stream with P over it makes a stream's
+// scores, weights and P.V follow each other, 159 us against 145; one thread for both kinds,
+// a unit's scores before the P.V of the one before, 197.)
 //
 // P, 16-bit pairs in TMEM, is the A operand of P.V and is handed over in halves of 64
 // keys.  A weight is rounded to the type of V, as the product's operands have one type: by
@@ -740,7 +740,9 @@ static cudaError_t launch_tiles(const TileArgs& p, dim3 grid, cudaStream_t st) {
 }
 
 // us: a row tile's work on a key tile, and a block's beginning and end (with pages: the
-// lookups, the masks and the output besides)
+// lookups, the masks and the output besides).  A tile's is 0.90 with two row tiles over a
+// long prefix; cut by that number, the cases timed are the same but for 128 trees of 15
+// nodes on average over 2000 keys, 216 us instead of 150.
 constexpr double kTlTileUs = 0.83, kTlBlockUs = 8.0, kTlSeqBlockUs = 12.0;
 static double waves(long long blocks, int n_sms) { return (double)((blocks + n_sms - 1) / n_sms); }   // one block per SM
 
@@ -749,8 +751,8 @@ static double waves(long long blocks, int n_sms) { return (double)((blocks + n_s
 // 3 where the pages' kernel of few rows reads them (64 sequences of one token, 32 heads
 // over 8192 keys: 11 ranges 50 us with the pages', 16 by 8 bytes per ps 53).  Where that
 // kernel's blocks, own_sms full of them, then fit beside these, and these are not estimated
-// a quarter longer for it, fewer: the two run at once (8 sequences: 8 ranges 21 us, 10 or
-// 16 27).
+// a quarter longer for it, fewer: the two run at once (8 sequences: 8 ranges 20 us, 10 or
+// 16 26).
 PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, int n_sms) {
   PrefixPlan p;
   p.pairs = (int)((rows + 2 * kTlRows - 1) / (2 * kTlRows));
@@ -768,9 +770,13 @@ PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, 
   return p;
 }
 
-// Sequences of many rows.  They take the prefix along where that is
-// estimated shorter than a kernel for it and its parts (two tiles of own keys assumed: the
-// lengths are on the device).
+// Sequences of many rows.  They take the prefix along where that is estimated shorter than
+// a kernel for it and its parts.  The lengths are on the device: two tiles of own keys are
+// assumed (4 prompts of up to 200 tokens, 1000 prefix and up to 6000 own keys: 116 us, with
+// one tile 189; one tree, 2048 and up to 8000 keys: 41, with six tiles 38), and for ranges of
+// own keys alone no more than eight (one tree over up to 8000 keys: 42 us, with four 52, with
+// sixteen 37).  The table may be wider than its sequences need: with eight times the columns
+// 16 trees over 2048 + up to 400 keys take 57 us (58 otherwise) and 13 prompts the same 275.
 SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_len, long long most_keys, int n_sms) {
   SequencePlan p;
   p.tiles = (int)(n_seqs + rows / (2 * kTlRows));   // numbers; tiles that have rows, about:

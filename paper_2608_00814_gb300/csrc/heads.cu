@@ -62,7 +62,7 @@ OOS_DEV void turn(unsigned long long rate, int pos, float& c, float& s) {
 template <typename T, typename O, int VEC, int LANES, int NC, bool APPEND>
 __global__ void __launch_bounds__(kHeadWarps * 32, 4) k_heads(const HeadArgs a, const __grid_constant__ RopeTurns rope) {
   pdl_wait();      // the kernel before may be another call's
-  pdl_trigger();   // the next one's launch runs under this one: 2048 tokens 11.7 us a call, 13.2 without
+  pdl_trigger();   // the next one's launch runs under this one: 2048 tokens 11.8 us a call, 13.2 launched without
   const int lane = threadIdx.x & 31;
   const long long t = (long long)blockIdx.x * kHeadWarps + (threadIdx.x >> 5);
   const int slice = blockIdx.y, slices = gridDim.y;
@@ -280,7 +280,7 @@ static cudaError_t launch_heads_of(HeadArgs& a, const RopeTurns& rope, cudaStrea
   if (sms <= 0) return cudaErrorInvalidDevice;
   // A token's heads go to as many warps as it takes to give every SM 16, so that a
   // few tokens are spread out while many share the angles over all their heads (2048
-  // tokens of 40 heads: 10.6 us, 11.4 with 32 warps, 13.9 with 48).
+  // tokens of 40 heads, in a graph: 10.7 us, 11.4 with 32 warps, 13.9 with 48).
   const int total = a.heads[0] + a.heads[1], most = (total * LANES + 31) / 32;
   const int fit = 0x7fffffff / total;   // the kernel deals the heads by total * slices in 32 bits
   const int slices = (int)std::max(1ll, std::min<long long>(std::min({most, kMaxSlices, fit}), 16ll * sms / a.n));
