@@ -459,12 +459,12 @@ int oos_qk_norm_rope(int32_t dtype, int32_t n, int32_t n_q_heads, int32_t n_kv_h
  *                  row is then left out and the others are appended.
  * Two sequences whose tables name the same page must not append to the same
  * position of it.
- * After a step with trees the accepted nodes lie among the others.  Before the
- * next step append their rows of k and v again, as a batch of the accepted rows
- * alone in the order of their path, with the positions they had and seq_len the
- * positions before the step and the accepted ones: they then stand where later
- * steps take committed positions to be (oos_kv_compact does it for a contiguous
- * cache), and what lies behind them is overwritten before it is seen.
+ * After a step with trees the accepted nodes lie among the others: oos_paged_compact
+ * moves them to where later steps take committed positions to be, in all layers.
+ * (Appending their rows of k and v again, as a batch of the accepted rows alone in the
+ * order of their path, with the positions they had and seq_len the positions before the
+ * step and the accepted ones, does the same for one layer.)  What lies behind them is
+ * overwritten before it is seen.
  * Returns OOS_EINVAL, OOS_EUNSUPPORTED, OOS_ECUDA. */
 int oos_paged_append(const oos_paged_cache* cache, const oos_batch* batch, int32_t dtype, const void* k,
                      int64_t k_stride, const void* v, int64_t v_stride, const void* k_norm, float eps,
@@ -507,6 +507,104 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
                                 const oos_paged_cache* cache, const oos_batch* batch, const int32_t* tree_parent,
                                 float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
                                 int32_t* out_status, void* stream);
+
+/* ---- The same with pages of 8 bits ----------------------------------------
+ * A decoding step reads every position that its sequences hold; in 8 bits that is
+ * half the bytes, and twice the positions fit.  An element is an e4m3 code c (4
+ * significant bits, no infinity, magnitudes up to 448) and stands for c 2^e; e is
+ * shared by OOS_SCALE_BLOCK consecutive positions of a page, one kv head, K and V
+ * apart, and held as the byte e + 127, e in -117 .. 119 (the power of two that the
+ * byte is as an 8-bit exponent; other bytes count as the nearest of these). */
+#define OOS_SCALE_BLOCK 16
+
+/* One layer's pages: codes in [n_pages][page_size][n_kv_heads][head_dim], scales in
+ * [n_pages][page_size / OOS_SCALE_BLOCK][n_kv_heads]. */
+typedef struct {
+    int32_t n_kv_heads;
+    int32_t head_dim;    /* even, 2..128 */
+    int32_t page_size;   /* positions per page, a multiple of OOS_SCALE_BLOCK */
+    int32_t n_pages;
+    void* k;             /* DEVICE, e4m3 codes */
+    void* v;             /* DEVICE, e4m3 codes */
+    uint8_t* k_scale;    /* DEVICE */
+    uint8_t* v_scale;    /* DEVICE */
+} oos_paged_cache8;
+
+/* oos_paged_append into 8-bit pages: the same arguments, values, status and refusals.
+ * A block's scale is the least power of two with |x| <= 448 2^e for all of its rows.
+ *   - A block whose first position is one of the step's rows is begun anew: its scale
+ *     is that of the step's rows alone.
+ *   - Into one that holds positions from before the rows are added: where they need a
+ *     larger scale, the codes already there are rounded again to it; a smaller one is
+ *     not taken.  So a position appended alone may be rounded up to once more for each
+ *     octave that the scale grows by, each time by half a step of the new one.
+ * The scale is of the fp32 values after norm and rotation, which are then rounded once
+ * (nearest even).  Values that are not finite become NaN and do not count toward the
+ * scale; magnitudes above 448 2^119 become it.
+ * Two sequences must not append to the same block of positions of a page: a page that
+ * several sequences continue has to be copied first (oos_pages_copy8). */
+int oos_paged_append8(const oos_paged_cache8* cache, const oos_batch* batch, int32_t dtype, const void* k,
+                      int64_t k_stride, const void* v, int64_t v_stride, const void* k_norm, float eps,
+                      const oos_rope_config* rope, const int32_t* positions, int32_t* out_status, void* stream);
+
+/* oos_shared_prefix_attention over 8-bit pages; the prefix stays as it is.
+ *   prefix_dtype   of prefix_k / prefix_v: dtype's, or OOS_DTYPE_F16 with dtype BF16
+ *                  (OOS_EUNSUPPORTED otherwise; not looked at when prefix_len is 0)
+ * With 16-bit types and heads of 128, codes start on 16-byte boundaries (OOS_EINVAL
+ * otherwise), scores are of q with an error of at most 2^-22 of a row's largest |q| in
+ * every element, and the weights that own positions' v is multiplied by are rounded to
+ * 2^-16, or to bf16 (2^-8, a sixteenth of what a code is rounded by) where sequences have
+ * many rows; a row is divided by the sum of the rounded weights.  Everything else is as
+ * in oos_shared_prefix_attention, its status and refusals included. */
+size_t oos_shared_prefix_attention8_workspace_bytes(int32_t dtype, int32_t n_q_heads, int32_t prefix_len,
+                                                    const oos_paged_cache8* cache, const oos_batch* batch);
+int oos_shared_prefix_attention8(int32_t dtype, int32_t n_q_heads, const void* q, int64_t q_stride,
+                                 int32_t prefix_dtype, const void* prefix_k, const void* prefix_v, int32_t prefix_len,
+                                 const oos_paged_cache8* cache, const oos_batch* batch, const int32_t* tree_parent,
+                                 float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                                 int32_t* out_status, void* stream);
+
+/* ---- Pages between two steps ------------------------------------------------
+ * What becomes of pages after a step, for all layers of a model at once: layers are
+ * n_layers caches of one shape (and dtype), which share the page table; they are read
+ * on the host, during the call.  n_layers is 1 .. 1024; OOS_EINVAL otherwise, or where
+ * the layers differ in anything but their addresses.  Values move as they are, at any
+ * address that is a multiple of the element size (4-byte aligned rows take wider
+ * accesses).
+ *
+ * oos_paged_compact: after a step with trees, the accepted nodes of every sequence to
+ * the places where later steps take committed positions to be (what oos_kv_compact does
+ * for a contiguous cache): position first_b + j <- position first_b + nodes_b[j], first_b =
+ * seq_len[b] - n_b, for j < accepted_len[b], as they were before the call.
+ *   batch          of the step that appended the nodes
+ *   accepted       DEVICE int32[n_tokens]: nodes_b = accepted + q_start[b], places among
+ *                  the sequence's rows, strictly ascending (a path from the root down is)
+ *   accepted_len   DEVICE int32[n_seqs]: 0 .. n_b, of a sequence with at most 128 rows
+ *   out_seq_len    DEVICE int32[n_seqs]: first_b + accepted_len[b], the positions that
+ *                  count from now on; overlaps no other argument
+ *   out_status     DEVICE int32[1], the caller's to clear: OOS_EBATCH when a sequence's
+ *                  offsets, length, nodes or pages are out of range; all its positions then
+ *                  stay as they are, and out_seq_len[b] is seq_len[b].
+ * Sequences whose tables share a page must not share the positions of a step in it (of
+ * 8-bit pages: the blocks of positions).
+ * oos_paged_compact8: a block that positions are moved into takes the largest of its own
+ * scale and theirs, and all its codes are rounded to it (those of the largest stay as
+ * they are).
+ *
+ * oos_pages_copy: pages of forked sequences: page dst[i] <- page src[i], whole pages.
+ * A page may be src of several pairs; one that is a dst must be no other pair's dst or src.
+ *   src, dst       DEVICE int32[n], n in 0 .. 2^20; a pair out of range is left out and sets
+ *                  OOS_EBATCH
+ * All are stream-ordered, allocate nothing and may be captured into a CUDA graph. */
+int oos_paged_compact(const oos_paged_cache* layers, int32_t n_layers, const oos_batch* batch, const int32_t* accepted,
+                      const int32_t* accepted_len, int32_t* out_seq_len, int32_t* out_status, void* stream);
+int oos_paged_compact8(const oos_paged_cache8* layers, int32_t n_layers, const oos_batch* batch,
+                       const int32_t* accepted, const int32_t* accepted_len, int32_t* out_seq_len,
+                       int32_t* out_status, void* stream);
+int oos_pages_copy(const oos_paged_cache* layers, int32_t n_layers, const int32_t* src, const int32_t* dst, int32_t n,
+                   int32_t* out_status, void* stream);
+int oos_pages_copy8(const oos_paged_cache8* layers, int32_t n_layers, const int32_t* src, const int32_t* dst,
+                    int32_t n, int32_t* out_status, void* stream);
 
 /* Synchronise `stream` and return the device status of the last verify or
  * prefill (all of its prompt) on this handle: OOS_OK, OOS_ETREE or

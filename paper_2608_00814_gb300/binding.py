@@ -26,6 +26,7 @@ OOS_EBATCH = -8
 OOS_DTYPE_F32 = 0
 OOS_DTYPE_BF16 = 1
 OOS_DTYPE_F16 = 2
+OOS_SCALE_BLOCK = 16
 
 MAX_T = 128
 
@@ -70,6 +71,11 @@ class OosRopeConfig(ctypes.Structure):
 class OosPagedCache(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("n_kv_heads", c_i32), ("head_dim", c_i32), ("page_size", c_i32),
                 ("n_pages", c_i32), ("k", c_vp), ("v", c_vp)]
+
+
+class OosPagedCache8(ctypes.Structure):
+    _fields_ = [("n_kv_heads", c_i32), ("head_dim", c_i32), ("page_size", c_i32), ("n_pages", c_i32), ("k", c_vp),
+                ("v", c_vp), ("k_scale", c_vp), ("v_scale", c_vp)]
 
 
 class OosBatch(ctypes.Structure):
@@ -129,6 +135,20 @@ def lib():
                                                   P(OosBatch), c_vp, ctypes.c_float, c_vp, c_i64, c_vp,
                                                   ctypes.c_size_t, c_vp, c_vp]
         L.oos_shared_prefix_attention.restype = ctypes.c_int
+        L.oos_paged_append8.argtypes = [P(OosPagedCache8)] + L.oos_paged_append.argtypes[1:]
+        L.oos_paged_append8.restype = ctypes.c_int
+        L.oos_shared_prefix_attention8_workspace_bytes.argtypes = [c_i32, c_i32, c_i32, P(OosPagedCache8), P(OosBatch)]
+        L.oos_shared_prefix_attention8_workspace_bytes.restype = ctypes.c_size_t
+        L.oos_shared_prefix_attention8.argtypes = [c_i32, c_i32, c_vp, c_i64, c_i32, c_vp, c_vp, c_i32,
+                                                   P(OosPagedCache8), P(OosBatch), c_vp, ctypes.c_float, c_vp, c_i64,
+                                                   c_vp, ctypes.c_size_t, c_vp, c_vp]
+        L.oos_shared_prefix_attention8.restype = ctypes.c_int
+        for fn in ("oos_paged_compact", "oos_paged_compact8"):
+            getattr(L, fn).argtypes = [c_vp, c_i32, P(OosBatch), c_vp, c_vp, c_vp, c_vp, c_vp]
+            getattr(L, fn).restype = ctypes.c_int
+        for fn in ("oos_pages_copy", "oos_pages_copy8"):
+            getattr(L, fn).argtypes = [c_vp, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp]
+            getattr(L, fn).restype = ctypes.c_int
         L.oos_status_string.argtypes = [ctypes.c_int]
         L.oos_status_string.restype = ctypes.c_char_p
         for fn in ("oos_model_create", "oos_model_destroy", "oos_tree_verify", "oos_tree_verify_debug",
@@ -413,6 +433,62 @@ class PagedCache:
         return PagedCache(k, torch.zeros_like(k))
 
 
+_CODES = (torch.float8_e4m3fn,)
+_SCALES = (torch.uint8, torch.float8_e8m0fnu)
+
+
+class PagedCache8:
+    """One layer's pages of 8 bits: k and v float8_e4m3fn device tensors [n_pages, page_size, nkv, d], k_scale and
+    v_scale [n_pages, page_size / 16, nkv] of bytes (uint8, or the same as float8_e8m0fnu), plus the C view."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        _require(k.dim() == 4 and k.dtype in _CODES and k.is_contiguous() and k.device.type == "cuda", "PagedCache8: k")
+        _require(v.dtype is k.dtype and v.shape == k.shape and v.is_contiguous() and v.device == k.device,
+                 "PagedCache8: v")
+        n_pages, page_size, nkv, d = k.shape
+        _require(max(k.shape) <= _MAX and page_size % OOS_SCALE_BLOCK == 0, "PagedCache8: k")
+        for t in (k_scale, v_scale):
+            _require(t.dtype in _SCALES and t.shape == (n_pages, page_size // OOS_SCALE_BLOCK, nkv) and
+                     t.is_contiguous() and t.device == k.device, "PagedCache8: k_scale, v_scale")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.dev = k.get_device()
+        self.heads, self.d = nkv, d
+        self.c = OosPagedCache8(nkv, d, page_size, n_pages, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                                v_scale.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def empty(n_pages, page_size, n_kv_heads, head_dim, device="cuda"):
+        _require(page_size % OOS_SCALE_BLOCK == 0, "PagedCache8.empty: page_size")
+        shape, blocks = (n_pages, page_size, n_kv_heads, head_dim), (n_pages, page_size // OOS_SCALE_BLOCK, n_kv_heads)
+        return PagedCache8(*(torch.zeros(shape, dtype=torch.uint8, device=device).view(_CODES[0]) for _ in range(2)),
+                           *(torch.full(blocks, 127, dtype=torch.uint8, device=device) for _ in range(2)))
+
+    def dequantized(self):
+        """(k, v) as fp32 tensors."""
+        def values(codes, scale):
+            e = (scale.view(torch.uint8).float() - 127).clamp(-117, 119)
+            return codes.float() * torch.exp2(e).repeat_interleave(OOS_SCALE_BLOCK, 1)[..., None]
+        return values(self.k, self.k_scale), values(self.v, self.v_scale)
+
+
+class PagedLayers:
+    """The pages of all layers of a model, PagedCaches (or PagedCache8s) of one shape, as one C array."""
+
+    def __init__(self, layers):
+        self.layers = list(layers)
+        _require(len(self.layers) >= 1, "PagedLayers: layers")
+        first = self.layers[0]
+        kind = type(first)
+        _require(kind in (PagedCache, PagedCache8), "PagedLayers: layers")
+        for x in self.layers:
+            _require(type(x) is kind and x.dev == first.dev and x.k.shape == first.k.shape and x.k.dtype is first.k.dtype,
+                     "PagedLayers: layers")
+        self.kind, self.dev, self.n = kind, first.dev, len(self.layers)
+        self.c = (type(first.c) * self.n)(*[x.c for x in self.layers])
+        self.ref = ctypes.cast(self.c, c_vp)
+
+
 class Batch:
     """The ragged rows of one step: int32 device tensors q_start [B + 1], seq_len [B] and block_table
     [B, max_pages], and the number of rows, plus the C view."""
@@ -506,6 +582,107 @@ def oos_shared_prefix_attention(q, prefix_k, prefix_v, prefix_len, cache, batch,
         _dense(out_status, _I32, (1,), dev, "oos_shared_prefix_attention: out_status"), _raw_stream(stream, dev))
     if code:
         raise OosError(code, "oos_shared_prefix_attention")
+
+
+def oos_paged_append8(cache, batch, k, v, k_norm, eps, rope, positions, out_status, stream=None):
+    """As oos_paged_append, into a PagedCache8."""
+    dt, dev, n, nkv, d = k.dtype, _here(k, "oos_paged_append8: device"), batch.n_tokens, cache.heads, cache.d
+    _require(type(cache) is PagedCache8 and dt in _DTYPES and cache.dev == dev and batch.dev == dev,
+             "oos_paged_append8: cache, k, device")
+    kp, ks = _head_rows(k, dt, n, nkv, d, dev, "oos_paged_append8: k")
+    vp, vs = _head_rows(v, dt, n, nkv, d, dev, "oos_paged_append8: v")
+    code = (_lib or lib()).oos_paged_append8(
+        cache.ref, batch.ref, _DTYPES[dt], kp, ks, vp, vs, _dense(k_norm, dt, (d,), dev, "oos_paged_append8: k_norm"),
+        eps, rope, _dense(positions, _I32, (n,), dev, "oos_paged_append8: positions"),
+        _dense(out_status, _I32, (1,), dev, "oos_paged_append8: out_status"), _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, "oos_paged_append8")
+
+
+def oos_shared_prefix_attention8_workspace_bytes(q, prefix_len, cache, batch):
+    if not 0 <= prefix_len <= _MAX or q.dim() != 3 or q.shape[1] > _MAX or q.dtype not in _DTYPES:
+        return 0
+    return int(lib().oos_shared_prefix_attention8_workspace_bytes(_DTYPES[q.dtype], q.shape[1], prefix_len, cache.ref,
+                                                                  batch.ref))
+
+
+def oos_shared_prefix_attention8(q, prefix_k, prefix_v, prefix_len, cache, batch, tree_parent, scale, out, workspace,
+                                 out_status, stream=None):
+    """As oos_shared_prefix_attention, over a PagedCache8; the prefix is of q's type, or float16 with bfloat16 q."""
+    _require(q.dim() == 3 and q.dtype in _DTYPES and type(cache) is PagedCache8, "oos_shared_prefix_attention8: q, cache")
+    dt, dev, n = q.dtype, _here(q, "oos_shared_prefix_attention8: device"), batch.n_tokens
+    nkv, d, nq = cache.heads, cache.d, q.shape[1]
+    _require(cache.dev == dev and batch.dev == dev and workspace.get_device() == dev and workspace.is_contiguous(),
+             "oos_shared_prefix_attention8: device, workspace")
+    qp, qs = _head_rows(q, dt, n, nq, d, dev, "oos_shared_prefix_attention8: q")
+    op, os_ = _head_rows(out, dt, n, nq, d, dev, "oos_shared_prefix_attention8: out")
+    pk = pv = None
+    pt = _DTYPES[dt]
+    _require(0 <= prefix_len <= _MAX, "oos_shared_prefix_attention8: prefix_len")
+    if prefix_len > 0:
+        _require(prefix_k is not None and prefix_v is not None and prefix_k.dtype in _DTYPES,
+                 "oos_shared_prefix_attention8: prefix_k, prefix_v")
+        shape, kv = prefix_k.shape, prefix_k.dtype
+        _require(len(shape) == 3 and shape[0] >= prefix_len and shape[1] == nkv and shape[2] == d,
+                 "oos_shared_prefix_attention8: prefix_k")
+        pk = _dense(prefix_k, kv, shape, dev, "oos_shared_prefix_attention8: prefix_k")
+        pv = _dense(prefix_v, kv, shape, dev, "oos_shared_prefix_attention8: prefix_v")
+        pt = _DTYPES[kv]
+    code = (_lib or lib()).oos_shared_prefix_attention8(
+        _DTYPES[dt], nq, qp, qs, pt, pk, pv, prefix_len, cache.ref, batch.ref,
+        _dense(tree_parent, _I32, (n,), dev, "oos_shared_prefix_attention8: tree_parent"), scale, op, os_,
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+        _dense(out_status, _I32, (1,), dev, "oos_shared_prefix_attention8: out_status"), _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, "oos_shared_prefix_attention8")
+
+
+def _compact(name, kind, layers, batch, accepted, accepted_len, out_seq_len, out_status, stream):
+    dev = _here(accepted, name + ": device")
+    _require(type(layers) is PagedLayers and layers.kind is kind and layers.dev == dev and batch.dev == dev,
+             name + ": layers, device")
+    B = batch.c.n_seqs
+    code = getattr(_lib or lib(), name)(
+        layers.ref, layers.n, batch.ref, _dense(accepted, _I32, (batch.n_tokens,), dev, name + ": accepted"),
+        _dense(accepted_len, _I32, (B,), dev, name + ": accepted_len"),
+        _dense(out_seq_len, _I32, (B,), dev, name + ": out_seq_len"),
+        _dense(out_status, _I32, (1,), dev, name + ": out_status"), _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, name)
+
+
+def oos_paged_compact(layers, batch, accepted, accepted_len, out_seq_len, out_status, stream=None):
+    """layers: PagedLayers of PagedCaches; accepted: int32 [batch.n_tokens], sequence b's nodes from q_start[b] on;
+    accepted_len, out_seq_len: int32 [n_seqs]; out_status: int32 [1]."""
+    _compact("oos_paged_compact", PagedCache, layers, batch, accepted, accepted_len, out_seq_len, out_status, stream)
+
+
+def oos_paged_compact8(layers, batch, accepted, accepted_len, out_seq_len, out_status, stream=None):
+    """As oos_paged_compact, with PagedLayers of PagedCache8s."""
+    _compact("oos_paged_compact8", PagedCache8, layers, batch, accepted, accepted_len, out_seq_len, out_status, stream)
+
+
+def _pages_copy(name, kind, layers, src, dst, out_status, stream):
+    dev = _here(src, name + ": device")
+    _require(type(layers) is PagedLayers and layers.kind is kind and layers.dev == dev and src.dim() == 1,
+             name + ": layers, src, device")
+    n = src.shape[0]
+    _require(n <= _MAX, name + ": src")
+    code = getattr(_lib or lib(), name)(
+        layers.ref, layers.n, _dense(src, _I32, (n,), dev, name + ": src"), _dense(dst, _I32, (n,), dev, name + ": dst"),
+        n, _dense(out_status, _I32, (1,), dev, name + ": out_status"), _raw_stream(stream, dev))
+    if code:
+        raise OosError(code, name)
+
+
+def oos_pages_copy(layers, src, dst, out_status, stream=None):
+    """layers: PagedLayers of PagedCaches; src, dst: int32 [n] page numbers; out_status: int32 [1]."""
+    _pages_copy("oos_pages_copy", PagedCache, layers, src, dst, out_status, stream)
+
+
+def oos_pages_copy8(layers, src, dst, out_status, stream=None):
+    """As oos_pages_copy, with PagedLayers of PagedCache8s."""
+    _pages_copy("oos_pages_copy8", PagedCache8, layers, src, dst, out_status, stream)
 
 
 class VerifyOutputs:

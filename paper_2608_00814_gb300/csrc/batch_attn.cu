@@ -9,225 +9,20 @@
 // rows of all sequences stand in one tile, so that its keys are read once for
 // all; in the sequence's parts a tile holds rows of one sequence.
 //
-// k_attn_rows: CUDA cores, fp32 products, for every type and head size.  The 16-bit
-// types with heads of 128 take the tensor-core kernels of batch_tiles.cu and
+// k_attn_rows (batch_rows.cuh): CUDA cores, fp32 products, for every type and head size.
+// The 16-bit types with heads of 128 take the tensor-core kernels of batch_tiles.cu and
 // batch_pages.cu.
 #include <math.h>
 
 #include <algorithm>
 
 #include "batch_attn.cuh"
+#include "batch_rows.cuh"
+#include "pages8.cuh"
 
 namespace oos {
 
-constexpr int kRowKeys = 32;       // keys per tile
-constexpr int kRowThreads = 128;
 constexpr int kMaxParts = 32;      // parts of a row (a lane each in the join)
-
-// RT rows x 32 keys per step, 128 threads: thread (r, c) of 16 x 8 (of 4 x 32 with 4 rows)
-// has RT / 16 rows (one) and keys c, c + 8, c + 16, c + 24 (c) of S, and four columns in
-// 32 (in 128) of O.  The threads of a row share its statistics by shuffles.
-//
-// Bound by latency: lookups, loads, products, statistics and products of a tile follow each
-// other (40 sequences of up to 3 rows, 6 heads of 128, 900 + up to 300 keys, 16-row tiles:
-// 82 us, issue slots 39 % used, shared memory 40 %).  So a tile's places are looked up under
-// the tile before, the keys are dealt to as many blocks as help, and sequences of few rows
-// have tiles of 4 or 8, more of whose blocks fit on an SM (the same: 61 us).
-template <typename TQ, typename TK, int RT, int VEC>
-__global__ void __launch_bounds__(kRowThreads, RT == 64 ? 3 : RT == 16 ? 4 : 6) k_attn_rows(const BatchAttnArgs a) {
-  extern __shared__ __align__(16) float sm[];
-  constexpr int GROUPS = RT < 16 ? RT : 16, RPT = RT / GROUPS, TPR = kRowThreads / GROUPS;   // TPR: threads of a row
-  constexpr int KPT = kRowKeys / TPR, CPT = kMaxHeadDim / (4 * TPR);                         // keys, column quads of a thread
-  const int d = a.pages.d, ld = ((d + 3) & ~3) + 4, tid = threadIdx.x;
-  float* s_q = sm;                          // [RT][ld]
-  float* s_k = s_q + RT * ld;               // [32][ld]
-  float* s_v = s_k + kRowKeys * ld;
-  float* s_p = s_v + kRowKeys * ld;         // [RT][36]
-  constexpr int ldp = kRowKeys + 4;
-  __shared__ TreeScratch s_tree;
-  __shared__ long long s_at[2][kRowKeys];   // slot of each key in its buffer, -1: none; of two tiles in turn
-
-  // behind the prefix's launch, which has waited for what the caller wrote before it
-  // triggers, only the end waits
-  if (!a.own_part) pdl_wait();
-  pdl_trigger();
-  const int g = blockIdx.y;
-  const bool prefix = (int)blockIdx.x < a.p_tiles * a.p_splits;
-  const int local = prefix ? blockIdx.x : blockIdx.x - a.p_tiles * a.p_splits;
-  const int tile = prefix ? local / a.p_splits : local / a.s_splits;
-  const int split = prefix ? local % a.p_splits : local % a.s_splits;
-  const int splits = prefix ? a.p_splits : a.s_splits;
-  TileRows t;
-  if (prefix) {
-    t.seq = -1;
-    t.q0 = 0;
-    t.r0 = tile * RT;
-    t.rows = min(RT, a.batch.n_tokens * a.group - t.r0);
-    t.first = t.len = a.prefix_len;
-  } else if (!sequence_tile(a, tile, RT, &t)) {
-    if (a.own_part && blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();   // the join counts on the prefix's launch, too
-    return;
-  }
-  const unsigned long long (*anc)[2] = nullptr;
-  if (!prefix && a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
-  // the keys any row of the tile sees, dealt to the splits in whole tiles
-  const int last = (t.r0 + t.rows - 1) / a.group;   // its last token, counted from q0
-  const int n_keys = prefix || anc ? t.len : max(0, min(t.len, t.first + last + 1));
-  const int n_tiles = (n_keys + kRowKeys - 1) / kRowKeys;
-  const int k0 = (int)((long long)n_tiles * split / splits) * kRowKeys;
-  const int k1 = min(n_keys, (int)((long long)n_tiles * (split + 1) / splits) * kRowKeys);
-
-  for (int i = tid; i < RT * (ld - 4); i += kRowThreads) {
-    const int r = i / (ld - 4), c = i % (ld - 4);
-    float v = 0.f;
-    if (r < t.rows && c < d) {
-      const int row = t.r0 + r;
-      v = to_f32(((const TQ*)a.q)[(long long)(t.q0 + row / a.group) * a.q_stride + (g * a.group + row % a.group) * d + c]);
-    }
-    s_q[r * ld + c] = v;
-  }
-  const int tr = tid / TPR, tc = tid % TPR;
-  float o[RPT][CPT][4], m[RPT], l[RPT];
-#pragma unroll
-  for (int r = 0; r < RPT; ++r) {
-    m[r] = -INFINITY;
-    l[r] = 0.f;
-#pragma unroll
-    for (int c = 0; c < CPT; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[r][c][e] = 0.f;
-  }
-  const long long heads_d = (long long)a.pages.nkv * d;
-  auto look_up = [&](int key0) {   // the places of a tile's keys, while the tile before is worked on
-    if (tid >= kRowKeys) return;
-    const int key = key0 + tid;
-    long long at = -1;
-    if (key < k1) {
-      at = prefix ? key : page_slot(a.batch, a.pages.page_size, a.pages.n_pages, t.seq, key);
-      if (at < 0) *a.status = OOS_EBATCH;
-    }
-    s_at[(key0 - k0) / kRowKeys & 1][tid] = at;
-  };
-  look_up(k0);
-  for (int key0 = k0; key0 < k1; key0 += kRowKeys) {
-    __syncthreads();   // the tile before is read, this one's places are known
-    const long long* at_of = s_at[(key0 - k0) / kRowKeys & 1];
-    const TK* kb = (const TK*)(prefix ? a.pk : a.pages.k);
-    const TK* vb = (const TK*)(prefix ? a.pv : a.pages.v);
-    const int chunks = (ld - 4) / VEC;
-    for (int i = tid; i < kRowKeys * chunks; i += kRowThreads) {
-      const int key = i / chunks, c = (i % chunks) * VEC;
-      float kv[VEC], vv[VEC];
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) kv[e] = vv[e] = 0.f;   // keys that are not there must not reach a sum
-      if (at_of[key] >= 0 && c < d) {
-        const long long off = at_of[key] * heads_d + (long long)g * d + c;
-        load_vec<TK, VEC>(kb + off, kv);
-        load_vec<TK, VEC>(vb + off, vv);
-      }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        s_k[key * ld + c + e] = kv[e];
-        s_v[key * ld + c + e] = vv[e];
-      }
-    }
-    look_up(key0 + kRowKeys);
-    __syncthreads();
-    float s[RPT][KPT];
-    bool see[RPT][KPT];
-#pragma unroll
-    for (int r = 0; r < RPT; ++r)
-#pragma unroll
-      for (int j = 0; j < KPT; ++j) s[r][j] = 0.f;
-    for (int c = 0; c < ld - 4; c += 4) {
-      float4 kk[KPT];
-#pragma unroll
-      for (int j = 0; j < KPT; ++j) kk[j] = *reinterpret_cast<const float4*>(s_k + (tc + TPR * j) * ld + c);
-#pragma unroll
-      for (int r = 0; r < RPT; ++r) {
-        const float4 qq = *reinterpret_cast<const float4*>(s_q + (tr * RPT + r) * ld + c);
-#pragma unroll
-        for (int j = 0; j < KPT; ++j)
-          s[r][j] += qq.x * kk[j].x + qq.y * kk[j].y + qq.z * kk[j].z + qq.w * kk[j].w;
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < RPT; ++r) {
-      const int token = (t.r0 + tr * RPT + r) / a.group;
-      float mx = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < KPT; ++j) {
-        const int key = key0 + tc + TPR * j, own = key - t.first;
-        bool ok = at_of[tc + TPR * j] >= 0;
-        if (!prefix && own >= 0)
-          ok = ok && (anc ? token < t.n && own < kMaxTreeRows && ((anc[token][own >> 6] >> (own & 63)) & 1) : own <= token);
-        see[r][j] = ok;
-        s[r][j] = ok ? s[r][j] * a.scale_log2 : -INFINITY;
-        mx = max_nan(mx, s[r][j]);
-      }
-#pragma unroll
-      for (int x = 1; x < TPR; x *= 2) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-      const float mn = max_nan(m[r], mx);
-      const bool live = mn != -INFINITY;
-      const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mn);
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < KPT; ++j) {
-        const float p = live ? exp2f(s[r][j] - mn) : 0.f;
-        sum += p;
-        s_p[(tr * RPT + r) * ldp + tc + TPR * j] = see[r][j] ? p : -1.f;   // negative: not seen
-      }
-#pragma unroll
-      for (int x = 1; x < TPR; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      l[r] = l[r] * f + sum;
-      m[r] = mn;
-#pragma unroll
-      for (int c = 0; c < CPT; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[r][c][e] *= f;
-    }
-    __syncwarp();   // a row's weights are written and read by the same lanes
-#pragma unroll 8
-    for (int key = 0; key < kRowKeys; ++key) {
-      float p[RPT];
-#pragma unroll
-      for (int r = 0; r < RPT; ++r) p[r] = s_p[(tr * RPT + r) * ldp + key];
-#pragma unroll
-      for (int c = 0; c < CPT; ++c) {
-        const int col = tc * 4 + 4 * TPR * c;
-        if (col >= d) continue;
-        const float4 v = *reinterpret_cast<const float4*>(s_v + key * ld + col);
-#pragma unroll
-        for (int r = 0; r < RPT; ++r) {
-          if (p[r] < 0.f) continue;   // whatever its v is
-          o[r][c][0] += p[r] * v.x;
-          o[r][c][1] += p[r] * v.y;
-          o[r][c][2] += p[r] * v.z;
-          o[r][c][3] += p[r] * v.w;
-        }
-      }
-    }
-    __syncwarp();
-  }
-  const int part = prefix ? split : a.p_splits + split;
-  const long long n_rows = (long long)a.batch.n_tokens * a.nq;
-#pragma unroll
-  for (int r = 0; r < RPT; ++r) {
-    const int lr = tr * RPT + r;
-    if (lr >= t.rows) continue;
-    const int row = t.r0 + lr;
-    const long long at = part * n_rows + (long long)(t.q0 + row / a.group) * a.nq + g * a.group + row % a.group;
-    if (tc == 0) a.part_ml[at] = make_float2(m[r], l[r]);
-#pragma unroll
-    for (int c = 0; c < CPT; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int col = tc * 4 + 4 * TPR * c + e;
-        if (col < d) a.part_o[at * d + col] = o[r][c][e];
-      }
-  }
-  if (a.own_part && blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();
-}
 
 // A warp per row adds its parts up: weights 2^(m - max m), the sum divided by the
 // weighted l.  Parts are taken in order, so the result does not depend on timing.
@@ -348,13 +143,14 @@ cudaError_t kernel_ready(std::atomic<uint64_t>& ready, const void* kernel, int s
   return e;
 }
 
-static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, const oos_batch& b, BatchAttnPlan* p) {
+// own8: pages of 8 bits; c.dtype: the type of the prefix, and of other pages
+static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, const oos_batch& b, bool own8, BatchAttnPlan* p) {
   const int sms = device_sms();
   if (sms <= 0) return false;
   const int G = nq / c.n_kv_heads;
   const long long rows = (long long)b.n_tokens * G;
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, kMaxKeys);
-  p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
+  p->tc = !own8 && c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc) {
     // Tiles of 16 rows that read their sequence's pages again (from L2), or tiles of up to
     // 256 that are mostly empty.  Trees of 4 rows a node, 8 kv heads, 2048 prefix keys: 24
@@ -410,102 +206,76 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   return true;
 }
 
-template <typename TQ, typename TK, int RT, int VEC>
-static cudaError_t launch_rows_of(const BatchAttnArgs& a, cudaStream_t st) {
-  const int ld = ((a.pages.d + 3) & ~3) + 4;
-  auto smem_of = [](int ld_) { return ((RT + 2 * kRowKeys) * ld_ + RT * (kRowKeys + 4)) * 4; };
-  const size_t smem = smem_of(ld);
-  static std::atomic<uint64_t> ready{0};
-  cudaError_t e = kernel_ready(ready, (const void*)k_attn_rows<TQ, TK, RT, VEC>, smem_of(kMaxHeadDim + 4));
-  if (e != cudaSuccess) return e;
-  const int blocks = a.p_tiles * a.p_splits + a.s_tiles * a.s_splits;
-  return launch(true, k_attn_rows<TQ, TK, RT, VEC>, dim3(blocks, a.pages.nkv), dim3(kRowThreads), smem, st, a);
-}
-
+// TK: elements of the prefix, and of pages that are not of 8 bits
 template <typename TQ, typename TK>
-static cudaError_t launch_rows(const BatchAttnArgs& a, int rt, bool vec, cudaStream_t st) {
-  if (rt == 4) return vec ? launch_rows_of<TQ, TK, 4, 4>(a, st) : launch_rows_of<TQ, TK, 4, 1>(a, st);
-  if (rt == 8) return vec ? launch_rows_of<TQ, TK, 8, 4>(a, st) : launch_rows_of<TQ, TK, 8, 1>(a, st);
-  if (rt == 16) return vec ? launch_rows_of<TQ, TK, 16, 4>(a, st) : launch_rows_of<TQ, TK, 16, 1>(a, st);
-  return vec ? launch_rows_of<TQ, TK, 64, 4>(a, st) : launch_rows_of<TQ, TK, 64, 1>(a, st);
-}
-
-template <typename TQ, typename TK>
-static cudaError_t launch_batch_rows(BatchAttnArgs& a, const BatchAttnPlan& p, cudaStream_t st) {
+static cudaError_t launch_batch_rows(BatchAttnArgs& a, const BatchAttnPlan& p, int dtype, cudaStream_t st) {
+  const bool own8 = a.k_scale != nullptr;
   a.p_tiles = p.p_tiles;
   a.p_splits = p.p_splits;
   a.s_tiles = p.s_tiles;
   a.s_splits = p.s_splits;
   // rows of whole aligned 4-element groups, else one element at a time
-  const uintptr_t any = (uintptr_t)a.pages.k | (uintptr_t)a.pages.v | (uintptr_t)a.pk | (uintptr_t)a.pv;
+  const uintptr_t any = (own8 ? 0 : (uintptr_t)a.pages.k | (uintptr_t)a.pages.v) | (uintptr_t)a.pk | (uintptr_t)a.pv;
   const bool vec = a.pages.d % 4 == 0 && any % (4 * sizeof(TK)) == 0;
   cudaError_t e = cudaSuccess;
-  if (p.p_tiles > 0 && p.p_rt != p.rt) {   // the prefix's blocks in a launch of their own
+  if (p.p_tiles > 0 && (own8 || p.p_rt != p.rt)) {   // the prefix's blocks in a launch of their own
     a.s_tiles = 0;
     e = launch_rows<TQ, TK>(a, p.p_rt, vec, st);
     a.s_tiles = p.s_tiles;
     a.p_tiles = 0;
     a.own_part = true;
   }
-  if (e == cudaSuccess) e = launch_rows<TQ, TK>(a, p.rt, vec, st);
+  if (e == cudaSuccess) e = own8 ? launch_rows8(a, dtype, p.rt, st) : launch_rows<TQ, TK>(a, p.rt, vec, st);
   if (e != cudaSuccess) return e;
   const long long rows = (long long)a.batch.n_tokens * a.nq;
   return launch(true, k_attn_join<TQ>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, a);
 }
 
-static bool attn_shape_ok(int nq, int prefix_len, const oos_paged_cache* c, const oos_batch* b) {
-  if (!c || !b || nq < 1 || prefix_len < 0 || prefix_len > kMaxKeys || c->n_kv_heads < 1 || c->page_size < 1 || c->n_pages < 1) return false;
-  if (nq % c->n_kv_heads || c->n_kv_heads > 65535 || b->n_seqs < 1 || b->n_tokens < 0 || b->max_pages < 1) return false;
+static bool attn_shape_ok(int nq, int prefix_len, const oos_paged_cache& c, const oos_batch* b) {
+  if (!b || nq < 1 || prefix_len < 0 || prefix_len > kMaxKeys || c.n_kv_heads < 1 || c.page_size < 1 || c.n_pages < 1) return false;
+  if (nq % c.n_kv_heads || c.n_kv_heads > 65535 || b->n_seqs < 1 || b->n_tokens < 0 || b->max_pages < 1) return false;
   return (long long)b->n_tokens * nq + b->n_seqs < (1ll << 31) / kMaxParts && nq <= (1 << 20);
 }
 
-}  // namespace oos
-
-using namespace oos;
-
-extern "C" {
-
-size_t oos_shared_prefix_attention_workspace_bytes(int32_t n_q_heads, int32_t prefix_len, const oos_paged_cache* cache,
-                                                   const oos_batch* batch) {
-  if (!attn_shape_ok(n_q_heads, prefix_len, cache, batch)) return 0;
-  if (!dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return 0;
-  BatchAttnPlan p;
-  return plan_batch_attn(n_q_heads, prefix_len, *cache, *batch, &p) ? std::max<size_t>(p.bytes, 256) : 0;
+// the shape and codes of 8-bit pages, beside a prefix of dtype
+static oos_paged_cache pages_of(const oos_paged_cache8& c, int dtype) {
+  return {dtype, c.n_kv_heads, c.head_dim, c.page_size, c.n_pages, c.k, c.v};
 }
 
-int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q, int64_t q_stride,
-                                const void* prefix_k, const void* prefix_v, int32_t prefix_len,
-                                const oos_paged_cache* cache, const oos_batch* batch, const int32_t* tree_parent,
-                                float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
-                                int32_t* out_status, void* stream) {
-  if (!attn_shape_ok(n_q_heads, prefix_len, cache, batch) || !pages_ok(cache) || !batch_ok(batch) || !out_status)
-    return OOS_EINVAL;
-  if (!(scale > 0.f) || !(scale < INFINITY)) return OOS_EINVAL;
-  if (!dtype_ok(dtype) || !dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return OOS_EUNSUPPORTED;
-  if (dtype != cache->dtype && !(dtype == OOS_DTYPE_BF16 && cache->dtype == OOS_DTYPE_F16)) return OOS_EUNSUPPORTED;
+static bool attn_dtypes_ok(int dtype, int kv_dtype) {   // of queries, of 16-bit or fp32 keys
+  return dtype == kv_dtype || (dtype == OOS_DTYPE_BF16 && kv_dtype == OOS_DTYPE_F16);
+}
+
+// c: the pages, of 8 bits where scales are given; c.dtype: the prefix's type then
+static int attend(int dtype, int n_q_heads, const void* q, int64_t q_stride, const void* prefix_k, const void* prefix_v,
+                  int prefix_len, const oos_paged_cache& c, const uint8_t* k_scale, const uint8_t* v_scale,
+                  const oos_batch* batch, const int32_t* tree_parent, float scale, void* out, int64_t out_stride,
+                  void* workspace, size_t ws_bytes, int32_t* out_status, void* stream) {
+  const bool own8 = k_scale != nullptr;
   if (prefix_len > 0 && (!prefix_k || !prefix_v)) return OOS_EINVAL;
-  if (cache->dtype != OOS_DTYPE_F32) {
-    const uintptr_t any = (uintptr_t)cache->k | (uintptr_t)cache->v |
-                          (prefix_len > 0 ? (uintptr_t)prefix_k | (uintptr_t)prefix_v : 0);
-    if (any & 15) return OOS_EINVAL;
-  }
+  const uintptr_t prefix = prefix_len > 0 ? (uintptr_t)prefix_k | (uintptr_t)prefix_v : 0, pages = (uintptr_t)c.k | (uintptr_t)c.v;
+  if (own8 ? dtype != OOS_DTYPE_F32 && ((prefix | (c.head_dim == 128 ? pages : 0)) & 15)
+           : c.dtype != OOS_DTYPE_F32 && ((prefix | pages) & 15))
+    return OOS_EINVAL;
   if (batch->n_tokens == 0) return OOS_OK;
-  const long long w = (long long)n_q_heads * cache->head_dim;
+  const long long w = (long long)n_q_heads * c.head_dim;
   if (!q || !out || q_stride < w || out_stride < w) return OOS_EINVAL;
   BatchAttnPlan p;
-  if (!plan_batch_attn(n_q_heads, prefix_len, *cache, *batch, &p)) return OOS_ECUDA;
+  if (!plan_batch_attn(n_q_heads, prefix_len, c, *batch, own8, &p)) return OOS_ECUDA;
   if (!workspace || ((uintptr_t)workspace & 255) || ws_bytes < p.bytes) return OOS_EWORKSPACE;
   BatchAttnArgs a = {};
-  a.pages = view_of(*cache);
+  a.pages = view_of(c);
   a.batch = view_of(*batch);
   a.q = q;
   a.q_stride = q_stride;
   a.pk = prefix_len > 0 ? (const uint8_t*)prefix_k : nullptr;
   a.pv = prefix_len > 0 ? (const uint8_t*)prefix_v : nullptr;
   a.prefix_len = prefix_len;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
   a.parent = tree_parent;
   a.nq = n_q_heads;
-  a.group = n_q_heads / cache->n_kv_heads;
+  a.group = n_q_heads / c.n_kv_heads;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.out = out;
   a.out_stride = out_stride;
@@ -518,10 +288,10 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
     a.p_splits = p.prefix.splits;
     a.s_splits = p.few ? p.pages.splits : p.sequence.splits;
     a.own_part = p.few && p.pages.part;
-    e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, cache->dtype, st) : cudaSuccess;
+    e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, c.dtype, st) : cudaSuccess;
     if (e == cudaSuccess)
-      e = p.few ? launch_pages_tc(a, p.pages, dtype, cache->dtype, st)
-                : launch_sequence_tc(a, p.sequence, dtype, cache->dtype, st);
+      e = p.few ? launch_pages_tc(a, p.pages, dtype, c.dtype, st)
+                : launch_sequence_tc(a, p.sequence, dtype, c.dtype, st);
     if (p.few) a.s_splits = p.pages.part;   // for the join
     if (e == cudaSuccess && (p.few ? p.pages.part : a.s_splits > 1)) {
       const dim3 grid((unsigned)(((long long)batch->n_tokens * n_q_heads + 7) / 8));
@@ -529,15 +299,68 @@ int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q,
                                   : launch(true, k_attn_join_parts<__half>, grid, dim3(256), 0, st, a);
     }
   } else if (dtype == OOS_DTYPE_F32) {
-    e = launch_batch_rows<float, float>(a, p, st);
-  } else if (cache->dtype == OOS_DTYPE_BF16) {
-    e = launch_batch_rows<__nv_bfloat16, __nv_bfloat16>(a, p, st);
+    e = launch_batch_rows<float, float>(a, p, dtype, st);
+  } else if (c.dtype == OOS_DTYPE_BF16) {
+    e = launch_batch_rows<__nv_bfloat16, __nv_bfloat16>(a, p, dtype, st);
   } else if (dtype == OOS_DTYPE_BF16) {
-    e = launch_batch_rows<__nv_bfloat16, __half>(a, p, st);
+    e = launch_batch_rows<__nv_bfloat16, __half>(a, p, dtype, st);
   } else {
-    e = launch_batch_rows<__half, __half>(a, p, st);
+    e = launch_batch_rows<__half, __half>(a, p, dtype, st);
   }
   return e == cudaSuccess ? OOS_OK : OOS_ECUDA;
+}
+
+}  // namespace oos
+
+using namespace oos;
+
+extern "C" {
+
+size_t oos_shared_prefix_attention_workspace_bytes(int32_t n_q_heads, int32_t prefix_len, const oos_paged_cache* cache,
+                                                   const oos_batch* batch) {
+  if (!cache || !attn_shape_ok(n_q_heads, prefix_len, *cache, batch)) return 0;
+  if (!dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return 0;
+  BatchAttnPlan p;
+  return plan_batch_attn(n_q_heads, prefix_len, *cache, *batch, false, &p) ? std::max<size_t>(p.bytes, 256) : 0;
+}
+
+int oos_shared_prefix_attention(int32_t dtype, int32_t n_q_heads, const void* q, int64_t q_stride,
+                                const void* prefix_k, const void* prefix_v, int32_t prefix_len,
+                                const oos_paged_cache* cache, const oos_batch* batch, const int32_t* tree_parent,
+                                float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                                int32_t* out_status, void* stream) {
+  if (!cache || !attn_shape_ok(n_q_heads, prefix_len, *cache, batch) || !pages_ok(cache) || !batch_ok(batch) || !out_status)
+    return OOS_EINVAL;
+  if (!(scale > 0.f) || !(scale < INFINITY)) return OOS_EINVAL;
+  if (!dtype_ok(dtype) || !dtype_ok(cache->dtype) || !head_dim_ok(cache->head_dim)) return OOS_EUNSUPPORTED;
+  if (!attn_dtypes_ok(dtype, cache->dtype)) return OOS_EUNSUPPORTED;
+  return attend(dtype, n_q_heads, q, q_stride, prefix_k, prefix_v, prefix_len, *cache, nullptr, nullptr, batch,
+                tree_parent, scale, out, out_stride, workspace, ws_bytes, out_status, stream);
+}
+
+size_t oos_shared_prefix_attention8_workspace_bytes(int32_t dtype, int32_t n_q_heads, int32_t prefix_len,
+                                                    const oos_paged_cache8* cache, const oos_batch* batch) {
+  if (!cache || !attn_shape_ok(n_q_heads, prefix_len, pages_of(*cache, dtype), batch)) return 0;
+  if (!dtype_ok(dtype) || !head_dim_ok(cache->head_dim) || cache->page_size % kScaleBlock) return 0;
+  BatchAttnPlan p;
+  return plan_batch_attn(n_q_heads, prefix_len, pages_of(*cache, dtype), *batch, true, &p) ? std::max<size_t>(p.bytes, 256) : 0;
+}
+
+int oos_shared_prefix_attention8(int32_t dtype, int32_t n_q_heads, const void* q, int64_t q_stride,
+                                 int32_t prefix_dtype, const void* prefix_k, const void* prefix_v, int32_t prefix_len,
+                                 const oos_paged_cache8* cache, const oos_batch* batch, const int32_t* tree_parent,
+                                 float scale, void* out, int64_t out_stride, void* workspace, size_t ws_bytes,
+                                 int32_t* out_status, void* stream) {
+  if (!cache || !attn_shape_ok(n_q_heads, prefix_len, pages_of(*cache, dtype), batch) || !pages8_ok(cache) ||
+      !batch_ok(batch) || !out_status)
+    return OOS_EINVAL;
+  if (!(scale > 0.f) || !(scale < INFINITY)) return OOS_EINVAL;
+  if (prefix_len == 0) prefix_dtype = dtype;
+  if (!dtype_ok(dtype) || !dtype_ok(prefix_dtype) || !head_dim_ok(cache->head_dim)) return OOS_EUNSUPPORTED;
+  if (!attn_dtypes_ok(dtype, prefix_dtype)) return OOS_EUNSUPPORTED;
+  return attend(dtype, n_q_heads, q, q_stride, prefix_k, prefix_v, prefix_len, pages_of(*cache, prefix_dtype),
+                cache->k_scale, cache->v_scale, batch, tree_parent, scale, out, out_stride, workspace, ws_bytes,
+                out_status, stream);
 }
 
 }  // extern "C"

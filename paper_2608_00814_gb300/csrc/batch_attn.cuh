@@ -23,6 +23,8 @@ struct BatchAttnArgs {
   const uint8_t* pk;
   const uint8_t* pv;
   int prefix_len;
+  const uint8_t* k_scale;   // of 8-bit pages
+  const uint8_t* v_scale;
   const int32_t* parent;
   int nq, group;
   float scale_log2;
@@ -185,6 +187,8 @@ struct SequencePlan {
 };
 SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_len, long long most_keys, int n_sms);
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
+// own keys in 8-bit pages on CUDA cores, tiles of rt rows: parts p_splits ..
+cudaError_t launch_rows8(const BatchAttnArgs& a, int dtype, int rt, cudaStream_t st);
 // the prefix's parts of every row
 cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dtype, int kv_dtype, cudaStream_t st);
 // the sequences' own keys, joined with the prefix's p_splits parts into out; with several

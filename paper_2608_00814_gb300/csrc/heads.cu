@@ -44,18 +44,6 @@ struct HeadArgs {
   int32_t* status;
 };
 
-// cos and sin of pos * rate, the rate in units of 2^-64 turns
-OOS_DEV void turn(unsigned long long rate, int pos, float& c, float& s) {
-  const unsigned long long t = (unsigned long long)(long long)pos * rate;
-  const unsigned long long quarter = (t + (1ull << 61)) >> 62;
-  const float x = (float)(long long)(t - (quarter << 62)) * 0x1p-63f;   // in half turns, |x| <= 1/4
-  float sn, cs;
-  sincospif(x, &sn, &cs);
-  const float a = quarter & 1 ? sn : cs, b = quarter & 1 ? cs : sn;
-  c = (quarter + 1) & 2 ? -a : a;
-  s = quarter & 2 ? -b : b;
-}
-
 // T: elements of the inputs and gains, O: of the outputs.  VEC: values per access.
 // LANES: lanes per head, NC: chunks of half a head per lane.  APPEND: in[1] goes to
 // the pages' K, v to their V.

@@ -1,0 +1,272 @@
+// Append of a step's K (normed and turned on the way) and V to 8-bit pages.
+//
+// A scale belongs to 16 positions of a head, so a warp takes one such block of K or V: its
+// rows (up to 16) are loaded, K's are normed and turned as in heads.cu, all stay in
+// registers as fp32 while their largest magnitude is found, and are rounded once to the
+// scale it needs.  A block of threads holds the heads of the same positions, whose angles
+// it forms once, in shared memory.
+//
+// Where the block held positions before, its scale may only grow, as the codes there would
+// gain nothing by a smaller one; when it does, they are read, divided by a power of two and
+// rounded again.
+//
+// Bytes: the rows read once and half (a quarter) as many written.
+#include <math.h>
+
+#include <algorithm>
+
+#include "internal.h"
+#include "pages8.cuh"
+
+namespace oos {
+
+constexpr int kApMaxHeads = 8;   // of a block: a warp for K and one for V each
+
+struct Append8Args {
+  Pages8View pages;
+  BatchView batch;
+  const void* in[2];   // K, V
+  long long stride[2];
+  const void* gain;
+  const int32_t* positions;   // nullptr: no rotation
+  float eps;
+  int32_t* status;
+};
+
+// T: elements of the rows.  A row's half is dealt in chunks of VEC to LANES lanes, NC each;
+// 32 / LANES rows at once.
+template <typename T, int VEC, int LANES, int NC>
+__global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args a, const __grid_constant__ RopeTurns rope) {
+  constexpr int ROWS = 32 / LANES, PASSES = kScaleBlock / ROWS;
+  __shared__ float2 s_turn[kScaleBlock][kMaxHeadDim / 2];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, heads = blockDim.x / 64;
+  const int d = a.pages.p.d, d2 = d / 2, nkv = a.pages.p.nkv;
+  const int side = warp >= heads, h = blockIdx.y * heads + warp - side * heads;   // 0: K, 1: V
+  pdl_wait();
+  pdl_trigger();
+  // Sequence b's blocks of positions are numbered from 2 b + floor(q_start[b] / 16): a count
+  // known without a scan, at the price of numbers that have none.
+  const BatchView& b = a.batch;
+  auto start = [&](int s) { return 2ll * s + b.q_start[s] / kScaleBlock; };
+  const int seq = warp_count_le(b.n_seqs - 1, start, blockIdx.x);
+  const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], len = b.seq_len[seq];
+  const bool in_order = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1;
+  const long long before = (long long)len - (q1 - q0);
+  if ((!in_order || before < 0) && threadIdx.x == 0) *a.status = OOS_EBATCH;
+  if (!in_order || (long long)blockIdx.x < start(seq)) return;
+  const long long p0 = (max(before, 0ll) / kScaleBlock + (blockIdx.x - start(seq))) * kScaleBlock;
+  if (p0 >= len || q0 == q1) return;
+  const long long slot = page_slot(b, a.pages.p.page_size, a.pages.p.n_pages, seq, (int)p0);
+  if (slot < 0) {   // the whole block of threads
+    if (threadIdx.x == 0) *a.status = OOS_EBATCH;
+    return;
+  }
+  const int lo = (int)max(0ll, before - p0), hi = (int)min((long long)kScaleBlock, len - p0);   // its rows of this step
+  const long long t0 = q0 + (p0 - before);   // token of the block's first position
+  const int sub = lane % LANES, group = lane / LANES;
+  float y[PASSES][NC][2][VEC];
+  {
+    const T* in = (const T*)a.in[side];
+    Vec<T, VEC> x[PASSES][NC][2];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int r = p * ROWS + group;
+      const T* row = in + (t0 + r) * a.stride[side] + (long long)h * d;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int m = (c * LANES + sub) * VEC;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          x[p][c][half] = Vec<T, VEC>();
+          if (h < nkv && r >= lo && r < hi && m < d2) x[p][c][half] = *reinterpret_cast<const Vec<T, VEC>*>(row + half * d2 + m);
+        }
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) y[p][c][half][i] = to_f32(x[p][c][half].v[i]);
+  }
+  uint8_t* scale = (side ? a.pages.v_scale : a.pages.k_scale) + slot / kScaleBlock * nkv + h;
+  const bool begun = lo == 0 && before <= p0;
+  int old = kScaleLow;
+  if (!begun && h < nkv) old = scale_exp(*scale);
+  if (a.positions) {
+    for (int i = threadIdx.x; i < (hi - lo) * d2; i += blockDim.x) {
+      const int r = lo + i / d2, m = i % d2;
+      float c, s;
+      turn(rope.f[m], a.positions[t0 + r], c, s);
+      s_turn[r][m] = make_float2(c, s);
+    }
+    __syncthreads();
+  }
+  if (h >= nkv) return;
+  if (side == 0) {
+    const T* gain = (const T*)a.gain;
+    float g[NC][2][VEC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {   // element by element: a gain may start anywhere
+          const int m = (c * LANES + sub) * VEC;
+          g[c][half][i] = gain && m < d2 ? to_f32(gain[half * d2 + m + i]) : 1.f;
+        }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int r = p * ROWS + group;
+      if (p * ROWS + ROWS <= lo || p * ROWS >= hi) continue;   // warp-uniform
+      float f = 1.f;
+      if (gain) {
+        float ss = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) ss += y[p][c][0][i] * y[p][c][0][i] + y[p][c][1][i] * y[p][c][1][i];
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        f = rsqrtf(ss / (float)d + a.eps);
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const int m = (c * LANES + sub) * VEC + i;
+          float lo_ = y[p][c][0][i], hi_ = y[p][c][1][i];
+          if (gain) {
+            lo_ = lo_ * f * g[c][0][i];
+            hi_ = hi_ * f * g[c][1][i];
+          }
+          if (a.positions && m < d2 && r >= lo && r < hi) {
+            const float2 cs = s_turn[r][m];
+            const float turned = lo_ * cs.x - hi_ * cs.y;
+            hi_ = hi_ * cs.x + lo_ * cs.y;
+            lo_ = turned;
+          }
+          y[p][c][0][i] = lo_;
+          y[p][c][1][i] = hi_;
+        }
+    }
+  }
+  float amax = 0.f;   // of what is finite in the block's rows
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float v = fabsf(y[p][c][half][i]);
+          const int r = p * ROWS + group;
+          if (v < INFINITY && r >= lo && r < hi) amax = fmaxf(amax, v);
+        }
+  amax = warp_max(amax);
+  const int e = max(old, needed_exp(amax));
+  uint8_t* codes = (side ? a.pages.p.v : a.pages.p.k) + slot * nkv * d + (long long)h * d;
+  if (!begun && e > old) {   // the positions from before, and what lies behind the step's
+    for (int r = 0; r < kScaleBlock; ++r) {
+      if (r >= lo && r < hi) continue;
+      uint8_t* row = codes + (long long)r * nkv * d;
+      if constexpr (VEC >= 4) {
+        if (4 * lane < d) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(row + 4 * lane);
+          *w = rescale_codes4(*w, old - e);
+        }
+      } else {
+        for (int c = lane; c < d; c += 32) row[c] = (uint8_t)rescale_codes4(row[c], old - e);
+      }
+    }
+  }
+  const float inv = pow2f(-e);
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int r = p * ROWS + group;
+    if (r < lo || r >= hi) continue;
+    uint8_t* row = codes + (long long)r * nkv * d;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int m = (c * LANES + sub) * VEC;
+        if (m >= d2) continue;
+        float v[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = finite_or_nan(y[p][c][half][i]) * inv;
+        if constexpr (VEC == 1) {
+          row[half * d2 + m] = (uint8_t)f32x2_e4m3(v[0], 0.f);
+        } else {
+          Vec<uint16_t, VEC / 2> w;
+#pragma unroll
+          for (int i = 0; i < VEC / 2; ++i) w.v[i] = f32x2_e4m3(v[2 * i], v[2 * i + 1]);
+          *reinterpret_cast<Vec<uint16_t, VEC / 2>*>(row + half * d2 + m) = w;
+        }
+      }
+  }
+  if (lane == 0 && (begun || e > old)) *scale = (uint8_t)(e + 127);
+}
+
+template <typename T, int VEC, int LANES, int NC>
+static cudaError_t launch_append8_of(const Append8Args& a, const RopeTurns& rope, cudaStream_t st) {
+  const int heads = std::min(a.pages.p.nkv, kApMaxHeads);
+  const long long blocks = 2ll * a.batch.n_seqs + a.batch.n_tokens / kScaleBlock;
+  const dim3 grid((unsigned)blocks, (unsigned)((a.pages.p.nkv + heads - 1) / heads));
+  return launch(true, k_append8<T, VEC, LANES, NC>, grid, dim3(64 * heads), 0, st, a, rope);
+}
+
+template <typename T>
+static cudaError_t launch_append8(const Append8Args& a, const RopeTurns& rope, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const int d2 = a.pages.p.d / 2;
+  bool wide = d2 % V == 0 && ((uintptr_t)a.pages.p.k | (uintptr_t)a.pages.p.v) % V == 0;
+  for (int s = 0; s < 2; ++s) wide = wide && (uintptr_t)a.in[s] % 16 == 0 && a.stride[s] * sizeof(T) % 16 == 0;
+  if (wide) {
+    const int chunks = d2 / V;
+    if (chunks <= 4) return launch_append8_of<T, V, 4, 1>(a, rope, st);
+    if (chunks <= 8) return launch_append8_of<T, V, 8, 1>(a, rope, st);
+    return launch_append8_of<T, V, 16, 1>(a, rope, st);
+  }
+  if (d2 > 32) return launch_append8_of<T, 1, 32, 2>(a, rope, st);
+  return launch_append8_of<T, 1, 32, 1>(a, rope, st);
+}
+
+}  // namespace oos
+
+using namespace oos;
+
+extern "C" int oos_paged_append8(const oos_paged_cache8* cache, const oos_batch* batch, int32_t dtype, const void* k,
+                                 int64_t k_stride, const void* v, int64_t v_stride, const void* k_norm, float eps,
+                                 const oos_rope_config* rope, const int32_t* positions, int32_t* out_status,
+                                 void* stream) {
+  if (!cache || !batch || !pages8_ok(cache) || !batch_ok(batch) || !out_status || !(eps >= 0.f)) return OOS_EINVAL;
+  if (!dtype_ok(dtype) || !head_dim_ok(cache->head_dim)) return OOS_EUNSUPPORTED;
+  if (rope && !rope_ok(rope)) return OOS_EINVAL;
+  if (batch->n_tokens == 0) return OOS_OK;
+  const long long w = (long long)cache->n_kv_heads * cache->head_dim;
+  if (!k || !v || k_stride < w || v_stride < w || w > (1 << 24)) return OOS_EINVAL;
+  if (cache->n_kv_heads > 65535 || 2ll * batch->n_seqs + batch->n_tokens / kScaleBlock > 0x7fffffffll) return OOS_EINVAL;
+  if (rope && !positions) return OOS_EINVAL;
+  Append8Args a = {};
+  a.pages = view_of(*cache);
+  a.batch = view_of(*batch);
+  a.in[0] = k;
+  a.in[1] = v;
+  a.stride[0] = k_stride;
+  a.stride[1] = v_stride;
+  a.gain = k_norm;
+  a.positions = rope ? positions : nullptr;
+  a.eps = eps;
+  a.status = out_status;
+  static const RopeTurns none = {};
+  const RopeTurns& turns = rope ? rope_turns(*rope, cache->head_dim) : none;
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = dtype == OOS_DTYPE_F32    ? launch_append8<float>(a, turns, st)
+                        : dtype == OOS_DTYPE_BF16 ? launch_append8<__nv_bfloat16>(a, turns, st)
+                                                  : launch_append8<__half>(a, turns, st);
+  return e == cudaSuccess ? OOS_OK : OOS_ECUDA;
+}
