@@ -150,7 +150,17 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   const int G = nq / c.n_kv_heads;
   const long long rows = (long long)b.n_tokens * G;
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, kMaxKeys);
-  p->tc = !own8 && c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
+  p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
+  if (p->tc && own8) {
+    p->few = true;
+    p->sequence = {false, 0, 1};
+    p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
+    p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->pages.sms, sms) : PrefixPlan{0, 0, 0.0};
+    const int parts = p->prefix.splits + (p->pages.part ? p->pages.splits : 0);
+    p->ml_off = 0;
+    p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
+    return true;
+  }
   if (p->tc) {
     // Tiles of 16 rows that read their sequence's pages again (from L2), or tiles of up to
     // 256 that are mostly empty.  Trees of 4 rows a node, 8 kv heads, 2048 prefix keys: 24
@@ -290,9 +300,10 @@ static int attend(int dtype, int n_q_heads, const void* q, int64_t q_stride, con
     a.own_part = p.few && p.pages.part;
     e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, c.dtype, st) : cudaSuccess;
     if (e == cudaSuccess)
-      e = p.few ? launch_pages_tc(a, p.pages, dtype, c.dtype, st)
-                : launch_sequence_tc(a, p.sequence, dtype, c.dtype, st);
-    if (p.few) a.s_splits = p.pages.part;   // for the join
+      e = !p.few  ? launch_sequence_tc(a, p.sequence, dtype, c.dtype, st)
+          : own8  ? launch_pages8_tc(a, p.pages, dtype, st)
+                  : launch_pages_tc(a, p.pages, dtype, c.dtype, st);
+    if (p.few && !own8) a.s_splits = p.pages.part;   // for the join
     if (e == cudaSuccess && (p.few ? p.pages.part : a.s_splits > 1)) {
       const dim3 grid((unsigned)(((long long)batch->n_tokens * n_q_heads + 7) / 8));
       e = dtype == OOS_DTYPE_BF16 ? launch(true, k_attn_join_parts<__nv_bfloat16>, grid, dim3(256), 0, st, a)
