@@ -551,10 +551,17 @@ int oos_paged_append8(const oos_paged_cache8* cache, const oos_batch* batch, int
  *   prefix_dtype   of prefix_k / prefix_v: dtype's, or OOS_DTYPE_F16 with dtype BF16
  *                  (OOS_EUNSUPPORTED otherwise; not looked at when prefix_len is 0)
  * With 16-bit types and heads of 128, codes start on 16-byte boundaries (OOS_EINVAL
- * otherwise), scores are of q with an error of at most 2^-22 of a row's largest |q| in
- * every element, and the weights that own positions' v is multiplied by are rounded to
- * 2^-16, or to bf16 (2^-8, a sixteenth of what a code is rounded by) where sequences have
- * many rows; a row is divided by the sum of the rounded weights.  Everything else is as
+ * otherwise), and what is rounded depends on whether sequences have few rows (token,
+ * head of a group): 32 on average, up to 64 in small batches.
+ *   few    scores are of q with an error of at most 2^-22 of a row's largest |q| in
+ *          every element; the weights that own positions' v is multiplied by are rounded
+ *          to 2^-16
+ *   many   scores are of q with an error of at most 2^-17 of the largest; weights are
+ *          rounded to bf16 (2^-8, a sixteenth of what a code is rounded by) for BF16, and
+ *          for F16 to 2^-11, below 2^-21 of the row's largest weight times scale to 2^-32
+ *          of that, where a scale below 2^-60 counts as 2^-60 and its codes are rounded
+ *          to binary16 in the unit of that
+ * Where weights are bf16 a row is divided by their rounded sum.  Everything else is as
  * in oos_shared_prefix_attention, its status and refusals included. */
 size_t oos_shared_prefix_attention8_workspace_bytes(int32_t dtype, int32_t n_q_heads, int32_t prefix_len,
                                                     const oos_paged_cache8* cache, const oos_batch* batch);

@@ -152,11 +152,13 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, kMaxKeys);
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc && own8) {
-    p->few = true;
+    p->few = rows <= 32ll * b.n_seqs || (rows <= 64ll * b.n_seqs && rows / 16 * c.n_kv_heads <= 4ll * sms);
     p->sequence = {false, 0, 1};
-    p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
-    p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->pages.sms, sms) : PrefixPlan{0, 0, 0.0};
-    const int parts = p->prefix.splits + (p->pages.part ? p->pages.splits : 0);
+    if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
+    else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, 0, most_keys, sms);   // the prefix apart
+    p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->few ? p->pages.sms : 0, sms) : PrefixPlan{0, 0, 0.0};
+    const int own = p->few ? (p->pages.part ? p->pages.splits : 0) : p->sequence.splits > 1 ? p->sequence.splits : 0;
+    const int parts = p->prefix.splits + own;
     p->ml_off = 0;
     p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
     return true;
@@ -300,9 +302,9 @@ static int attend(int dtype, int n_q_heads, const void* q, int64_t q_stride, con
     a.own_part = p.few && p.pages.part;
     e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, c.dtype, st) : cudaSuccess;
     if (e == cudaSuccess)
-      e = !p.few  ? launch_sequence_tc(a, p.sequence, dtype, c.dtype, st)
-          : own8  ? launch_pages8_tc(a, p.pages, dtype, st)
-                  : launch_pages_tc(a, p.pages, dtype, c.dtype, st);
+      e = !p.few ? (own8 ? launch_sequence8_tc(a, p.sequence, dtype, st) : launch_sequence_tc(a, p.sequence, dtype, c.dtype, st))
+                 : own8 ? launch_pages8_tc(a, p.pages, dtype, st)
+                        : launch_pages_tc(a, p.pages, dtype, c.dtype, st);
     if (p.few && !own8) a.s_splits = p.pages.part;   // for the join
     if (e == cudaSuccess && (p.few ? p.pages.part : a.s_splits > 1)) {
       const dim3 grid((unsigned)(((long long)batch->n_tokens * n_q_heads + 7) / 8));

@@ -198,5 +198,6 @@ cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtyp
 // the same over 8-bit pages, queries of dtype; several splits leave parts
 PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
 cudaError_t launch_pages8_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, cudaStream_t st);
+cudaError_t launch_sequence8_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, cudaStream_t st);   // a plan without the prefix
 
 }  // namespace oos

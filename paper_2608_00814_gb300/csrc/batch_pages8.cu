@@ -30,7 +30,7 @@
 
 #include "attn.cuh"
 #include "batch_attn.cuh"
-#include "pages8.cuh"
+#include "codes8.cuh"
 
 namespace oos {
 
@@ -74,15 +74,6 @@ OOS_DEV void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-OOS_DEV uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// bytes 0 and 2 (1 and 3) of a word of codes as bf16 of 2^-120 the value
-OOS_DEV uint32_t even_codes(uint32_t w) { return ((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u); }
-OOS_DEV uint32_t odd_codes(uint32_t w) { return (w & 0x80008000u) | ((w >> 4) & 0x07f007f0u); }
-
 template <typename TQ, int NT>
 __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(const __grid_constant__ BatchAttnArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
