@@ -154,7 +154,7 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   if (p->tc && own8) {
     p->few = rows <= 32ll * b.n_seqs || (rows <= 64ll * b.n_seqs && rows / 16 * c.n_kv_heads <= 4ll * sms);
     p->sequence = {false, 0, 1};
-    if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, most_keys, sms);
+    if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, prefix_len > 0, most_keys, sms);
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, 0, most_keys, sms);   // the prefix apart
     p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->few ? p->pages.sms : 0, sms) : PrefixPlan{0, 0, 0.0};
     const int own = p->few ? (p->pages.part ? p->pages.splits : 0) : p->sequence.splits > 1 ? p->sequence.splits : 0;

@@ -180,6 +180,7 @@ struct PagesPlan {
   int tiles, splits;
   int sms;         // that its blocks fill at once, about
   bool part;       // leaves a part for a join
+  int extra;       // of 8-bit pages: blocks for ranges beyond a tile's first, all kv heads' apart
 };
 struct SequencePlan {
   bool takes_prefix;   // in the same kernel
@@ -196,7 +197,7 @@ cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dt
 cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, int kv_dtype, cudaStream_t st);
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
 // the same over 8-bit pages, queries of dtype; several splits leave parts
-PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);
+PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, bool prefix, long long most_keys, int n_sms);
 cudaError_t launch_pages8_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, cudaStream_t st);
 cudaError_t launch_sequence8_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, cudaStream_t st);   // a plan without the prefix
 

@@ -4,25 +4,37 @@
 //
 // A block owns a tile of 8 or 16 rows (token, head of one kv head's group) of one sequence
 // and a range of its keys, dealt to its four warps 32 at a time: two blocks of 16 positions,
-// each with one scale.  Every warp has a ring of its own, filled by 16-byte asynchronous
-// copies (a key row is 128 bytes: 8 lanes), and no block barrier before the end.  Places and
-// scales of 16 such pairs are looked up at once, a lane each.
+// each with one scale.  Every warp has a ring of its own, filled by TMA, a block of positions
+// a copy (what lies behind the sequence's end comes along and is masked), and no block
+// barrier before the end.  Places and scales of 16 such pairs are looked up at once by the
+// lane that issues the copy.
 //
-// S^T = K Q^T (keys on the product's 16 rows) takes the codes of K as they are, on
-// mma.sync m16n8k32 of e4m3: a row of q, scaled by a power of two so that its largest element
-// lies in [2^7, 2^8), is the sum of two (bf16) or three (binary16) e4m3 parts, each the
-// rounded rest of the one before times 2^5.  That holds 8 (11) bits exactly, down to elements
-// of 2^-8 (2^-6) of the largest, and smaller ones to 2^-22 of it.  The parts' products cost what one of
-// 16-bit K would, whose conversion would cost more than both.  Sums of e4m3 products are
-// full fp32 (truncated) on this chip.
+// Where sequences are cut into ranges, how many each gets follows from all lengths, which
+// are on the device: every warp adds them up and finds its block's place, so that ranges
+// are about as long everywhere.
 //
-// O^T = V^T P^T takes V as bf16: a transposed load of pairs of codes brings the same two of
-// d for neighbouring keys, and the bytes of either d, moved apart, are bf16 numbers of
-// 2^-120 the value.  The missing 2^120 and V's scale are powers of two in the weights, which
-// are two bf16 halves (2^-16).  The bits of a NaN code would read as 480, so V's rows are also
-// multiplied by zero as e4m3 (a product of 32 of d a step, half of what Q K^T takes); where
-// that says so, the columns are set to NaN in the rows that see the key.  A NaN that a row does
-// not see is multiplied as 480 by 0.
+// Both products are mma.sync m16n8k16 of binary16 with keys or d on the 16 rows, and take
+// the codes through the conversion of two at a time, which is exact: two operations of half
+// rate for four codes (moving bits takes eleven issue slots; products of e4m3 itself are as
+// fast, but leave the sum of each to four additions).
+//
+// S^T = K Q^T.  A word of codes is four neighbours of d, so a step's 16 of d are taken in the
+// order 4 (lane % 4) + 0, 1 and + 2, 3 on both sides.  bf16 rows of q are scaled by a power of
+// two that brings their largest element to [1, 2): exact down to 2^-14 of that, smaller ones
+// to 2^-25 of it.
+//
+// O^T = V^T P^T.  A transposed load of pairs of codes brings the same two of d for
+// neighbouring keys; a byte permutation puts either d's together.  V's scale 2^e is in the
+// weights, 2^(s + e - M + 7) with M a maximum of s + e, rounded to binary16: to 2^-11, below
+// 2^-21 of the row's largest weight times scale to 2^-32 of that.  The sum of the weights is of
+// 2^(s - m), with a maximum of its own, so that scales far apart cost it nothing.  Maxima move
+// when a score passes them by 2^8, which one comparison a score finds; only then lanes meet.
+//
+// A NaN in V reaches every row that sees its key.  Where some rows do not, in the units
+// behind a row's own position, such codes are taken out and their columns set.
+//
+// 64 requests of up to 4000 keys and 2048 shared ones, 32 heads over 8: 58 us, 4.0 TB/s, and
+// the longest requests' blocks end last; 6 requests of up to 64000, 64 heads: 70 us, 5.5 TB/s.
 #include <math.h>
 
 #include <algorithm>
@@ -40,8 +52,8 @@ constexpr int kP8Half = kScaleBlock * kP8D;            // bytes of K (or V) of a
 constexpr int kP8Stage = 4 * kP8Half;                  // both blocks, K and V
 constexpr int p8_stages(int nt) { return nt == 1 ? 2 : 3; }
 constexpr int p8_blocks(int nt) { return nt == 1 ? 3 : 2; }   // per SM
-constexpr int p8_smem(int nt) { return p8_stages(nt) * kP8Warps * kP8Stage; }
-static_assert(kP8Warps * 16 * kPartLd * 4 <= p8_smem(1), "staged rows over the rings");
+constexpr int p8_smem(int nt) { return p8_stages(nt) * kP8Warps * kP8Stage + 1024; }   // + alignment slack
+static_assert(kP8Warps * 16 * kPartLd * 4 <= p8_smem(1) - 1024, "staged rows over the rings");
 constexpr int kP8Unit = kP8Warps * kP8Keys;            // keys of a block's round
 constexpr int kP8MaxParts = 32;                        // of a row, the prefix's among them
 
@@ -62,32 +74,114 @@ OOS_DEV uint32_t turned8x8(uint32_t v) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-OOS_DEV void mma_e4m3(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+OOS_DEV void mma_half(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-OOS_DEV void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+OOS_DEV uint32_t half2_of(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+struct Pages8Args {
+  CUtensorMap kmap, vmap;   // codes [n_pages][page_size][nkv][128], as pairs
+  BatchAttnArgs a;
+  int extra;                // blocks beside one for each tile of rows, to share among long sequences
+};
+
+// The tile and range of keys of block i: every sequence's keys are cut into as many ranges
+// (at most `most_ranges`) of equal numbers of rounds as `extra` blocks more allow.  The whole warp;
+// false: no such block.
+OOS_DEV bool balanced_tile(const Pages8Args& p, int i, int tile_rows, int most_ranges, TileRows* t, int* split, int* ranges) {
+  const BatchAttnArgs& a = p.a;
+  const BatchView& b = a.batch;
+  const int lane = threadIdx.x & 31;
+  const long long most = min((long long)b.max_pages * a.pages.page_size, (long long)kMaxKeys);
+  struct Seq {
+    int q0, n, len, tiles, units;
+  };
+  auto look = [&](int seq, bool report) {
+    Seq s = {0, 0, 0, 0, 0};
+    if (seq >= b.n_seqs) return s;
+    const int q0 = b.q_start[seq], q1 = b.q_start[seq + 1], given = b.seq_len[seq], len = max(0, given);
+    const bool in_order = q0 >= 0 && q1 <= b.n_tokens && q0 <= q1, ok = in_order && (!a.parent || q1 - q0 <= kMaxTreeRows);
+    if (report && (!ok || given < q1 - q0 || len > most)) *a.status = in_order && !ok ? OOS_ETREE : OOS_EBATCH;
+    if (!ok) return s;
+    s.q0 = q0;
+    s.n = q1 - q0;
+    s.len = (int)min((long long)len, most);
+    s.tiles = (s.n * a.group + tile_rows - 1) / tile_rows;   // n_tokens * nq stays below 2^26
+    s.units = (s.len + kP8Unit - 1) / kP8Unit;
+    return s;
+  };
+  const bool report = i == 0 && blockIdx.y == 0 && threadIdx.x < 32;
+  long long total = 0;
+  for (int s0 = 0; s0 < b.n_seqs; s0 += 32) {
+    const Seq s = look(s0 + lane, report);
+    total += (long long)s.tiles * s.units;
+  }
+#pragma unroll
+  for (int x = 16; x; x /= 2) total += __shfl_xor_sync(0xffffffffu, total, x);
+  const int target = (int)max(2ll, min((total + p.extra - 1) / p.extra, (long long)kMaxKeys));   // rounds of a range
+  int base = 0;
+  for (int s0 = 0; s0 < b.n_seqs; s0 += 32) {
+    const Seq s = look(s0 + lane, false);
+    const int r = max(1, min(most_ranges, (s.units + target - 1) / target));
+    int upto = s.tiles * r;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, x);
+      if (lane >= x) upto += v;
+    }
+    const uint32_t above = __ballot_sync(0xffffffffu, base + upto > i);
+    if (above == 0) {
+      base += __shfl_sync(0xffffffffu, upto, 31);
+      continue;
+    }
+    const int src = __ffs(above) - 1;
+    t->seq = s0 + src;
+    t->q0 = __shfl_sync(0xffffffffu, s.q0, src);
+    t->n = __shfl_sync(0xffffffffu, s.n, src);
+    t->len = __shfl_sync(0xffffffffu, s.len, src);
+    t->first = t->len - t->n;
+    *ranges = __shfl_sync(0xffffffffu, r, src);
+    const int at = i - base - __shfl_sync(0xffffffffu, upto - s.tiles * r, src);
+    *split = at % *ranges;
+    t->r0 = at / *ranges * tile_rows;
+    t->rows = min(tile_rows, t->n * a.group - t->r0);
+    return true;
+  }
+  return false;
+}
+
 template <typename TQ, int NT>
-__global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(const __grid_constant__ BatchAttnArgs a) {
-  extern __shared__ __align__(128) unsigned char smem[];
+__global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(const __grid_constant__ Pages8Args p) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   constexpr int ROWS = 8 * NT, STAGES = p8_stages(NT);
-  constexpr int PARTS = std::is_same<TQ, __nv_bfloat16>::value ? 2 : 3;
   __shared__ TreeScratch s_tree;
+  __shared__ uint64_t s_full[kP8Warps][STAGES];
+  const BatchAttnArgs& a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = blockIdx.y, S = a.s_splits, split = blockIdx.x % S;
+  const int g = blockIdx.y, S = a.s_splits;
+  uint64_t* full = s_full[warp];
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) mbar_init(full + i, 2);   // a lane for each block of positions
+    mbar_fence_init();
+    tma_prefetch_desc(&p.kmap);
+    tma_prefetch_desc(&p.vmap);
+  }
+  __syncwarp();
   // behind the prefix's kernel, which has waited for what the caller wrote before it
   // triggers, only the join waits
   if (a.p_splits == 0) pdl_wait();
   pdl_trigger();
   TileRows t;
-  if (!sequence_tile(a, blockIdx.x / S, ROWS, &t)) {
+  int split = 0, ranges = 1;
+  if (!(S > 1 ? balanced_tile(p, blockIdx.x, ROWS, S, &t, &split, &ranges) : sequence_tile(a, blockIdx.x, ROWS, &t))) {
     if (blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();       // the grid must not end before the one it follows
     return;
   }
@@ -95,64 +189,67 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
   if (a.parent) anc = tree_sets(a, t.q0, t.n, &s_tree);
   const int last = (t.r0 + t.rows - 1) / a.group;
   const int n_keys = anc ? t.len : max(0, min(t.len, t.first + last + 1));
-  // as many ranges as have two rounds each; the others are empty
-  const int units = (n_keys + kP8Unit - 1) / kP8Unit, ranges = max(1, min(S, units / 2));
-  const int k0 = split < ranges ? (int)((long long)units * split / ranges) * kP8Unit : n_keys;
-  const int k1 = split < ranges ? min(n_keys, (int)((long long)units * (split + 1) / ranges) * kP8Unit) : n_keys;
+  const int units = (n_keys + kP8Unit - 1) / kP8Unit;
+  const int k0 = (int)((long long)units * split / ranges) * kP8Unit;
+  const int k1 = min(n_keys, (int)((long long)units * (split + 1) / ranges) * kP8Unit);
   const int n_rounds = max(0, k1 - k0 + kP8Unit - 1) / kP8Unit;
 
   // ---- places and scales of 16 rounds: lane 2 r + h has block h of round r
   const int* table = a.batch.table + (size_t)t.seq * a.batch.max_pages;
   const int per_page = a.pages.page_size / kScaleBlock;
-  auto look_up = [&](int round, long long& block, int& sk, int& sv) {   // block of the pool, -1: none
+  struct Place {
+    int page, slot;   // of the first position; page -1: none
+    int scales;       // K's byte and V's, and above them 1
+  };
+  auto look_up = [&](int round) {
+    Place at = {-1, 0, 127 | 127 << 8};
     const int key = k0 + (round + (lane >> 1)) * kP8Unit + warp * kP8Keys + (lane & 1) * kScaleBlock;
-    block = -1;
-    sk = sv = 127;
     if (round + (lane >> 1) < n_rounds && key < k1) {   // no further than the table
       const int b = key / kScaleBlock, col = b / per_page, page = __ldg(table + col);
       if (page >= 0 && page < a.pages.n_pages) {
-        block = (long long)page * per_page + (b - col * per_page);
-        sk = __ldg(a.k_scale + block * a.pages.nkv + g);
-        sv = __ldg(a.v_scale + block * a.pages.nkv + g);
+        const int in_page = b - col * per_page;
+        const long long block = ((long long)page * per_page + in_page) * a.pages.nkv + g;
+        at = {page, in_page * kScaleBlock, 1 << 16 | __ldg(a.k_scale + block) | __ldg(a.v_scale + block) << 8};
       } else {
         *a.status = OOS_EBATCH;
       }
     }
+    return at;
   };
-  long long block = -1, block2 = -1;   // of this batch of 16 rounds and the next
-  int sk = 127, sv = 127, sk2 = 127, sv2 = 127;
-  look_up(0, block, sk, sv);
+  Place place = look_up(0), place2 = {-1, 0, 0};   // of this batch of 16 rounds and the next
 
   // ---- copies: this warp's two blocks of a round into its own ring
-  const uint32_t ring = smem_addr(smem) + warp * (STAGES * kP8Stage);
-  const long long key_bytes = (long long)a.pages.nkv * kP8D;
-  const uint8_t* kg = a.pages.k + (long long)g * kP8D + (lane & 7) * 16;
-  const uint8_t* vg = a.pages.v + (long long)g * kP8D + (lane & 7) * 16;
-  auto copy = [&](int round, int place, long long from) {   // from: a lane's block of the batch
-    if (round < n_rounds) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const long long at = __shfl_sync(0xffffffffu, from, 2 * (round & 15) + h);
-        const int n = k1 - (k0 + round * kP8Unit + warp * kP8Keys + h * kScaleBlock);   // keys from its first on
-        const uint32_t dst = ring + place * kP8Stage + h * 2 * kP8Half;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = 4 * i + (lane >> 3);
-          const bool ok = at >= 0 && key < n;
-          const long long off = ok ? (at * kScaleBlock + key) * key_bytes : 0;
-          const uint32_t o = key * kP8D + (((lane & 7) ^ (key & 7)) << 4);
-          cp_async16(dst + o, kg + off, ok);
-          cp_async16(dst + kP8Half + o, vg + off, ok);
-        }
+  unsigned char* ring = smem + warp * (STAGES * kP8Stage);
+  const uint64_t policy = t.n * a.group <= ROWS ? policy_evict_first() : policy_evict_last();   // read once, or by other tiles too
+  auto copy = [&](int round, int stage, const Place& at) {
+    if (round < n_rounds && (lane >> 1) == (round & 15)) {
+      if (at.page >= 0) {
+        unsigned char* dst = ring + stage * kP8Stage + (lane & 1) * 2 * kP8Half;
+        mbar_arrive_expect_tx(full + stage, 2 * kP8Half);
+        tma_load_4d(dst, &p.kmap, full + stage, 0, g, at.slot, at.page, policy);
+        tma_load_4d(dst + kP8Half, &p.vmap, full + stage, 0, g, at.slot, at.page, policy);
+      } else {
+        mbar_arrive(full + stage);
       }
     }
-    cp_async_commit();
+  };
+  auto landed = [&](int stage, uint32_t parity) {   // a wait of at most kWaitLimitNs
+    const uint32_t addr = smem_addr(full + stage);
+    if (mbar_test_sleep(addr, parity, 20000u)) return true;
+    const unsigned long long t0 = globaltimer();
+    while (!mbar_test_sleep(addr, parity, 20000u)) {
+      if (globaltimer() - t0 > kWaitLimitNs) {
+        *a.status = OOS_ETIMEOUT;
+        return false;
+      }
+    }
+    return true;
   };
 #pragma unroll
-  for (int c = 0; c < STAGES - 1; ++c) copy(c, c, block);
+  for (int c = 0; c < STAGES - 1; ++c) copy(c, c, place);
 
-  // ---- the queries' e4m3 parts as B fragments: row lane / 4 of each 8, d = 32 kk + 16 e + 4 (lane % 4) ..
-  uint32_t qf[PARTS][NT][4][2];
+  // ---- the queries as B fragments: row lane / 4 of each 8, d = 16 k + 4 (lane % 4) ..
+  uint32_t qf[NT][8][2];
   float sc[NT][2];   // a column's two rows of this thread: 8 n + 2 (lane & 3) + e
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -161,41 +258,29 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
     const TQ* q = (const TQ*)a.q + (long long)(t.q0 + (on ? row / a.group : 0)) * a.q_stride +
                   (g * a.group + row % a.group) * kP8D + (lane & 3) * 4;
     const bool wide = (((uintptr_t)a.q | (uintptr_t)(a.q_stride * 2)) & 7) == 0;
-    float x[4][2][4], mx = 0.f;
+    float x[8][4], mx = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
+    for (int k = 0; k < 8; ++k) {
+      Vec<TQ, 4> v = {};
+      if (on && wide) v = *reinterpret_cast<const Vec<TQ, 4>*>(q + 16 * k);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        Vec<TQ, 4> v = {};
-        if (on && wide) v = *reinterpret_cast<const Vec<TQ, 4>*>(q + 32 * kk + 16 * e);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (on && !wide) v.v[i] = q[32 * kk + 16 * e + i];
-          x[kk][e][i] = on ? finite_or_nan(to_f32(v.v[i])) : 0.f;
-          mx = fmaxf(mx, fabsf(x[kk][e][i]));
-        }
+      for (int i = 0; i < 4; ++i) {
+        if (on && !wide) v.v[i] = q[16 * k + i];
+        x[k][i] = on ? finite_or_nan(to_f32(v.v[i])) : 0.f;
+        mx = fmaxf(mx, fabsf(x[k][i]));
       }
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    const int e2 = row_exponent(mx);
+    }
+    int e2 = 0;
+    if constexpr (std::is_same<TQ, __nv_bfloat16>::value) {
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      e2 = row_exponent(mx);
+    }
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float (&y)[4] = x[kk][e];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = y[i] * exp2i(-e2) * 128.f;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-          const uint16_t w0 = f32x2_e4m3(y[0], y[1]), w1 = f32x2_e4m3(y[2], y[3]);
-          qf[p][n][kk][e] = (uint32_t)w0 | (uint32_t)w1 << 16;
-          const float2 z0 = e4m3x2_f32(w0), z1 = e4m3x2_f32(w1);
-          y[0] = (y[0] - z0.x) * 32.f;
-          y[1] = (y[1] - z0.y) * 32.f;
-          y[2] = (y[2] - z1.x) * 32.f;
-          y[3] = (y[3] - z1.y) * 32.f;
-        }
-      }
+    for (int k = 0; k < 8; ++k) {
+      qf[n][k][0] = half2_of(x[k][0] * exp2i(-e2), x[k][1] * exp2i(-e2));
+      qf[n][k][1] = half2_of(x[k][2] * exp2i(-e2), x[k][3] * exp2i(-e2));
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) sc[n][e] = a.scale_log2 * __shfl_sync(0xffffffffu, exp2i(e2), ((lane & 3) * 2 + e) * 4);
   }
@@ -214,7 +299,8 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
     }
   const int tok_lo = t.r0 / a.group, tok_hi = last;
 
-  float o[8][NT][4], m[NT][2], l[NT][2];
+  // O of rows 8 n + 2 (lane & 3) + e is in 2^(mo - 7), l in 2^m
+  float o[8][NT][4], m[NT][2], mo[NT][2], l[NT][2];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -223,78 +309,74 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
       for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      m[n][e] = -INFINITY;
+      m[n][e] = mo[n][e] = -INFINITY;
       l[n][e] = 0.f;
     }
   }
   // ldmatrix rows of this lane: 8 keys of a 16-byte column, the 16 keys of one column and of the next
   const uint32_t l_key = lane & 15, l_col = lane >> 4;
 
+  int at = 0;   // of the ring
+  uint32_t parity = 0;
 #pragma unroll 1
   for (int c = 0; c < n_rounds; ++c) {
-    cp_async_wait<STAGES - 2>();
-    __syncwarp();
-    if ((c & 15) == 8) look_up((c & ~15) + 16, block2, sk2, sv2);
+    if (!__all_sync(0xffffffffu, landed(at, parity))) {
+      for (int i = 1; i < STAGES; ++i) {   // the copies on their way end before the block does
+        if (++at == STAGES) at = 0, parity ^= 1;
+        if (c + i < n_rounds) landed(at, parity);
+      }
+      break;
+    }
+    if ((c & 15) == 8) place2 = look_up((c & ~15) + 16);
     {
       const int ahead = c + STAGES - 1;
-      copy(ahead, ahead % STAGES, (ahead ^ c) & 16 ? block2 : block);
+      copy(ahead, at == 0 ? STAGES - 1 : at - 1, (ahead ^ c) & 16 ? place2 : place);
     }
     const int key0 = k0 + c * kP8Unit + warp * kP8Keys;
-    const uint32_t buf = ring + (c % STAGES) * kP8Stage;
+    const uint32_t buf = smem_addr(ring) + at * kP8Stage;
+    if (++at == STAGES) at = 0, parity ^= 1;
     int there[2], ek[2], ev[2];   // keys of either block that are there, from its first on; its exponents
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int from = 2 * (c & 15) + h;
-      there[h] = __shfl_sync(0xffffffffu, block, from) >= 0 ? max(0, min(kScaleBlock, k1 - key0 - h * kScaleBlock)) : 0;
-      ek[h] = scale_exp(__shfl_sync(0xffffffffu, sk, from));
-      ev[h] = scale_exp(__shfl_sync(0xffffffffu, sv, from));
+      const int w = __shfl_sync(0xffffffffu, place.scales, 2 * (c & 15) + h);
+      there[h] = w >> 16 ? max(0, min(kScaleBlock, k1 - key0 - h * kScaleBlock)) : 0;
+      ek[h] = scale_exp(w & 255);
+      ev[h] = scale_exp(w >> 8 & 255);
     }
-    if ((c & 15) == 15) {
-      block = block2;
-      sk = sk2;
-      sv = sv2;
-    }
+    if ((c & 15) == 15) place = place2;
+    __syncwarp();
     // nothing there, or no row that sees the first key (warp-uniform)
     if (there[0] + there[1] == 0 || (!anc && key0 > t.first + tok_hi)) continue;
     float s[2][NT][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float acc[PARTS][NT][4];
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[p][n][e] = 0.f;
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        uint32_t k4[4];
-        ldm4(buf + h * 2 * kP8Half + l_key * kP8D + (((2 * kk + l_col) ^ (l_key & 7)) << 4), k4);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) mma_e4m3(acc[p][n], k4, qf[p][n][kk][0], qf[p][n][kk][1]);
-      }
-      const float pk = pow2f(ek[h] - 7);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = acc[PARTS - 1][n][e];
+        for (int e = 0; e < 4; ++e) s[h][n][e] = 0.f;
 #pragma unroll
-          for (int p = PARTS - 2; p >= 0; --p) v = fmaf(v, 0x1p-5f, acc[p][n][e]);
-          s[h][n][e] = v * (sc[n][e & 1] * pk);
+      for (int kk = 0; kk < 4; ++kk) {
+        uint32_t k4[4];   // keys 0-7 and 8-15 of 16 of d, and of the next 16
+        ldm4(buf + h * 2 * kP8Half + l_key * kP8D + (((2 * kk + l_col) ^ (l_key & 7)) << 4), k4);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t a0 = e4m3x2_half2((uint16_t)k4[2 * j]), a2 = e4m3x2_half2((uint16_t)(k4[2 * j] >> 16));
+          const uint32_t a1 = e4m3x2_half2((uint16_t)k4[2 * j + 1]), a3 = e4m3x2_half2((uint16_t)(k4[2 * j + 1] >> 16));
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_half(s[h][n], a0, a1, a2, a3, qf[n][2 * kk + j][0], qf[n][2 * kk + j][1]);
         }
+      }
+      const float pk = pow2f(ek[h]);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[h][n][e] *= sc[n][e & 1] * pk;
     }
     // keys that each of this thread's rows sees
     const int seen = t.first - key0;   // those before it are committed
-    const bool full = there[0] + there[1] == kP8Keys && (anc ? seen : seen + tok_lo + 1) >= kP8Keys;
+    const bool whole = there[0] + there[1] == kP8Keys && (anc ? seen : seen + tok_lo + 1) >= kP8Keys;
     uint32_t bits[NT][2];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) bits[n][e] = ~0u;
-    if (!full) {
+    if (!whole) {
       const uint32_t here = ((1u << there[0]) - 1) | ((1u << there[1]) - 1) << 16;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -316,88 +398,83 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
           }
         }
     }
-    bool move = false;
-    float mn[NT][2];
+    const float fv[2] = {(float)ev[0], (float)ev[1]};
+    bool move = false;   // a NaN is above any maximum
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float mx = max_nan(max_nan(s[0][n][e], s[0][n][2 + e]), max_nan(s[1][n][e], s[1][n][2 + e]));
-        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-        mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-        mn[n][e] = !(mx <= m[n][e] + 8.f) ? mx : m[n][e];   // a NaN moves it, and stays
-        move = move || mn[n][e] != m[n][e];
-      }
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          move = move || !(max_nan(s[h][n][e], s[h][n][2 + e]) <= fminf(m[n][e] + 8.f, mo[n][e] + 8.f - fv[h]));
     if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float f = m[n][e] == mn[n][e] ? 1.f : m[n][e] == -INFINITY ? 0.f : exp2f(m[n][e] - mn[n][e]);
-          l[n][e] *= f;
+          const float top[2] = {max_nan(s[0][n][e], s[0][n][2 + e]), max_nan(s[1][n][e], s[1][n][2 + e])};
+          float mx = max_nan(top[0], top[1]), mv = max_nan(top[0] + fv[0], top[1] + fv[1]);
+#pragma unroll
+          for (int x = 4; x < 32; x *= 2) {
+            mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+            mv = max_nan(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+          }
+          auto moved = [](float& was, float to) {   // and the factor of what stands in 2^was
+            if (to <= was + 8.f) return 1.f;
+            const float f = was == -INFINITY ? 0.f : exp2f(was - to);
+            was = to;
+            return f;
+          };
+          l[n][e] *= moved(m[n][e], mx);
+          const float f = moved(mo[n][e], mv);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             o[i][n][e] *= f;
             o[i][n][2 + e] *= f;
           }
-          m[n][e] = mn[n][e];
         }
     }
+    // without a finite score yet every score is -inf, and gives 0
+    uint32_t pf[2][NT][2];   // as B fragments: 8 x 8 of (key, row) turned to (row, key)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (there[h] == 0) continue;
-      // the weights' factor 2^(120 + ev), as far as it fits beside their 2^8; the rest goes to V
-      const int ew = min(ev[h], -1);
-      const float pv = pow2f(120 + ew);
-      uint32_t pf[NT][2], pl[NT][2];   // two bf16 halves, as B fragments: 8 x 8 of (key, row) turned to (row, key)
+    for (int n = 0; n < NT; ++n) {
+      const float by[2] = {m[n][0] == -INFINITY ? 0.f : -m[n][0], m[n][1] == -INFINITY ? 0.f : -m[n][1]};
+      const float byo[2] = {mo[n][0] == -INFINITY ? 0.f : kHalfBias - mo[n][0], mo[n][1] == -INFINITY ? 0.f : kHalfBias - mo[n][1]};
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        // without a finite score yet every score is -inf, and gives 0
-        const float neg[2] = {m[n][0] == -INFINITY ? 0.f : -m[n][0], m[n][1] == -INFINITY ? 0.f : -m[n][1]};
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          float p0 = ex2_approx(s[h][n][2 * u] + neg[0]), p1 = ex2_approx(s[h][n][2 * u + 1] + neg[1]);
-          l[n][0] += p0;
-          l[n][1] += p1;
-          p0 *= pv;
-          p1 *= pv;
-          const uint32_t hi = __byte_perm(__float_as_uint(p0), __float_as_uint(p1), 0x7632);   // cut off
-          const __nv_bfloat162 lo = __floats2bfloat162_rn(p0 - bf16_lo(hi), p1 - bf16_hi(hi));
-          pf[n][u] = turned8x8(hi);
-          pl[n][u] = turned8x8(*reinterpret_cast<const uint32_t*>(&lo));
+          const float s0 = s[h][n][2 * u], s1 = s[h][n][2 * u + 1];
+          l[n][0] += ex2_approx(s0 + by[0]);
+          l[n][1] += ex2_approx(s1 + by[1]);
+          pf[h][n][u] = turned8x8(half2_of(ex2_approx(s0 + (byo[0] + fv[h])), ex2_approx(s1 + (byo[1] + fv[h]))));
         }
-      }
+    }
+    auto add_block = [&](int h, const uint32_t (&pf)[NT][2], auto some_masked) {
       const uint32_t vbuf = buf + (2 * h + 1) * kP8Half;
-      const bool large = ev[h] > ew;   // warp-uniform, as all of a block's is
-      const uint32_t fv = (uint32_t)(ev[h] - ew + 127) << 7, fv2 = fv | fv << 16;
+      uint32_t nan = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t w[4];   // keys 0-7 and 8-15 of 16 columns, and of the next 16
         ldm4_trans(vbuf + l_key * kP8D + (((2 * i + l_col) ^ (l_key & 7)) << 4), w);
+        if (some_masked) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint32_t v[4] = {even_codes(w[2 * j]), odd_codes(w[2 * j]), even_codes(w[2 * j + 1]), odd_codes(w[2 * j + 1])};
-          if (large) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) v[x] = mul_bf16x2(v[x], fv2);
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            mma_bf16(o[2 * i + j][n], v[0], v[1], v[2], v[3], pf[n][0], pf[n][1]);
-            mma_bf16(o[2 * i + j][n], v[0], v[1], v[2], v[3], pl[n][0], pl[n][1]);
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t is = ((w[x] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            nan |= is;
+            w[x] &= ~((is >> 7) * 0xffu);
           }
         }
-      }
-      // a NaN in V: rows of zero times it
-      float nan[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        uint32_t v4[4];
-        ldm4(vbuf + l_key * kP8D + (((2 * kk + l_col) ^ (l_key & 7)) << 4), v4);
-        mma_e4m3(nan, v4, 0u, 0u);
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t lo = __byte_perm(w[2 * j], 0, 0x3120), hi = __byte_perm(w[2 * j + 1], 0, 0x3120);   // even of d, odd of d
+          const uint32_t a0 = e4m3x2_half2((uint16_t)lo), a1 = e4m3x2_half2((uint16_t)(lo >> 16));
+          const uint32_t a2 = e4m3x2_half2((uint16_t)hi), a3 = e4m3x2_half2((uint16_t)(hi >> 16));
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_half(o[2 * i + j][n], a0, a1, a2, a3, pf[n][0], pf[n][1]);
+        }
       }
-      if (__any_sync(0xffffffffu, nan[0] != 0.f || nan[2] != 0.f)) {   // a column for all
+      if (some_masked && __any_sync(0xffffffffu, nan != 0)) {   // the columns' rows that see the key
 #pragma unroll 1
         for (int key = 0; key < kScaleBlock; ++key)
 #pragma unroll
@@ -414,11 +491,26 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
                   if ((bits[n][e] >> (16 * h + key)) & 1) o[i][n][2 * u + e] = __int_as_float(0x7fffffff);
             }
       }
+    };
+    if (whole) {
+      add_block(0, pf[0], std::false_type());
+      add_block(1, pf[1], std::false_type());
+    } else {
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        uint32_t now[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) now[n][u] = h ? pf[1][n][u] : pf[0][n][u];
+        if ((h ? there[1] : there[0]) > 0) add_block(h, now, std::true_type());
+      }
     }
   }
-  cp_async_wait<0>();
   __syncthreads();
   // ---- join: O rows with (m, l), staged over the rings, of every warp, and the prefix's parts
+  constexpr float kUnbias = 0x1p-7f;
+  static_assert(kHalfBias == 7.f, "the weights' power");
   float* stage = reinterpret_cast<float*>(smem);   // [warp][row][kPartLd]
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -427,9 +519,10 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
 #pragma unroll
       for (int x = 4; x < 32; x *= 2) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], x);
       float* row = stage + (warp * ROWS + 8 * n + (lane & 3) * 2 + e) * kPartLd;
+      const float f = mo[n][e] == -INFINITY ? 1.f : exp2f(mo[n][e] - m[n][e]);   // O in 2^m, too
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<float2*>(row + 16 * i + 2 * (lane >> 2)) = make_float2(o[i][n][e], o[i][n][2 + e]);
+        *reinterpret_cast<float2*>(row + 16 * i + 2 * (lane >> 2)) = make_float2(o[i][n][e] * kUnbias * f, o[i][n][2 + e] * kUnbias * f);
       if (lane < 4) *reinterpret_cast<float2*>(row + kP8D) = make_float2(m[n][e], l[n][e]);
     }
   const int pre_parts = a.own_part ? 0 : a.p_splits;
@@ -477,6 +570,8 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
       // the maximum over the parts passes a NaN by, the sum does not: stored with a maximum of
       // -inf it would read as a part without keys
       if (lane == 0) *reinterpret_cast<float2*>(to + kP8D) = make_float2(den == den ? top : den, den);
+      // parts that the sequence has no ranges for
+      if (split == ranges - 1 && lane < S - ranges) *reinterpret_cast<float2*>(to + (1 + lane) * part_step + kP8D) = make_float2(-INFINITY, 0.f);
     } else {
       store_row<TQ>(a, g, t.q0, t.r0 + r, weighted_mean(acc, den));
     }
@@ -484,31 +579,48 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_pages8(co
   if (a.own_part && blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();   // a kernel that waits for this one counts on the prefix's
 }
 
-PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms) {
-  PagesPlan p;
+PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, bool prefix, long long most_keys, int n_sms) {
+  PagesPlan p = {};
+  const int per_sm = p8_blocks(rows <= 8ll * n_seqs ? 1 : 2);
   p.tile_rows = rows <= 8ll * n_seqs ? 8 : 16;
   p.tiles = (int)(n_seqs + rows / p.tile_rows);
   const long long live = std::max((long long)n_seqs, (rows + p.tile_rows - 1) / p.tile_rows) * nkv;
-  // ranges enough for eight blocks an SM, each with two rounds at least
-  const long long want = 8ll * n_sms / live;
-  p.splits = (int)std::max(1ll, std::min({want, most_keys / (2 * kP8Unit), (long long)kP8MaxParts - kMaxPrefixParts}));
-  p.sms = (int)std::min<long long>(n_sms, (live * p.splits + p8_blocks(p.tile_rows / 8) - 1) / p8_blocks(p.tile_rows / 8));
+  // Ranges, each with two rounds at least, for as many blocks as the chip holds: a block's
+  // beginning and end cost as much as a few rounds (6 requests of up to 64000 keys, 8 kv heads:
+  // 70 us, for twice as many 76, three times 87).
+  const long long most = (long long)per_sm * n_sms, ranges = std::min<long long>(kP8MaxParts - (prefix ? kMaxPrefixParts : 0), most_keys / (2 * kP8Unit));
+  p.extra = (int)((most - live) / nkv);
+  p.splits = p.extra > 0 ? (int)std::max(1ll, ranges) : 1;
+  p.sms = (int)std::min<long long>(n_sms, ((p.splits > 1 ? most : live) + per_sm - 1) / per_sm);
   p.part = p.splits > 1;
   return p;
 }
 
 template <typename TQ, int NT>
-static cudaError_t launch_pages8_of(const BatchAttnArgs& a, const PagesPlan& p, cudaStream_t st) {
+static cudaError_t launch_pages8_of(const Pages8Args& a, const PagesPlan& p, cudaStream_t st) {
   static std::atomic<uint64_t> ready{0};
   const cudaError_t e = kernel_ready(ready, (const void*)k_attn_pages8<TQ, NT>, p8_smem(NT));
   if (e != cudaSuccess) return e;
-  return launch(true, k_attn_pages8<TQ, NT>, dim3((unsigned)(p.tiles * p.splits), a.pages.nkv), dim3(kP8Warps * 32), p8_smem(NT), st, a);
+  const dim3 grid((unsigned)(p.tiles + (p.splits > 1 ? p.extra : 0)), a.a.pages.nkv);
+  return launch(true, k_attn_pages8<TQ, NT>, grid, dim3(kP8Warps * 32), p8_smem(NT), st, a);
 }
 
 cudaError_t launch_pages8_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, cudaStream_t st) {
+  Pages8Args args;
+  memset(&args, 0, sizeof(args));
+  args.a = a;
+  args.extra = p.extra;
+  // two codes an element of the copy
+  const uint64_t row = (uint64_t)a.pages.nkv * kP8D;
+  const uint64_t dims[4] = {kP8D / 2, (uint64_t)a.pages.nkv, (uint64_t)a.pages.page_size, (uint64_t)a.pages.n_pages};
+  const uint64_t strides[3] = {kP8D, row, row * a.pages.page_size};
+  const uint32_t box[4] = {kP8D / 2, 1, (uint32_t)kScaleBlock, 1};
+  if (!encode_bf16_map(&args.kmap, a.pages.k, 4, dims, strides, box, false) ||
+      !encode_bf16_map(&args.vmap, a.pages.v, 4, dims, strides, box, false))
+    return cudaErrorInvalidValue;
   if (dtype == OOS_DTYPE_BF16)
-    return p.tile_rows == 8 ? launch_pages8_of<__nv_bfloat16, 1>(a, p, st) : launch_pages8_of<__nv_bfloat16, 2>(a, p, st);
-  return p.tile_rows == 8 ? launch_pages8_of<__half, 1>(a, p, st) : launch_pages8_of<__half, 2>(a, p, st);
+    return p.tile_rows == 8 ? launch_pages8_of<__nv_bfloat16, 1>(args, p, st) : launch_pages8_of<__nv_bfloat16, 2>(args, p, st);
+  return p.tile_rows == 8 ? launch_pages8_of<__half, 1>(args, p, st) : launch_pages8_of<__half, 2>(args, p, st);
 }
 
 }  // namespace oos

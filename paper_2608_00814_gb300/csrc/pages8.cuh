@@ -38,9 +38,13 @@ OOS_DEV int needed_exp(float amax) {
 struct E4M3 {
   uint8_t c;
 };
-OOS_DEV float2 e4m3x2_f32(uint16_t two) {   // the low byte first
+OOS_DEV uint32_t e4m3x2_half2(uint16_t two) {   // the low byte first
   uint32_t h;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
+  return h;
+}
+OOS_DEV float2 e4m3x2_f32(uint16_t two) {
+  const uint32_t h = e4m3x2_half2(two);
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 OOS_DEV float to_f32(E4M3 v) { return e4m3x2_f32(v.c).x; }

@@ -91,35 +91,43 @@ def check_append(step, before, after, y, tol, what=""):
 
 
 def attention(step, q, pk, pv, cache, scale, parent=None):
-    """(out, weights times |v|, largest sum |q k| scale, (what q's parts may leave of a score, largest |v|)).  q is
-    taken in parts of four bits, which leave up to 2^-22 of its largest element in each; where sequences have more
-    than 32 rows (token, head of a group) on average up to 2^-17: e4m3's steps are 2^-9, half of one is left, and
-    the largest element stands at 2^7 or more."""
+    """(out, weights times |v|, largest sum |q k| scale, bounds of the tensor-core kernels), the bounds being
+      - what is left out of q, of a score: 2^-25 of a row's largest |q| in each element (binary16 after a scaling to
+        [1, 2)), and 2^-17 where sequences have more than 32 rows (token, head of a group) on average: parts of four
+        bits in e4m3, whose steps are 2^-9, so that half of one is left, of a largest element of 2^7 or more
+      - what weights are rounded by: to bf16 with a bf16 prefix, or bf16 queries in sequences of many rows, to
+        binary16 otherwise
+      - what is left of a term below binary16's normal numbers: 2^-25 where the row's largest weight times scale stands
+        at 2^7 or more, 2^-32 of that for each key, and of codes up to 448
+      - the largest |v|."""
     kp, vp = values(cache.k, cache.k_scale), values(cache.v, cache.v_scale)
     out, mag, size = R.attention(step, q, pk, pv, kp, vp, scale, parent)
-    seen = [kp[step.where(b, s)] for b, n in enumerate(step.lens) if step.counts[b] for s in range(max(n, 0))]
-    top = max([float(k.abs().sum(-1).max()) for k in seen] or [0.0])
-    fine = q[:step.n].double().abs()
-    fine = fine.max() * (2.0 ** -17 if fine.shape[0] * (q.shape[1] // cache.k.shape[-2]) > 32 * len(step.counts) else 2.0 ** -22) if fine.numel() else 0
-    v = [vp[step.where(b, s)].abs().max() for b, n in enumerate(step.lens) if step.counts[b] for s in range(max(n, 0))]
-    v += [pv.double().abs().max().cpu()] if pv.numel() else []
-    return out, mag, size, (float(fine) * top * scale, float(max(v)) if v else 0.0)
+    slots = [step.where(b, s) for b, n in enumerate(step.lens) if step.counts[b] for s in range(max(n, 0))]
+    many = step.n * (q.shape[1] // cache.k.shape[-2]) > 32 * len(step.counts)
+    most = max([float(kp[s].abs().sum(-1).max()) for s in slots] or [0.0])
+    fine = float(q[:step.n].double().abs().max()) if step.n else 0.0
+    weights = torch.bfloat16 if pk.dtype is torch.bfloat16 or (many and q.dtype is torch.bfloat16) else torch.float16
+    es = exps(cache.v_scale)
+    unit = max([float(es[p, s // BLOCK].max()) for p, s in slots] or [LOW])
+    v = [float(vp[s].abs().max()) for s in slots] + ([float(pv.double().abs().max())] if pv.numel() else [])
+    return out, mag, size, (fine * most * scale * 2.0 ** (-17 if many else -25), R.U[weights], 2.0 ** (unit - 32) * 448, max(v or [0.0]))
 
 
-def check_attention(got, ref, mag, size, tops, keys, what=""):
+def check_attention(got, ref, mag, size, bounds, keys, what=""):
     """The bound of batch_ref.check_attention -- half a step of the output; a score's (d + 3) half steps of fp32 of
     sum |q k| and the exponential's 4, each twice; the sums' half steps per key -- and, for the 16-bit types: the
-    weights' rounding to bf16 (2^-8, beside one part's to binary16 or two bf16 halves), the tensor cores' truncated
-    sums, and what q's parts leave of a score, twice that of a weight.  All of these are relative to a weight.  One
-    below 2^-126 of the row's largest is no normal fp32 number and counts as 0, so that its own error is all of it:
-    2^-126 |v| for each key at most, which shows where v is 0 at every key of weight.  An output of binary16 whose
-    bound reaches past the type's largest number may be infinite."""
-    got, t, (qk, v) = got.double().cpu(), got.dtype, tops
+    weights' rounding, the tensor cores' truncated sums, what is left out of q, of a score and so twice of a weight, and
+    of small terms.  All but the last are relative to a weight.  One below 2^-126 of the row's largest is no normal fp32
+    number and counts as 0, so that its own error is all of it: 2^-126 |v| for each key at most, which shows where v is 0
+    at every key of weight.  An output of binary16 whose bound reaches past the type's largest number may be infinite."""
+    got, t, (left, weights, term, v) = got.double().cpu(), got.dtype, bounds
     d = got.shape[-1]
     rel = 2 * ((d + 3) * R.F32 * size + 4 * R.F32) + (4 * keys + 64) * R.F32
+    off = 2.0 ** -126 * keys * v
     if t is not torch.float32:
-        rel += R.U[torch.bfloat16] + d * R.F32 * 2 * size + 2 * qk
-    tol = R.U[t] * ref.abs().clamp(min=torch.finfo(t).tiny) + rel * mag + 2.0 ** -126 * keys * v
+        rel += weights + d * R.F32 * 2 * size + 2 * left
+        off += keys * term
+    tol = R.U[t] * ref.abs().clamp(min=torch.finfo(t).tiny) + rel * mag + off
     past = torch.isinf(got) & (got.sign() * ref + tol > 65504) if t is torch.float16 else torch.zeros_like(got, dtype=torch.bool)
     bad = ~((got - ref).abs() <= tol) & ~past
     assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), float((got - ref).abs().max()))
