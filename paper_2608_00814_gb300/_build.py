@@ -19,7 +19,7 @@ LIB = os.path.join(OUT_DIR, "liboos.so")
 LIB_TIMELINE = os.path.join(OUT_DIR, "liboos_timeline.so")
 UNITS = ["oos_api.cu", "small.cu", "gemm.cu", "attn.cu", "prefill.cu", "f32.cu", "noalloc.cu", "hint.cu", "decode.cu",
          "heads.cu", "heads8.cu", "pages.cu", "batch_attn.cu", "batch_rows8.cu", "batch_tiles.cu", "batch_pages.cu",
-         "batch_pages8.cu", "batch_tiles8.cu"]
+         "batch_pages8.cu", "batch_stream8.cu", "batch_tiles8.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -120,6 +120,9 @@ struct BatchAttnPlan {
   PrefixPlan prefix;
   PagesPlan pages;
   SequencePlan sequence;
+  bool stream;         // 8-bit pages, few rows: equal shares of all keys
+  StreamPlan shares;
+  size_t shares_off;
   int p_rt, rt, p_tiles, p_splits, s_tiles, s_splits;   // CUDA cores: rows of a tile over the prefix, over own keys
   size_t ml_off, bytes;
 };
@@ -154,13 +157,19 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   if (p->tc && own8) {
     p->few = rows <= 32ll * b.n_seqs || (rows <= 64ll * b.n_seqs && rows / 16 * c.n_kv_heads <= 4ll * sms);
     p->sequence = {false, 0, 1};
-    if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, prefix_len > 0, most_keys, sms);
+    if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, sms);
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, 0, most_keys, sms);   // the prefix apart
     p->prefix = prefix_len > 0 ? plan_prefix_tc(rows, c.n_kv_heads, prefix_len, p->few ? p->pages.sms : 0, sms) : PrefixPlan{0, 0, 0.0};
     const int own = p->few ? (p->pages.part ? p->pages.splits : 0) : p->sequence.splits > 1 ? p->sequence.splits : 0;
     const int parts = p->prefix.splits + own;
     p->ml_off = 0;
     p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
+    p->stream = p->few && b.n_seqs <= kStreamSeqs && most_keys > 256;
+    if (p->stream) {
+      p->shares = plan_stream8(rows, b.n_seqs, b.n_tokens, c.n_kv_heads, p->prefix, sms);
+      p->shares_off = p->bytes;
+      p->bytes += p->shares.bytes;
+    }
     return true;
   }
   if (p->tc) {
@@ -301,7 +310,8 @@ static int attend(int dtype, int n_q_heads, const void* q, int64_t q_stride, con
     a.s_splits = p.few ? p.pages.splits : p.sequence.splits;
     a.own_part = p.few && p.pages.part;
     e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, c.dtype, st) : cudaSuccess;
-    if (e == cudaSuccess)
+    if (e == cudaSuccess && p.stream) e = launch_stream8(a, p.shares, (uint8_t*)workspace + p.shares_off, dtype, st);
+    else if (e == cudaSuccess)
       e = !p.few ? (own8 ? launch_sequence8_tc(a, p.sequence, dtype, st) : launch_sequence_tc(a, p.sequence, dtype, c.dtype, st))
                  : own8 ? launch_pages8_tc(a, p.pages, dtype, st)
                         : launch_pages_tc(a, p.pages, dtype, c.dtype, st);

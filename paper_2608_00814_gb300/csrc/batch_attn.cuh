@@ -180,7 +180,6 @@ struct PagesPlan {
   int tiles, splits;
   int sms;         // that its blocks fill at once, about
   bool part;       // leaves a part for a join
-  int extra;       // of 8-bit pages: blocks for ranges beyond a tile's first, all kv heads' apart
 };
 struct SequencePlan {
   bool takes_prefix;   // in the same kernel
@@ -197,8 +196,18 @@ cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dt
 cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, int kv_dtype, cudaStream_t st);
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
 // the same over 8-bit pages, queries of dtype; several splits leave parts
-PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, bool prefix, long long most_keys, int n_sms);
+PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, int n_sms);
 cudaError_t launch_pages8_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, cudaStream_t st);
+// the same, an equal share of all keys for every warp, and the join; n_seqs <= kStreamSeqs
+constexpr int kStreamSeqs = 256;
+struct StreamPlan {
+  int tile_rows, blocks, places;
+  int late;                   // units that the prefix's blocks keep a block behind them from
+  int early;                  // blocks that they do not
+  size_t tokens_off, bytes;   // of its workspace
+};
+StreamPlan plan_stream8(long long rows, int n_seqs, int n_tokens, int nkv, const PrefixPlan& prefix, int n_sms);
+cudaError_t launch_stream8(const BatchAttnArgs& a, const StreamPlan& p, void* workspace, int dtype, cudaStream_t st);
 cudaError_t launch_sequence8_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, cudaStream_t st);   // a plan without the prefix
 
 }  // namespace oos
