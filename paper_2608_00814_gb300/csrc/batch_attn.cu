@@ -155,7 +155,11 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   const long long most_keys = std::min<long long>((long long)b.max_pages * c.page_size, kMaxKeys);
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc && own8) {
-    p->few = rows <= 32ll * b.n_seqs || (rows <= 64ll * b.n_seqs && rows / 16 * c.n_kv_heads <= 4ll * sms);
+    // Tiles of 16 rows that each read their sequence's pages, or tiles of up to 256.  Trees of
+    // 4 rows a node, 8 kv heads, 2048 prefix keys: 36 rows on average over up to 400 keys 33 us
+    // against 48 (16 sequences) and 77 against 111 (64), over up to 2000 118 against 209 (64); 72
+    // rows 47 against 49 (16), 138 against 125 (64), 227 against 216 (64, up to 2000 keys).
+    p->few = rows <= 64ll * b.n_seqs;
     p->sequence = {false, 0, 1};
     if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, sms);
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, 0, most_keys, sms);   // the prefix apart
@@ -164,7 +168,11 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     const int parts = p->prefix.splits + own;
     p->ml_off = 0;
     p->bytes = ((size_t)parts * b.n_tokens * nq * kPartLd * 4 + 255) / 256 * 256;
-    p->stream = p->few && b.n_seqs <= kStreamSeqs && most_keys > 256;
+    // Equal shares of all keys, or a block for each tile that joins its rows itself.  One token
+    // of 4 rows, 8 kv heads, 2048 prefix keys: 1 sequence of up to 800 keys 15.6 us against 12.5,
+    // 16 of them 19.6 against 16.2, 20 of up to 4000 27 against 43; 64 of up to 100 23.0 against
+    // 22.6, of up to 300 22.0 against 24.9; 250 of up to 300 45 against 51.
+    p->stream = p->few && b.n_seqs <= kStreamSeqs && (most_keys > 1024 || (most_keys > 256 && (long long)b.n_seqs * c.n_kv_heads >= 3ll * sms));
     if (p->stream) {
       p->shares = plan_stream8(rows, b.n_seqs, b.n_tokens, c.n_kv_heads, p->prefix, sms);
       p->shares_off = p->bytes;

@@ -93,7 +93,7 @@ def check_append(step, before, after, y, tol, what=""):
 def attention(step, q, pk, pv, cache, scale, parent=None):
     """(out, weights times |v|, largest sum |q k| scale, bounds of the tensor-core kernels), the bounds being
       - what is left out of q, of a score: 2^-25 of a row's largest |q| in each element (binary16 after a scaling to
-        [1, 2)), and 2^-17 where sequences have more than 32 rows (token, head of a group) on average: parts of four
+        [1, 2)), and 2^-17 where sequences have more than 64 rows (token, head of a group) on average: parts of four
         bits in e4m3, whose steps are 2^-9, so that half of one is left, of a largest element of 2^7 or more
       - what weights are rounded by: to bf16 with a bf16 prefix, or bf16 queries in sequences of many rows, to
         binary16 otherwise
@@ -103,7 +103,7 @@ def attention(step, q, pk, pv, cache, scale, parent=None):
     kp, vp = values(cache.k, cache.k_scale), values(cache.v, cache.v_scale)
     out, mag, size = R.attention(step, q, pk, pv, kp, vp, scale, parent)
     slots = [step.where(b, s) for b, n in enumerate(step.lens) if step.counts[b] for s in range(max(n, 0))]
-    many = step.n * (q.shape[1] // cache.k.shape[-2]) > 32 * len(step.counts)
+    many = step.n * (q.shape[1] // cache.k.shape[-2]) > 64 * len(step.counts)
     most = max([float(kp[s].abs().sum(-1).max()) for s in slots] or [0.0])
     fine = float(q[:step.n].double().abs().max()) if step.n else 0.0
     weights = torch.bfloat16 if pk.dtype is torch.bfloat16 or (many and q.dtype is torch.bfloat16) else torch.float16
