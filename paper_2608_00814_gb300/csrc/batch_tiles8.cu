@@ -10,20 +10,20 @@
 // to the scores, a factor for each 16 columns of the thread's row.
 //
 // P.V: kind::f16.  Four warps convert V, each two blocks of 16 positions of a tile, from a
-// ring of copies of the codes.  Bytes are moved apart into 16-bit numbers, which leaves four
-// neighbours in the order 0, 2, 1, 3; O's columns are put right when they are staged.  A NaN
-// code's bits would come out as 480 and are set to NaN by the thread that finds them.
-//   bf16 queries: weights and V are bf16.  Moved bytes are 2^-120 of the value, a product with
-//     2^(120 + scale) does the rest, exactly.
-//   binary16 queries: weights and V are binary16, 2^-11 instead of 2^-8.  Moved bytes are
-//     2^-8 of the code, and the scale 2^e is a factor of the weight, 2^(score + e - m + 7) with
-//     m a maximum of score + e: what a row adds up is rounded to 2^-11, below 2^-21 of its
-//     largest term (448 2^e times the weight) to 2^-32 of that.  The sum of the weights is
+// ring of copies of the codes.
+//   bf16 queries: weights and V are bf16.  Bytes are moved apart into numbers of 2^-120 of the
+//     value, a product with 2^(120 + scale) does the rest, exactly.  It leaves the codes of four
+//     neighbours in the order 0, 2, 1, 3; O's columns are put right when they are staged.  A NaN
+//     code's bits would come out as 480 and are set to NaN by the thread that finds them.
+//   binary16 queries: weights and V are binary16, 2^-11 instead of 2^-8.  The codes go through
+//     the conversion of two at a time, and the scale 2^e is a factor of the weight,
+//     2^(score + e - m + 7) with m a maximum of score + e: what a row adds up is rounded to
+//     2^-11, below 2^-21 of its largest term (448 2^e times the weight) to 2^-32 of that.  The sum of the weights is
 //     taken of unrounded ones without the scales, which a weight's own has to leave some of in
 //     32 bits: an e below -60 counts as -60, and the codes are made smaller instead.
 //
 // 13 prompts of up to 300 tokens, 40 heads over 8, 1000 shared and up to 1800 own keys in
-// binary16: 252 us; 16 trees of up to 64 nodes, 32 heads, 2048 shared and up to 464 own keys
+// binary16: 243 us; 16 trees of up to 64 nodes, 32 heads, 2048 shared and up to 464 own keys
 // in bf16: 71 (batch_pages8.cu's kernel: 783 and 128).  The shared keys are the other kernel's.
 #include <math.h>
 
@@ -31,7 +31,7 @@
 #include <type_traits>
 
 #include "batch_tiles.cuh"
-#include "codes8.cuh"
+#include "pages8.cuh"
 
 namespace oos {
 
@@ -52,6 +52,22 @@ struct T8 {
   static_assert(kTlStaged <= kOffExp, "staged rows and their weights over the rings and queries");
   static_assert(kSmem <= 227 * 1024, "shared memory per block");
 };
+
+OOS_DEV uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// bytes 0 and 2 (1 and 3) of a word of codes as bf16 of 2^-120 the value
+OOS_DEV uint32_t even_codes(uint32_t w) { return ((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u); }
+OOS_DEV uint32_t odd_codes(uint32_t w) { return (w & 0x80008000u) | ((w >> 4) & 0x07f007f0u); }
+OOS_DEV uint32_t mul_half2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// 2^e as binary16, e <= 0; 0 below 2^-24
+OOS_DEV uint32_t half_power(int e) { return e >= -14 ? (uint32_t)(min(e, 0) + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u; }
 
 // Instruction descriptor of tcgen05.mma.kind::f8f6f4 with e4m3 A and B (format 0 in both
 // fields), fp32 D, both K-major
@@ -314,8 +330,8 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
           uint32_t x[8], top = 0;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            x[2 * j] = F16 ? even_codes_half(w[j]) : mul_bf16x2(even_codes(w[j]), f1 | f1 << 16);
-            x[2 * j + 1] = F16 ? odd_codes_half(w[j]) : mul_bf16x2(odd_codes(w[j]), f1 | f1 << 16);
+            x[2 * j] = F16 ? e4m3x2_half2((uint16_t)w[j]) : mul_bf16x2(even_codes(w[j]), f1 | f1 << 16);
+            x[2 * j + 1] = F16 ? e4m3x2_half2((uint16_t)(w[j] >> 16)) : mul_bf16x2(odd_codes(w[j]), f1 | f1 << 16);
             top |= (w[j] & 0x7f7f7f7fu) + 0x01010101u;
           }
           if (F16 ? ev < kT8LowExp : ev > 7) {
@@ -325,7 +341,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
           if (top & 0x80808080u) {
             nan = true;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < (F16 ? 0 : 4); ++j) {
               const uint32_t is = ((w[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
               if (is & 0x80u) x[2 * j] |= 0x7fffu;
               if (is & 0x800000u) x[2 * j] |= 0x7fff0000u;
@@ -543,7 +559,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
               const __half2 v = __floats2half2_rn(e.x, e.y);
               pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
               sum = (i & 15) == 0 ? e : add2(sum, e);
-              if ((i & 15) == 14) l_new = fmaf(sum.x + sum.y, exp2i(-8 - (int)sve[2 * c + (i >> 4)]), l_new);
+              if ((i & 15) == 14) l_new = fmaf(sum.x + sum.y, exp2i(-(int)sve[2 * c + (i >> 4)]), l_new);
             } else {
               const __nv_bfloat162 v = __floats2bfloat162_rn(e.x, e.y);
               pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
@@ -615,9 +631,11 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
 #pragma unroll
       for (int i = 0; i < 32; i += 4)
         *reinterpret_cast<float4*>(row + 32 * c + i) =
-            have ? make_float4(ov[i], ov[i + 2], ov[i + 1], ov[i + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);   // V's order
+            !have ? make_float4(0.f, 0.f, 0.f, 0.f)
+            : F16 ? make_float4(ov[i], ov[i + 1], ov[i + 2], ov[i + 3])
+                  : make_float4(ov[i], ov[i + 2], ov[i + 1], ov[i + 3]);   // V's order
     }
-    *reinterpret_cast<float2*>(row + kTlD) = make_float2(have ? (F16 ? m + 1.f : m) : -INFINITY, have ? l : 0.f);   // 2^7 and 2^-8
+    *reinterpret_cast<float2*>(row + kTlD) = make_float2(have ? (F16 ? m - kHalfBias : m) : -INFINITY, have ? l : 0.f);
   }
   tc_fence_before();
   __syncthreads();   // rows staged
