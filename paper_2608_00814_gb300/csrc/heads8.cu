@@ -3,8 +3,8 @@
 // A scale belongs to 16 positions of a head, so a warp takes one such block of K or V: its
 // rows (up to 16) are loaded, K's are normed and turned as in heads.cu, all stay in
 // registers as fp32 while their largest magnitude is found, and are rounded once to the
-// scale it needs.  A block of threads holds the heads of the same positions, whose angles
-// it forms once, in shared memory.
+// scale it needs.  A block of threads holds heads of K (or of V) at the same positions, whose
+// angles it forms once, in shared memory.
 //
 // Where the block held positions before, its scale may only grow, as the codes there would
 // gain nothing by a smaller one; when it does, they are read, divided by a power of two and
@@ -20,7 +20,7 @@
 
 namespace oos {
 
-constexpr int kApMaxHeads = 8;   // of a block: a warp for K and one for V each
+constexpr int kApMaxHeads = 8;   // of a block, a warp each
 
 struct Append8Args {
   Pages8View pages;
@@ -36,12 +36,14 @@ struct Append8Args {
 // T: elements of the rows.  A row's half is dealt in chunks of VEC to LANES lanes, NC each;
 // 32 / LANES rows at once.
 template <typename T, int VEC, int LANES, int NC>
-__global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args a, const __grid_constant__ RopeTurns rope) {
+__global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Args a, const __grid_constant__ RopeTurns rope) {
   constexpr int ROWS = 32 / LANES, PASSES = kScaleBlock / ROWS;
-  __shared__ float2 s_turn[kScaleBlock][kMaxHeadDim / 2];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, heads = blockDim.x / 64;
+  // of element m = (c LANES + sub) VEC + i of a half: at (c VEC + i) LANES + sub, so that a
+  // row's lanes read neighbours
+  __shared__ float2 s_turn[kScaleBlock][NC * LANES * VEC];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, heads = blockDim.x / 32;
   const int d = a.pages.p.d, d2 = d / 2, nkv = a.pages.p.nkv;
-  const int side = warp >= heads, h = blockIdx.y * heads + warp - side * heads;   // 0: K, 1: V
+  const int side = blockIdx.y & 1, h = (blockIdx.y >> 1) * heads + warp;   // 0: K, 1: V
   pdl_wait();
   pdl_trigger();
   // Sequence b's blocks of positions are numbered from 2 b + floor(q_start[b] / 16): a count
@@ -95,12 +97,13 @@ __global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args 
   const bool begun = lo == 0 && before <= p0;
   int old = kScaleLow;
   if (!begun && h < nkv) old = scale_exp(*scale);
-  if (a.positions) {
+  if (a.positions && side == 0) {
     for (int i = threadIdx.x; i < (hi - lo) * d2; i += blockDim.x) {
       const int r = lo + i / d2, m = i % d2;
       float c, s;
       turn(rope.f[m], a.positions[t0 + r], c, s);
-      s_turn[r][m] = make_float2(c, s);
+      const int chunk = m / VEC;
+      s_turn[r][(chunk / LANES * VEC + m % VEC) * LANES + chunk % LANES] = make_float2(c, s);
     }
     __syncthreads();
   }
@@ -143,7 +146,7 @@ __global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args 
             hi_ = hi_ * f * g[c][1][i];
           }
           if (a.positions && m < d2 && r >= lo && r < hi) {
-            const float2 cs = s_turn[r][m];
+            const float2 cs = s_turn[r][(c * VEC + i) * LANES + sub];
             const float turned = lo_ * cs.x - hi_ * cs.y;
             hi_ = hi_ * cs.x + lo_ * cs.y;
             lo_ = turned;
@@ -153,7 +156,7 @@ __global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args 
         }
     }
   }
-  float amax = 0.f;   // of what is finite in the block's rows
+  float amax = 0.f;   // of what is finite in the block's rows; the others' are zeros
 #pragma unroll
   for (int p = 0; p < PASSES; ++p)
 #pragma unroll
@@ -161,12 +164,23 @@ __global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args 
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float v = fabsf(y[p][c][half][i]);
-          const int r = p * ROWS + group;
-          if (v < INFINITY && r >= lo && r < hi) amax = fmaxf(amax, v);
-        }
+        for (int i = 0; i < VEC; ++i) amax = fmaxf(amax, fabsf(y[p][c][half][i]));   // passes a NaN by
   amax = warp_max(amax);
+  if (amax == INFINITY) {   // once more, with what is infinite as NaN
+    amax = 0.f;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            y[p][c][half][i] = finite_or_nan(y[p][c][half][i]);
+            amax = fmaxf(amax, fabsf(y[p][c][half][i]));
+          }
+    amax = warp_max(amax);
+  }
   const int e = max(old, needed_exp(amax));
   uint8_t* codes = (side ? a.pages.p.v : a.pages.p.k) + slot * nkv * d + (long long)h * d;
   if (!begun && e > old) {   // the positions from before, and what lies behind the step's
@@ -197,7 +211,7 @@ __global__ void __launch_bounds__(kApMaxHeads * 64) k_append8(const Append8Args 
         if (m >= d2) continue;
         float v[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = finite_or_nan(y[p][c][half][i]) * inv;
+        for (int i = 0; i < VEC; ++i) v[i] = y[p][c][half][i] * inv;
         if constexpr (VEC == 1) {
           row[half * d2 + m] = (uint8_t)f32x2_e4m3(v[0], 0.f);
         } else {
@@ -215,8 +229,8 @@ template <typename T, int VEC, int LANES, int NC>
 static cudaError_t launch_append8_of(const Append8Args& a, const RopeTurns& rope, cudaStream_t st) {
   const int heads = std::min(a.pages.p.nkv, kApMaxHeads);
   const long long blocks = 2ll * a.batch.n_seqs + a.batch.n_tokens / kScaleBlock;
-  const dim3 grid((unsigned)blocks, (unsigned)((a.pages.p.nkv + heads - 1) / heads));
-  return launch(true, k_append8<T, VEC, LANES, NC>, grid, dim3(64 * heads), 0, st, a, rope);
+  const dim3 grid((unsigned)blocks, 2u * (unsigned)((a.pages.p.nkv + heads - 1) / heads));
+  return launch(true, k_append8<T, VEC, LANES, NC>, grid, dim3(32 * heads), 0, st, a, rope);
 }
 
 template <typename T>
