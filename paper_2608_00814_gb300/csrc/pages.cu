@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kMaxMoved) k_compact(const __grid_constant__ C
   }
 }
 
-// 8-bit pages: a warp takes a head, a lane four columns, and the blocks of positions that are
+// 8-bit pages: a warp takes heads of K and V, a lane four columns, and the blocks of positions that are
 // moved into one after the other.  A block's sources lie in it or behind it, so they are as
 // they were when it is its turn.  W: the lane's columns lie side by side, and move as a word.
 template <bool W>
@@ -98,8 +98,6 @@ __global__ void __launch_bounds__(kMaxMoved) k_compact8(const __grid_constant__ 
   pdl_trigger();
   const int moved = look_up_moves(a, blockIdx.x, from, to);
   const int lane = threadIdx.x & 31, warps = kMaxMoved / 32;
-  uint8_t* base = a.l.data[blockIdx.y >> 1][blockIdx.y & 1];
-  uint8_t* scale = a.l.scale[blockIdx.y >> 1][blockIdx.y & 1];
   auto load = [&](const uint8_t* row) {
     if constexpr (W) return 4 * lane < a.d ? *reinterpret_cast<const uint32_t*>(row + 4 * lane) : 0u;
     uint32_t w = 0;
@@ -118,8 +116,10 @@ __global__ void __launch_bounds__(kMaxMoved) k_compact8(const __grid_constant__ 
     }
   };
 #pragma unroll 1
-  for (int h = blockIdx.z * warps + (threadIdx.x >> 5); h < a.nkv; h += warps * gridDim.z) {
-    uint8_t* head = base + (long long)h * a.d;
+  for (int p = blockIdx.z * warps + (threadIdx.x >> 5); p < 2 * a.nkv; p += warps * gridDim.z) {
+    const int h = p >> 1;
+    uint8_t* head = a.l.data[blockIdx.y][p & 1] + (long long)h * a.d;
+    uint8_t* scale = a.l.scale[blockIdx.y][p & 1];
     int j1;
 #pragma unroll 1
     for (int j0 = 0; j0 < moved; j0 = j1) {
@@ -131,21 +131,37 @@ __global__ void __launch_bounds__(kMaxMoved) k_compact8(const __grid_constant__ 
       const long long src = mine ? from[j0 + lane - r0] : block * kScaleBlock + (lane & 15);
       const int e_src = scale_exp(scale[src / kScaleBlock * a.nkv + h]);
       const int own = scale_exp(scale[block * a.nkv + h]);
+      // the first rows that move are on their way while their scales are looked up
+      constexpr int U = 8;
+      uint32_t v[U];
+      auto fetch = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (j0 + i0 + i < j1) v[i] = load(head + from[j0 + i0 + i] * a.row_bytes);
+      };
+      fetch(0);
       const int e = __reduce_max_sync(0xffffffffu, e_src);   // >= own: rows that stay, and lanes without one, bring it
-      uint32_t v[kScaleBlock];
-      uint32_t change = 0;   // rows
+      uint8_t* rows = head + block * kScaleBlock * a.row_bytes;
+#pragma unroll 1
+      for (int i0 = 0; j0 + i0 < j1; i0 += U) {
+        if (i0 > 0) fetch(i0);
 #pragma unroll
-      for (int r = 0; r < kScaleBlock; ++r) {
-        const long long s = __shfl_sync(0xffffffffu, src, r);
-        const int es = __shfl_sync(0xffffffffu, e_src, r);
-        if (s == block * kScaleBlock + r && es == e) continue;
-        change |= 1u << r;
-        v[r] = load(head + s * a.row_bytes);
-        if (es < e) v[r] = rescale_codes4(v[r], es - e);
+        for (int i = 0; i < U; ++i) {
+          const int j = j0 + i0 + i;
+          if (j >= j1) break;
+          const int es = __shfl_sync(0xffffffffu, e_src, r0 + i0 + i);
+          if (es < e) v[i] = rescale_codes4(v[i], es - e);
+          if (es < e || from[j] != to[j]) store(rows + (long long)(r0 + i0 + i) * a.row_bytes, v[i]);
+        }
       }
-#pragma unroll
-      for (int r = 0; r < kScaleBlock; ++r)
-        if ((change >> r) & 1) store(head + (block * kScaleBlock + r) * a.row_bytes, v[r]);
+      if (e > own) {   // the rows that stay, once those that move have been read
+#pragma unroll 4
+        for (int r = 0; r < kScaleBlock; ++r) {
+          if (r >= r0 && r < r0 + (j1 - j0)) continue;
+          uint8_t* row = rows + (long long)r * a.row_bytes;
+          store(row, rescale_codes4(load(row), own - e));
+        }
+      }
       if (lane == 0 && e > own) scale[block * a.nkv + h] = (uint8_t)(e + 127);
       __syncwarp();
     }
@@ -261,7 +277,9 @@ static int compact(const C* layers, int n_layers, const oos_batch* batch, const 
     dim3 grid(batch->n_seqs, 2 * n);
     cudaError_t e;
     if (l.scaled) {
-      grid.z = std::min((l.nkv + kMaxMoved / 32 - 1) / (kMaxMoved / 32), 64);
+      // A head's side a warp: two cost as much as what they save of lookups (32 paths of up to 9,
+      // 36 layers, 8 kv heads 14.3 us and 14.7; one path in one layer 3.2 and 4.6).
+      grid = dim3(batch->n_seqs, n, std::min((2 * l.nkv + kMaxMoved / 32 - 1) / (kMaxMoved / 32), 64));
       const bool words = l.d % 4 == 0 && l.addresses % 4 == 0;
       e = words ? launch(true, k_compact8<true>, grid, dim3(kMaxMoved), 0, st, a)
                 : launch(true, k_compact8<false>, grid, dim3(kMaxMoved), 0, st, a);
