@@ -10,7 +10,11 @@
 // gain nothing by a smaller one; when it does, they are read, divided by a power of two and
 // rounded again.
 //
-// Bytes: the rows read once and half (a quarter) as many written.
+// Bytes: the rows read once and half (a quarter) as many written.  12600 rows of 8 heads in 24
+// sequences: 26 us with rotation alone, 2.7 TB/s (28 normed, fp32 29): not bound by bytes but by
+// some 1100 instructions a warp, sixteen warps an SM, as a block's rows stay in registers.  Two
+// warps a head in half the registers took 30 to 40 us, three blocks an SM (spilled) 29, four
+// heads a block (their angles formed twice as often) 28.  One token of 64 sequences: 4.7 us.
 #include <math.h>
 
 #include <algorithm>
@@ -242,8 +246,9 @@ static cudaError_t launch_append8(const Append8Args& a, const RopeTurns& rope, c
   if (wide) {
     const int chunks = d2 / V;
     if (chunks <= 4) return launch_append8_of<T, V, 4, 1>(a, rope, st);
-    if (chunks <= 8) return launch_append8_of<T, V, 8, 1>(a, rope, st);
-    return launch_append8_of<T, V, 16, 1>(a, rope, st);
+    if constexpr (V == 4)
+      if (chunks > 8) return launch_append8_of<T, V, 16, 1>(a, rope, st);
+    return launch_append8_of<T, V, 8, 1>(a, rope, st);   // d <= 128
   }
   if (d2 > 32) return launch_append8_of<T, 1, 32, 2>(a, rope, st);
   return launch_append8_of<T, 1, 32, 1>(a, rope, st);
