@@ -149,6 +149,7 @@ cudaError_t kernel_ready(std::atomic<uint64_t>& ready, const void* kernel, int s
 // own8: pages of 8 bits; c.dtype: the type of the prefix, and of other pages
 static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, const oos_batch& b, bool own8, BatchAttnPlan* p) {
   const int sms = device_sms();
+  *p = {};
   if (sms <= 0) return false;
   const int G = nq / c.n_kv_heads;
   const long long rows = (long long)b.n_tokens * G;
