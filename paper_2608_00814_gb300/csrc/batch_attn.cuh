@@ -184,6 +184,7 @@ struct PagesPlan {
 struct SequencePlan {
   bool takes_prefix;   // in the same kernel
   int tiles, splits;
+  bool part;           // leaves a part for a join, with one split too
 };
 SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_len, long long most_keys, int n_sms);
 PagesPlan plan_pages_tc(long long rows, int n_seqs, int nkv, long long most_keys, int n_sms);

@@ -601,7 +601,7 @@ PrefixPlan plan_prefix_tc(long long rows, int nkv, int prefix_len, int own_sms, 
 // sixteen 37).  The table may be wider than its sequences need: with eight times the columns
 // 16 trees over 2048 + up to 400 keys take 57 us (58 otherwise) and 13 prompts the same 275.
 SequencePlan plan_sequence_tc(long long rows, int n_seqs, int nkv, int prefix_len, long long most_keys, int n_sms) {
-  SequencePlan p;
+  SequencePlan p = {};
   p.tiles = (int)(n_seqs + rows / (2 * kTlRows));   // numbers; tiles that have rows, about:
   const long long live = (long long)n_seqs * ((rows + 2ll * kTlRows * n_seqs - 1) / (2ll * kTlRows * n_seqs));
   const int pre = (prefix_len + kTlKeys - 1) / kTlKeys;

@@ -83,7 +83,7 @@ template <typename TQ, bool SEQ>
 OOS_DEV void store_rows(const BatchAttnArgs& a, const TileRows& t, int dual, int S, int split, int part0, int g, float* stage,
                         int soft0) {
   const int rows = t.rows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (SEQ && S == 1) {
+  if (SEQ && S == 1 && !a.own_part) {
     // ---------------------------------------------------------- the rows' parts, staged and the prefix's, into out
     if (warp < soft0) return;
     pdl_wait();
