@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
   const int n_pre = p.pre_tiles, n_all = n_pre + (n_own + kTlKeys - 1) / kTlKeys;
   const int t0 = (int)((long long)n_all * split / S);
   const int n_tiles = (int)((long long)n_all * (split + 1) / S) - t0;
+  const bool joined = SEQ && S == 1 && !a.own_part;   // its rows go into out
   const int units = n_tiles << dual;                  // unit u: tile u >> dual, stream u & 1
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
@@ -550,7 +551,11 @@ __global__ void __launch_bounds__(kTlThreads, 1) k_attn_tiles(const __grid_const
     tc_fence_after();
     tmem_dealloc(tmem, kTlTmCols);
   }
-  store_rows<TQ, SEQ>(a, t, dual, S, split, p.part0, g, stage, kTlSoft0);
+  if (!joined) {
+    store_part<SEQ>(a, t, dual, split, p.part0, g, stage, kTlSoft0);
+  } else if constexpr (SEQ) {
+    if (warp >= kTlSoft0) join_rows<TQ, 1>(a, t, dual, g, stage, kTlSoft0);
+  }
 }
 
 // ---- host

@@ -77,93 +77,102 @@ OOS_DEV float max3_nan(float a, float b, float c) {
   return r;
 }
 
-// A block's staged rows (O, m, l; both streams' apart) into out, with the prefix's parts, or
-// into the parts of its key range.  soft0: the first of eight softmax warps.
-template <typename TQ, bool SEQ>
-OOS_DEV void store_rows(const BatchAttnArgs& a, const TileRows& t, int dual, int S, int split, int part0, int g, float* stage,
-                        int soft0) {
+// A block's staged rows (O, m, l; both streams' apart) into out, with the prefix's parts: the
+// eight softmax warps from soft0 on, behind a barrier.  U: parts of a row on their way at once.
+template <typename TQ, int U>
+OOS_DEV void join_rows(const BatchAttnArgs& a, const TileRows& t, int dual, int g, float* stage, int soft0) {
   const int rows = t.rows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (SEQ && S == 1 && !a.own_part) {
-    // ---------------------------------------------------------- the rows' parts, staged and the prefix's, into out
-    if (warp < soft0) return;
-    pdl_wait();
-    const int halves = dual ? 1 : 2, parts = halves + a.p_splits;   // <= 18
-    const long long part_rows = (long long)a.batch.n_tokens * a.group, part_step = (long long)a.pages.nkv * part_rows * kPartLd;
-    const float* pre = a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0) * kPartLd;
-    float* s_w = stage + 2 * kTlRows * kPartLd;   // [part][row]: weight over the sum of all
-    long long* s_out = reinterpret_cast<long long*>(s_w + (kTlMaxSplits + 2) * 2 * kTlRows);   // [row]: where it goes
-    {
-      const int r = threadIdx.x - 32 * soft0;   // a thread per row
-      if (r < rows) {
-        float2 ml[2];
+  pdl_wait();
+  const int halves = dual ? 1 : 2, parts = halves + a.p_splits;   // <= 18
+  const long long part_rows = (long long)a.batch.n_tokens * a.group, part_step = (long long)a.pages.nkv * part_rows * kPartLd;
+  const float* pre = a.part_o + ((long long)g * part_rows + (long long)t.q0 * a.group + t.r0) * kPartLd;
+  float* s_w = stage + 2 * kTlRows * kPartLd;   // [part][row]: weight over the sum of all
+  long long* s_out = reinterpret_cast<long long*>(s_w + (kTlMaxSplits + 2) * 2 * kTlRows);   // [row]: where it goes
+  {
+    const int r = threadIdx.x - 32 * soft0;   // a thread per row
+    if (r < rows) {
+      float2 ml[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-          ml[k] = k < halves ? *reinterpret_cast<const float2*>(stage + (k * kTlRows + r) * kPartLd + kTlD) : make_float2(-INFINITY, 0.f);
-        float top = max_nan(ml[0].x, ml[1].x);
+      for (int k = 0; k < 2; ++k)
+        ml[k] = k < halves ? *reinterpret_cast<const float2*>(stage + (k * kTlRows + r) * kPartLd + kTlD) : make_float2(-INFINITY, 0.f);
+      float top = max_nan(ml[0].x, ml[1].x);
 #pragma unroll 4
-        for (int k = 0; k < a.p_splits; ++k) top = max_nan(top, pre[k * part_step + r * kPartLd + kTlD]);
-        auto weight = [&](float m) { return m == -INFINITY ? 0.f : exp2f(m - top); };
-        float den = weight(ml[0].x) * ml[0].y + weight(ml[1].x) * ml[1].y;
+      for (int k = 0; k < a.p_splits; ++k) top = max_nan(top, pre[k * part_step + r * kPartLd + kTlD]);
+      auto weight = [&](float m) { return m == -INFINITY ? 0.f : exp2f(m - top); };
+      float den = weight(ml[0].x) * ml[0].y + weight(ml[1].x) * ml[1].y;
 #pragma unroll 4
-        for (int k = 0; k < a.p_splits; ++k) {
-          const float2 q = *reinterpret_cast<const float2*>(pre + k * part_step + r * kPartLd + kTlD);
-          const float w = weight(q.x);
-          s_w[(halves + k) * 2 * kTlRows + r] = w;
-          den += w * q.y;
-        }
-        const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
-        s_w[r] = weight(ml[0].x) * f;
-        if (!dual) s_w[2 * kTlRows + r] = weight(ml[1].x) * f;
-        for (int k = 0; k < a.p_splits; ++k) s_w[(halves + k) * 2 * kTlRows + r] *= f;
-        const int row = t.r0 + r;
-        s_out[r] = (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kTlD;
+      for (int k = 0; k < a.p_splits; ++k) {
+        const float2 q = *reinterpret_cast<const float2*>(pre + k * part_step + r * kPartLd + kTlD);
+        const float w = weight(q.x);
+        s_w[(halves + k) * 2 * kTlRows + r] = w;
+        den += w * q.y;
       }
+      const float f = den == 0.f ? 0.f : 1.f / den;   // a row without keys: zeros
+      s_w[r] = weight(ml[0].x) * f;
+      if (!dual) s_w[2 * kTlRows + r] = weight(ml[1].x) * f;
+      for (int k = 0; k < a.p_splits; ++k) s_w[(halves + k) * 2 * kTlRows + r] *= f;
+      const int row = t.r0 + r;
+      s_out[r] = (long long)(t.q0 + row / a.group) * a.out_stride + (g * a.group + row % a.group) * kTlD;
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    // 16 lanes a row, eight columns each; R pairs of rows of a warp at once
-    constexpr int R = 4;
-    const int col = (lane & 15) * 8;
-    const bool vec = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * 2)) & 15) == 0;
+  }
+  asm volatile("bar.sync 1, 256;" ::: "memory");
+  // 16 lanes a row, eight columns each; R pairs of rows of a warp at once
+  constexpr int R = 4;
+  const int col = (lane & 15) * 8;
+  const bool vec = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * 2)) & 15) == 0;
 #pragma unroll 1
-    for (int r0 = 2 * (warp - soft0) + (lane >> 4); r0 - (lane >> 4) < rows; r0 += 16 * R) {
-      float o[R][8];
+  for (int r0 = 2 * (warp - soft0) + (lane >> 4); r0 - (lane >> 4) < rows; r0 += 16 * R) {
+    float o[R][8];
 #pragma unroll
-      for (int k = 0; k < R; ++k)
+    for (int k = 0; k < R; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[k][e] = 0.f;
+      for (int e = 0; e < 8; ++e) o[k][e] = 0.f;
 #pragma unroll 1
-      for (int i = 0; i < parts; ++i) {
+    for (int i0 = 0; i0 < parts; i0 += U) {
+      float4 v[U][R][2];
+      float f[U][R];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u;
+        if (i >= parts) continue;
         const float* src = i < halves ? stage + i * kTlRows * kPartLd : pre + (i - halves) * part_step;
-        float4 v[R][2];
-        float f[R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
           const int r = min(r0 + 16 * k, rows - 1);
-          v[k][0] = *reinterpret_cast<const float4*>(src + r * kPartLd + col);
-          v[k][1] = *reinterpret_cast<const float4*>(src + r * kPartLd + col + 4);
-          f[k] = s_w[i * 2 * kTlRows + r];
-        }
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-          const float x[8] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w, v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[k][e] = f[k] != 0.f ? fmaf(f[k], x[e], o[k][e]) : o[k][e];   // no weight counts for nothing
+          v[u][k][0] = *reinterpret_cast<const float4*>(src + r * kPartLd + col);
+          v[u][k][1] = *reinterpret_cast<const float4*>(src + r * kPartLd + col + 4);
+          f[u][k] = s_w[i * 2 * kTlRows + r];
         }
       }
 #pragma unroll
-      for (int k = 0; k < R; ++k) {
-        if (r0 + 16 * k >= rows) continue;
-        TQ* out = (TQ*)a.out + s_out[r0 + 16 * k] + col;
-        if (vec) {
-          store_vec<TQ, 8>(out, o[k]);
-        } else {
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u >= parts) continue;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) out[e] = from_f32<TQ>(o[k][e]);
+        for (int k = 0; k < R; ++k) {
+          const float x[8] = {v[u][k][0].x, v[u][k][0].y, v[u][k][0].z, v[u][k][0].w, v[u][k][1].x, v[u][k][1].y, v[u][k][1].z, v[u][k][1].w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[k][e] = f[u][k] != 0.f ? fmaf(f[u][k], x[e], o[k][e]) : o[k][e];   // no weight counts for nothing
         }
       }
     }
-    return;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (r0 + 16 * k >= rows) continue;
+      TQ* out = (TQ*)a.out + s_out[r0 + 16 * k] + col;
+      if (vec) {
+        store_vec<TQ, 8>(out, o[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = from_f32<TQ>(o[k][e]);
+      }
+    }
   }
+}
+
+// The same into the parts of the block's key range.  The whole block, behind a barrier.
+template <bool SEQ>
+OOS_DEV void store_part(const BatchAttnArgs& a, const TileRows& t, int dual, int split, int part0, int g, float* stage, int soft0) {
+  const int rows = t.rows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (!dual && warp >= soft0) {   // both streams' sums of the same rows
     for (int r = warp - soft0; r < rows; r += 8) {
       float* ra = stage + r * kPartLd;

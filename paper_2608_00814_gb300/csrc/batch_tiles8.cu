@@ -131,6 +131,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
   const int n_all = (n_own + kTlKeys - 1) / kTlKeys;
   const int t0 = (int)((long long)n_all * split / S);
   const int n_tiles = (int)((long long)n_all * (split + 1) / S) - t0;
+  const bool joined = S == 1 && !a.own_part;   // its rows go into out
   const int units = n_tiles << dual;                  // unit u: tile u >> dual, stream u & 1
   if (threadIdx.x == 0) {
     for (int i = 0; i < 3; ++i) {
@@ -636,6 +637,12 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
                   : make_float4(ov[i], ov[i + 2], ov[i + 1], ov[i + 3]);   // V's order
     }
     *reinterpret_cast<float2*>(row + kTlD) = make_float2(have ? (F16 ? m - kHalfBias : m) : -INFINITY, have ? l : 0.f);
+    // here the warps have the registers for two parts at once (16 trees over 2048 keys 65 us, one
+    // at a time behind all warps' barrier 68)
+    if (joined) {
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      join_rows<TQ, 2>(a, t, dual, g, stage, kT8Soft0);
+    }
   }
   tc_fence_before();
   __syncthreads();   // rows staged
@@ -643,7 +650,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
     tc_fence_after();
     tmem_dealloc(tmem, kTlTmCols);
   }
-  store_rows<TQ, true>(a, t, dual, S, split, a.p_splits, g, stage, kT8Soft0);
+  if (!joined) store_part<true>(a, t, dual, split, a.p_splits, g, stage, kT8Soft0);
 }
 
 // ---- host
