@@ -11,7 +11,7 @@
 //
 // k_attn_rows (batch_rows.cuh): CUDA cores, fp32 products, for every type and head size.
 // The 16-bit types with heads of 128 take the tensor-core kernels of batch_tiles.cu and
-// batch_pages.cu.
+// batch_pages.cu, over 8-bit pages batch_tiles8.cu, batch_pages8.cu and batch_stream8.cu.
 #include <math.h>
 
 #include <algorithm>

@@ -1,5 +1,6 @@
-// Attention of a batch step: what its kernels share (batch_attn.cu, batch_tiles.cu,
-// batch_pages.cu).
+// Attention of a batch step: what its kernels share (batch_attn.cu, batch_rows.cuh,
+// batch_tiles.cu, batch_pages.cu, and over 8-bit pages batch_tiles8.cu, batch_pages8.cu,
+// batch_stream8.cu).
 #pragma once
 
 #include "batch.cuh"

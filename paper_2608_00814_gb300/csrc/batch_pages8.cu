@@ -9,8 +9,10 @@
 // barrier before the end.  Places and scales of 16 such pairs are looked up at once by the
 // lane that issues the copy.
 //
-// For short sequences: batch_stream8.cu's warps go from sequence to sequence and leave the
-// join to a kernel of its own.
+// For short sequences and more of them than batch_stream8.cu's table holds; that file's warps
+// go from sequence to sequence, and leave the join to a kernel of its own.  One token of one
+// request over 1024 shared and 18 own keys: 7.3 us with the prefix's kernel, all latency (9 us
+// each when they run apart); 64 of up to 100 own keys, 32 heads, 2048 shared: 22.6.
 #include <math.h>
 #include <string.h>
 

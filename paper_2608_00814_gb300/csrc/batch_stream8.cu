@@ -11,6 +11,14 @@
 // units.  k_join8 adds a row's places up, and the prefix's parts.
 //
 // As many blocks as the chip holds at once are launched; short steps leave some idle.
+//
+// Bound by HBM while the copies run: 6 requests of up to 64000 keys, 64 heads over 8, take 65 us
+// under a profiler, 6.0 TB/s with a beginning of 5 us (lengths, places, first copies), and 68 with
+// the join (16-bit pages 233); 64 of up to 4000, 2048 shared, 32 heads 50 (104), where the
+// prefix's kernel holds 64 SMs for 12 us and the join takes 4.  The issue slots are 37 % used, by some
+// 550 instructions for 8 KB.  Three stages for two blocks an SM: 66 and 54 us.  Other orders of
+// the blocks' work were slower: ranges by length for a block each 70 and 58 us, two or
+// three times as many 76 and 63 to 87 and 70; copies with other cache policies 72 and 57.
 #include <math.h>
 #include <string.h>
 
@@ -21,10 +29,13 @@
 namespace oos {
 
 constexpr int kS8MaxSeqs = kStreamSeqs;   // of the table in shared memory
-constexpr int kS8LeastPiece = 4;     // units of a warp, where there are enough
+constexpr int kS8LeastPiece = 4;     // units of a warp (8: 64 requests of up to 400 keys 28 us, 24 with 4)
 constexpr int kS8MaxPlaces = 256;    // of a tile, about: longer pieces otherwise
 constexpr int kS8JoinThreads = 128;
-constexpr double kS8UnitsPerUs = 0.3;   // of a warp
+// Units that a warp takes in a microsecond, by which the shares of blocks that start when the
+// prefix's are done are smaller (64 requests as above: 0 59 us, 0.25 to 0.45 55, 0.65 56; 200 of
+// up to 1500 keys 83, 84 to 86, 93)
+constexpr double kS8UnitsPerUs = 0.3;
 
 // Shares of `piece` units for the first `early` warps, of `late` less for the others
 struct S8Shares {

@@ -23,8 +23,11 @@
 //     32 bits: an e below -60 counts as -60, and the codes are made smaller instead.
 //
 // 13 prompts of up to 300 tokens, 40 heads over 8, 1000 shared and up to 1800 own keys in
-// binary16: 243 us; 16 trees of up to 64 nodes, 32 heads, 2048 shared and up to 464 own keys
-// in bf16: 71 (batch_pages8.cu's kernel: 783 and 128).  The shared keys are the other kernel's.
+// binary16: 232 us (tiles of 16 rows, before this kernel: 783); 16 trees of up to 64 nodes, 32
+// heads, 2048 shared and up to 464 own keys in bf16: 64 (128).  The shared keys are the other
+// kernel's.  Without them 147 and 28 us, as 16-bit pages take (138 and 26): neither the
+// conversion (9 us of the 147), nor K's copies (7), nor the exponentials (12) bound it, but what
+// a block of few key tiles does one after the other, and its waves (3.2 of 152 blocks).
 #include <math.h>
 
 #include <algorithm>

@@ -1,5 +1,5 @@
 // Pages of 8 bits: e4m3 codes with a power of two for each block of 16 positions and kv
-// head, held as its exponent + 127 (batch_pages8.cu, heads8.cu, pages.cu).
+// head, held as its exponent + 127 (heads8.cu, pages.cu, and the attention's kernels).
 #pragma once
 
 #include "batch.cuh"
