@@ -44,6 +44,13 @@ def test_shares(dtype, kv, counts, most, page, nq, nkv, prefix):
     T.run_case8(counts, lens, page, 3, prefix, nq, nkv, 128, dtype, kv, seed=5)
 
 
+@pytest.mark.parametrize("counts, lens, nq, nkv", [([1, 1], [1100, 30], 460, 460), ([1, 0, 1], [2000, 7, 70], 64, 1),
+                                                   ([1, 2], [1030, 500], 48, 3)])
+def test_more_heads_than_blocks_and_wide_groups(counts, lens, nq, nkv):
+    """A block for each kv head where there are more of them than the chip holds blocks; groups of several tiles."""
+    T.run_case8(counts, lens, 16, 1, 40, nq, nkv, 128, BF16, BF16)
+
+
 @pytest.mark.parametrize("dtype, kv", HALVES)
 @pytest.mark.parametrize("n", [256, 257])
 def test_as_many_sequences_as_the_table_holds(dtype, kv, n):
