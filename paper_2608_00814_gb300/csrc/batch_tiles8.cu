@@ -23,11 +23,11 @@
 //     32 bits: an e below -60 counts as -60, and the codes are made smaller instead.
 //
 // 13 prompts of up to 300 tokens, 40 heads over 8, 1000 shared and up to 1800 own keys in
-// binary16: 232 us (tiles of 16 rows, before this kernel: 783); 16 trees of up to 64 nodes, 32
-// heads, 2048 shared and up to 464 own keys in bf16: 64 (128).  The shared keys are the other
-// kernel's.  Without them 147 and 28 us, as 16-bit pages take (138 and 26): neither the
-// conversion (9 us of the 147), nor K's copies (7), nor the exponentials (12) bound it, but what
-// a block of few key tiles does one after the other, and its waves (3.2 of 152 blocks).
+// binary16: 200 us (tiles of 16 rows, before this kernel: 783); 16 trees of up to 64 nodes, 32
+// heads, 2048 shared and up to 464 own keys in bf16: 60 (128).  The shared keys are the other
+// kernel's.  Without them the prompts take 119 us (16-bit pages 138): neither the conversion (9
+// us), nor K's copies (7), nor the exponentials (12) bound it, but what a block of few key tiles
+// does one after the other.
 #include <math.h>
 
 #include <algorithm>
@@ -42,6 +42,7 @@ constexpr int kT8Codes = kTlKeys * kTlD;   // bytes of a tile of codes
 constexpr int kT8VStages = 2;
 constexpr int kT8Threads = 512;            // K; scores; P.V; -; V x 4; softmax x 8
 constexpr int kT8Soft0 = 8, kT8V0 = 4;
+constexpr int kT8Ordered = 64;             // sequences whose tiles are dealt by length
 constexpr int kT8LowExp = -60;             // V's exponents in binary16 weights
 constexpr int kT8RegsIo = 64, kT8RegsSoft = 192, kT8RegsLaunch = 128;
 static_assert(256 * kT8RegsIo + 256 * kT8RegsSoft <= kT8Threads * kT8RegsLaunch, "register split");
@@ -86,6 +87,58 @@ OOS_DEV void tc_mma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32
       : "memory");
 }
 
+// Tile i of the sequences' tiles, the longest sequences' first: blocks of many key tiles that
+// begin last would leave most SMs idle behind them.  n_seqs <= kT8Ordered, two a lane; each
+// adds up the tiles of those before it.  In the sequences' order, heads slowest, the prompts
+// above take 233 us and the trees 64.  The whole warp; false: no such tile.
+OOS_DEV bool longest_first(const BatchAttnArgs& a, int i, TileRows* t) {
+  const BatchView& b = a.batch;
+  const int lane = threadIdx.x & 31;
+  const long long most = min((long long)b.max_pages * a.pages.page_size, (long long)kMaxKeys);
+  int q0[2], n[2], len[2], tiles[2], start[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int seq = lane + 32 * u;
+    q0[u] = n[u] = len[u] = tiles[u] = start[u] = 0;
+    if (seq >= b.n_seqs) continue;
+    const int from = b.q_start[seq], to = b.q_start[seq + 1], given = b.seq_len[seq], held = max(0, given);
+    const bool in_order = from >= 0 && to <= b.n_tokens && from <= to, ok = in_order && (!a.parent || to - from <= kMaxTreeRows);
+    if (blockIdx.x == 0 && threadIdx.x < 32 && (!ok || given < to - from || held > most))
+      *a.status = in_order && !ok ? OOS_ETREE : OOS_EBATCH;
+    if (!ok) continue;
+    q0[u] = from;
+    n[u] = to - from;
+    len[u] = (int)min((long long)held, most);
+    tiles[u] = (n[u] * a.group + 2 * kTlRows - 1) / (2 * kTlRows);   // n_tokens * nq stays below 2^26
+  }
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    if (32 * v >= b.n_seqs) break;
+#pragma unroll 4
+    for (int x = 0; x < 32; ++x) {
+      const int other = __shfl_sync(0xffffffffu, len[v], x), its = __shfl_sync(0xffffffffu, tiles[v], x);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (other > len[u] || (other == len[u] && x + 32 * v < lane + 32 * u)) start[u] += its;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t who = __ballot_sync(0xffffffffu, i >= start[u] && i < start[u] + tiles[u]);
+    if (who == 0) continue;
+    const int src = __ffs(who) - 1;
+    t->seq = src + 32 * u;
+    t->q0 = __shfl_sync(0xffffffffu, q0[u], src);
+    t->n = __shfl_sync(0xffffffffu, n[u], src);
+    t->len = __shfl_sync(0xffffffffu, len[u], src);
+    t->first = t->len - t->n;
+    t->r0 = (i - __shfl_sync(0xffffffffu, start[u], src)) * 2 * kTlRows;
+    t->rows = min(2 * kTlRows, t->n * a.group - t->r0);
+    return true;
+  }
+  return false;
+}
+
 template <typename TQ>
 __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_constant__ BatchAttnArgs a) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -116,15 +169,15 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
   volatile int* s_apart = abort_flag + 1;                       // [2] the stream's tile whose P.V is done, + 1
   static_assert(23 * 8 + 32 * 4 + 16 * 2 + 8 + 4 * 4 <= 384, "barrier block");
   int32_t* status = a.status;
-  const int S = a.s_splits, split = blockIdx.x % S, pair = blockIdx.x / S, g = blockIdx.y;
+  const int S = a.s_splits, nkv = a.pages.nkv, g = blockIdx.x % nkv, at = blockIdx.x / nkv, split = at % S, pair = at / S;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // behind the prefix's kernel, which has waited for what the caller wrote before it
   // triggers, only the end waits for the prefix's parts
   if (a.p_splits == 0) pdl_wait();
   pdl_trigger();
   TileRows t = {};
-  if (!sequence_tile(a, pair, 2 * kTlRows, &t)) {
-    if (blockIdx.x == 0 && blockIdx.y == 0) pdl_wait();   // the grid must not end before the one it follows
+  if (!(a.batch.n_seqs <= kT8Ordered ? longest_first(a, pair, &t) : sequence_tile(a, pair, 2 * kTlRows, &t))) {
+    if (blockIdx.x == 0) pdl_wait();   // the grid must not end before the one it follows
     return;
   }
   const int rows = t.rows;
@@ -640,8 +693,8 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
                   : make_float4(ov[i], ov[i + 2], ov[i + 1], ov[i + 3]);   // V's order
     }
     *reinterpret_cast<float2*>(row + kTlD) = make_float2(have ? (F16 ? m - kHalfBias : m) : -INFINITY, have ? l : 0.f);
-    // here the warps have the registers for two parts at once (16 trees over 2048 keys 65 us, one
-    // at a time behind all warps' barrier 68)
+    // here the warps have the registers for two parts at once (64 trees over 2048 keys 213 us,
+    // one at a time behind all warps' barrier 227)
     if (joined) {
       asm volatile("bar.sync 1, 256;" ::: "memory");
       join_rows<TQ, 2>(a, t, dual, g, stage, kT8Soft0);
@@ -666,7 +719,7 @@ static cudaError_t launch_tiles8(const BatchAttnArgs& a, dim3 grid, cudaStream_t
 }
 
 cudaError_t launch_sequence8_tc(const BatchAttnArgs& a, const SequencePlan& plan, int dtype, cudaStream_t st) {
-  const dim3 grid((unsigned)(plan.tiles * plan.splits), a.pages.nkv);
+  const dim3 grid((unsigned)(plan.tiles * plan.splits * a.pages.nkv));   // rows are many: below 2^31
   return dtype == OOS_DTYPE_BF16 ? launch_tiles8<__nv_bfloat16, 2>(a, grid, st) : launch_tiles8<__half, 3>(a, grid, st);
 }
 

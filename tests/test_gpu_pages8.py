@@ -307,6 +307,15 @@ def test_attention8_many_sequences(dtype, kv):
     run_case8(counts, [c + i % 5 for i, c in enumerate(counts)], 16, 1, 33, 20, 1, 128 if kv is not F32 else 64, dtype, kv)
 
 
+@pytest.mark.parametrize("dtype, kv", TYPES[1:])
+@pytest.mark.parametrize("n", [33, 64, 65])
+def test_attention8_many_rows_of_many_sequences(dtype, kv, n):
+    """Tiles dealt by their sequences' lengths, equal ones among them, and more sequences than that holds."""
+    counts = [0 if i % 9 == 4 else 70 if i % 5 else 130 for i in range(n)]
+    lens = [c + (i * 37) % 11 * 20 for i, c in enumerate(counts)]
+    run_case8(counts, lens, 16, 2, 30, 2, 2, 128, dtype, kv)
+
+
 @pytest.mark.parametrize("dtype, kv", TYPES)
 @pytest.mark.parametrize("counts, lens", [([1, 1, 2], [100, 300, 40]), ([90, 140], [200, 300])])
 @pytest.mark.parametrize("lo, hi", [(-117, -100), (-60, 30), (100, 119)])
