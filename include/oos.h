@@ -552,7 +552,7 @@ int oos_paged_append8(const oos_paged_cache8* cache, const oos_batch* batch, int
  *                  (OOS_EUNSUPPORTED otherwise; not looked at when prefix_len is 0)
  * With 16-bit types and heads of 128, codes start on 16-byte boundaries (OOS_EINVAL
  * otherwise), and what is rounded depends on whether sequences have few rows (token,
- * head of a group), up to 64 on average.
+ * head of a group): up to 64 on average, more in small batches.
  *   few    BF16 queries are scaled and rounded to binary16: 2^-25 of a row's largest |q|
  *          in every element; the weights that own positions' v is multiplied by to 2^-11,
  *          below 2^-21 of the row's largest weight times scale to 2^-32 of that

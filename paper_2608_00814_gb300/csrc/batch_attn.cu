@@ -157,10 +157,16 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
   p->tc = c.dtype != OOS_DTYPE_F32 && c.head_dim == 128;
   if (p->tc && own8) {
     // Tiles of 16 rows that each read their sequence's pages, or tiles of up to 256.  Trees of
-    // 4 rows a node, 8 kv heads, 2048 prefix keys: 36 rows on average over up to 400 keys 33 us
-    // against 48 (16 sequences) and 77 against 111 (64), over up to 2000 118 against 209 (64); 72
-    // rows 47 against 49 (16), 138 against 125 (64), 227 against 216 (64, up to 2000 keys).
-    p->few = rows <= 64ll * b.n_seqs;
+    // 4 rows a node, 8 kv heads, 2048 prefix keys: 48 rows on average over up to 400 keys 38 us
+    // against 41 (16 sequences) and 93 against 102 (64), 60 rows 44 against 41 and 111 against 118,
+    // 72 rows 47 against 44 and 138 against 126.  Where all tiles of 16 fit the chip about twice,
+    // more: 72 rows 21 against 33 (4 sequences; up to 4000 keys 37 against 85), 116 rows 17 against
+    // 29 (1; up to 4000 keys 30 both), 101 rows 28 against 34 (4); but 96 rows 40 against 36 (8).
+    // And over short tables where they fit it once: 232 rows 19 against 33 (1), 154 rows 21
+    // against 36 (2), but 164 rows 36 against 39 (4), and 304 rows over up to 4000 keys 52
+    // against 41 (1).
+    const long long tiles16 = rows / 16 * c.n_kv_heads;
+    p->few = rows <= 64ll * b.n_seqs || (rows <= 128ll * b.n_seqs && tiles16 <= 2ll * sms) || (most_keys <= 1024 && tiles16 <= sms);
     p->sequence = {false, 0, 1};
     if (p->few) p->pages = plan_pages8_tc(rows, b.n_seqs, c.n_kv_heads, sms);
     else p->sequence = plan_sequence_tc(rows, b.n_seqs, c.n_kv_heads, 0, most_keys, sms);   // the prefix apart
@@ -168,8 +174,8 @@ static bool plan_batch_attn(int nq, int prefix_len, const oos_paged_cache& c, co
     // Blocks of many rows that join with several parts of the prefix wait for them and read
     // them one after the other; they leave a part too.  Trees of 4 rows a node, 8 kv heads, up to
     // 464 own keys: 8 sequences, 2048 prefix keys in 3 parts 50 us against 61, 4 sequences 36
-    // against 56, 16 over 8000 keys 124 against 136; one part (16 over 2048) 69 against 68, (13
-    // prompts of 40 heads) 255 against 242.
+    // against 56, 16 over 8000 keys 124 against 136; with one part 16 sequences take
+    // 66 against 60, 13 prompts of 40 heads 227 against 202.
     p->sequence.part = !p->few && p->prefix.splits > 1;
     const int own = !p->few && (p->sequence.part || p->sequence.splits > 1) ? p->sequence.splits : 0;
     const int parts = p->prefix.splits + own;

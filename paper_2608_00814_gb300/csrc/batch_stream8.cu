@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kP8Warps * 32, p8_blocks(NT)) k_attn_stream8(c
   if (a.p_splits == 0) pdl_wait();
   pdl_trigger();
 
-  // ---- the table: thread i has sequences 4 i ..
+  // ---- the table: thread i has sequences PER i ..
   constexpr int PER = kS8MaxSeqs / (kP8Warps * 32);
   const long long most = min((long long)b.max_pages * a.pages.page_size, (long long)kMaxKeys);
   const bool report = blockIdx.x == 0;

@@ -186,3 +186,23 @@ def test_repeats_bit_for_bit(dtype, kv):
         assert torch.equal(base, T.attend8(step, q, pk, pv, 500, cache)[0])
         side.synchronize()
     assert int(st) == 0
+
+
+def test_calls_over_pages_of_both_kinds_in_turn():
+    """A call over 16-bit pages right behind one over 8-bit pages takes nothing of its plan."""
+    step = R.Step([1, 1, 2], [1200, 30, 500], 16)
+    q, pk, pv, cache = T.inputs8(step, 70, 8, 2, 128, BF16, BF16)
+    k, v = [torch.nan_to_num(t).to(BF16) for t in cache.dequantized()]
+    pages, batch, st = B.PagedCache(k, v), step.device(B), status()
+    ws = torch.empty(B.oos_shared_prefix_attention_workspace_bytes(q, 70, pages, batch), dtype=torch.uint8, device="cuda")
+
+    def wide():
+        out = torch.zeros_like(q)
+        B.oos_shared_prefix_attention(q, pk, pv, 70, pages, batch, None, 1 / math.sqrt(128), out, ws, st)
+        return out
+    base, base8 = wide(), T.attend8(step, q, pk, pv, 70, cache)[0]
+    for _ in range(3):
+        assert torch.equal(T.attend8(step, q, pk, pv, 70, cache)[0], base8)
+        assert torch.equal(wide(), base)
+    assert int(st) == 0
+    R.check_attention(base, *R.attention(step, q, pk[:70], pv[:70], k, v, 1 / math.sqrt(128)), 1270, BF16)
