@@ -539,7 +539,8 @@ typedef struct {
  *     not taken.  So a position appended alone may be rounded up to once more for each
  *     octave that the scale grows by, each time by half a step of the new one.
  * The scale is of the fp32 values after norm and rotation, which are then rounded once
- * (nearest even).  Values that are not finite become NaN and do not count toward the
+ * (nearest even; a value that fp32's error could bring over the border between two codes is
+ * computed in 64 bits).  Values that are not finite become NaN and do not count toward the
  * scale; magnitudes above 448 2^119 become it.
  * Two sequences must not append to the same block of positions of a page: a page that
  * several sequences continue has to be copied first (oos_pages_copy8). */

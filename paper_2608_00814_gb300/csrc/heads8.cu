@@ -11,10 +11,12 @@
 // rounded again.
 //
 // Bytes: the rows read once and half (a quarter) as many written.  12600 rows of 8 heads in 24
-// sequences: 26 us with rotation alone, 2.7 TB/s (28 normed, fp32 29): not bound by bytes but by
-// some 1100 instructions a warp, sixteen warps an SM, as a block's rows stay in registers.  Two
-// warps a head in half the registers took 30 to 40 us, three blocks an SM (spilled) 29, four
-// heads a block (their angles formed twice as often) 28.  One token of 64 sequences: 4.7 us.
+// sequences: 29 us with rotation alone, 2.4 TB/s (32 normed, fp32 32): not bound by bytes but by
+// some 1200 instructions a warp, sixteen warps an SM, as a block's rows stay in registers.
+// Before the search for values near a border that was 26 us, and two warps a head in half the
+// registers took 30 to 40, three blocks an SM (spilled) 29, four heads a block (their angles
+// formed twice as often) 28.  One token of 64 sequences: 9 us in a graph, 6 of them without a
+// warp that computes one again.
 #include <math.h>
 
 #include <algorithm>
@@ -36,6 +38,21 @@ struct Append8Args {
   float eps;
   int32_t* status;
 };
+
+// A code's steps are 2^20 of fp32's: where a normed or turned value lies within 8 of those
+// of the border between two codes, fp32's own errors choose between them.  Such pairs, in
+// three of a hundred warps, are computed again in 64 bits.
+OOS_DEV bool on_border(float v) { return (__float_as_uint(v) & 0xfffffu) - 0x7fff8u <= 16u; }
+// a value of 64 bits so that rounding it again to few bits gives what rounding once does
+OOS_DEV float round_to_odd(double v) {
+  const float f = __double2float_rz(v);
+  return (double)f == v || isnan(v) ? f : __uint_as_float(__float_as_uint(f) | 1u);
+}
+static __device__ __noinline__ double2 turn64(unsigned long long rate, int pos) {   // cos, sin
+  double s, c;
+  sincospi((double)(long long)((unsigned long long)(long long)pos * rate) * 0x1p-63, &s, &c);
+  return make_double2(c, s);
+}
 
 // T: elements of the rows.  A row's half is dealt in chunks of VEC to LANES lanes, NC each;
 // 32 / LANES rows at once.
@@ -202,6 +219,61 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
     }
   }
   const float inv = pow2f(-e);
+  if (side == 0 && (a.gain || a.positions)) {
+    uint32_t near = 0;   // passes
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      bool any = false;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) any = any || on_border(y[p][c][half][i] * inv);
+      near |= (any ? 1u : 0u) << p;
+    }
+    near = __reduce_or_sync(0xffffffffu, near);
+    if (near) {
+      const T* gain = (const T*)a.gain;
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int r = p * ROWS + group;
+        if (!((near >> p) & 1)) continue;
+        const bool there = r >= lo && r < hi;
+        const T* row = (const T*)a.in[0] + (t0 + (there ? r : lo)) * a.stride[0] + (long long)h * d;
+        double f = 1.0;
+        if (gain) {
+          double ss = 0.0;
+          for (int k = sub; k < d; k += LANES) ss += (double)to_f32(row[k]) * (double)to_f32(row[k]);
+#pragma unroll
+          for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          const double x = ss / d + (double)a.eps;   // a step of Newton's from fp32's root
+          f = (double)rsqrtf((float)x);
+          f *= 1.5 - 0.5 * x * f * f;
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const int m = (c * LANES + sub) * VEC + i;
+            if (!there || m >= d2 || !(on_border(y[p][c][0][i] * inv) || on_border(y[p][c][1][i] * inv))) continue;
+            double u = to_f32(row[m]), w = to_f32(row[d2 + m]);
+            if (gain) {
+              u *= f * (double)to_f32(gain[m]);
+              w *= f * (double)to_f32(gain[d2 + m]);
+            }
+            if (a.positions) {
+              const double2 cs = turn64(rope.f[m], a.positions[t0 + r]);
+              const double turned = u * cs.x - w * cs.y;
+              w = w * cs.x + u * cs.y;
+              u = turned;
+            }
+            y[p][c][0][i] = round_to_odd(u);
+            y[p][c][1][i] = round_to_odd(w);
+          }
+      }
+    }
+  }
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int r = p * ROWS + group;

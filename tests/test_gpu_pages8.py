@@ -131,6 +131,29 @@ def test_append8_special_values(dtype, d):
     assert bool(torch.isnan(p[0][step.where(0, 0)[0], 0].float()).all()) and int(st) == 0
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_append8_rounds_what_64_bits_give(dtype):
+    """Codes next to a border.  A turned value is off by at most 6.5 half steps of its pair's length (cosine and sine 2.5
+    each, their products and the sum 1.5), so by at most 8 steps of its own where it has nine tenths of that length; all
+    of those within 8 steps of a border are computed in 64 bits."""
+    n, nkv, d = 16384, 8, 128
+    step = R.Step([n], [n], 256)
+    g = gen(5)
+    k = randn(g, n, nkv, d, dtype=dtype)
+    pos = torch.randint(0, 100000, (n,), generator=g, device="cuda", dtype=torch.int32)
+    p = pool(g, step.n_pages, 256, nkv, d)
+    st = status()
+    B.oos_paged_append8(B.PagedCache8(*p), step.device(B), k, k, None, 0.0, B.OosRopeConfig(1e6), pos, st)
+    assert int(st) == 0
+    ref, r = R.norm_rope(k, None, 0.0, R.rates(d, 1e6), pos)
+    order = torch.tensor(step.table[0])
+    codes = p[0].cpu().double()[order].view(n, nkv, d)
+    e = R8.exps(p[2])[order].view(n // 16, nkv).repeat_interleave(16, 0)[..., None]
+    want = R8.e4m3(torch.ldexp(ref, -e))
+    large = ref.abs() >= 0.9 * r
+    assert int(large.sum()) > n * nkv * d // 5 and not bool((codes != want)[large].any())
+
+
 def test_append8_reports_rows_without_a_place():
     """A page outside the pool, a position outside the table, a length below the step's rows: those blocks are left
     out and reported, the others are appended."""
