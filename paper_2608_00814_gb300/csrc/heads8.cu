@@ -268,8 +268,9 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
               w = w * cs.x + u * cs.y;
               u = turned;
             }
-            y[p][c][0][i] = round_to_odd(u);
-            y[p][c][1][i] = round_to_odd(w);
+            // what fp32 passed stays NaN beside a partner that is computed again
+            if (!isnan(y[p][c][0][i])) y[p][c][0][i] = round_to_odd(u);
+            if (!isnan(y[p][c][1][i])) y[p][c][1][i] = round_to_odd(w);
           }
       }
     }
