@@ -538,10 +538,10 @@ typedef struct {
  *     larger scale, the codes already there are rounded again to it; a smaller one is
  *     not taken.  So a position appended alone may be rounded up to once more for each
  *     octave that the scale grows by, each time by half a step of the new one.
- * The scale is of the fp32 values after norm and rotation, which are then rounded once
- * (nearest even; a value that fp32's error could bring over the border between two codes is
- * computed in 64 bits).  Values that are not finite become NaN and do not count toward the
- * scale; magnitudes above 448 2^119 become it.
+ * The scale is of the fp32 values after norm and rotation, which are then rounded once,
+ * to the nearest even code: of two codes whose border lies within fp32's error of a value
+ * (a few 2^-24 of its pair's length) it may take either.  Values that are not finite become
+ * NaN and do not count toward the scale; magnitudes above 448 2^119 become it.
  * Two sequences must not append to the same block of positions of a page: a page that
  * several sequences continue has to be copied first (oos_pages_copy8). */
 int oos_paged_append8(const oos_paged_cache8* cache, const oos_batch* batch, int32_t dtype, const void* k,

@@ -11,12 +11,10 @@
 // rounded again.
 //
 // Bytes: the rows read once and half (a quarter) as many written.  12600 rows of 8 heads in 24
-// sequences: 29 us with rotation alone, 2.4 TB/s (32 normed, fp32 32): not bound by bytes but by
-// some 1200 instructions a warp, sixteen warps an SM, as a block's rows stay in registers.
-// Before the search for values near a border that was 26 us, and two warps a head in half the
-// registers took 30 to 40, three blocks an SM (spilled) 29, four heads a block (their angles
-// formed twice as often) 28.  One token of 64 sequences: 9 us in a graph, 6 of them without a
-// warp that computes one again.
+// sequences: 26 us with rotation alone, 2.7 TB/s (28 normed, fp32 28): not bound by bytes but by
+// some 1100 instructions a warp, sixteen warps an SM, as a block's rows stay in registers.  Two
+// warps a head in half the registers took 30 to 40 us, three blocks an SM (spilled) 29, four
+// heads a block (their angles formed twice as often) 28.  One token of 64 sequences: 4.7 us.
 #include <math.h>
 
 #include <algorithm>
@@ -39,10 +37,20 @@ struct Append8Args {
   int32_t* status;
 };
 
-// A code's steps are 2^20 of fp32's: where a normed or turned value lies within 8 of those
-// of the border between two codes, fp32's own errors choose between them.  Such pairs, in
-// three of a hundred warps, are computed again in 64 bits.
-OOS_DEV bool on_border(float v) { return (__float_as_uint(v) & 0xfffffu) - 0x7fff8u <= 16u; }
+// A code's steps are 2^20 of fp32's, and where a value lies next to the border of two codes
+// fp32's own error chooses between them.  For the larger element of a turned pair that is not
+// normed it is at most 6.5 half steps of fp32 (2^-24) of the pair's length -- cosine and sine
+// 2.5 each, their products and the sum 1.5 -- and so 9.2 steps of its own, as the length is at
+// most 2^1/2 of it.  Within ten steps of a border of normal codes such a pair, one in 50000,
+// is computed in 64 bits, by a few instructions a pair (no difference in the times above; 0.5
+// us where one of 64 tokens' has to be): the bits below a code's tell it, whatever the scale.
+// Elsewhere the error chooses.  To find every such value both ends of what it may be would have
+// to be rounded, and a third of the normed warps compute one again (35 us, 52 normed); either
+// code is as near as the other to 2^-20 of the pair's length.
+constexpr uint32_t kBorderSteps = 10;
+OOS_DEV uint32_t from_border(float larger) {   // at most 2 kBorderSteps << 12: within that of one
+  return (__float_as_uint(larger) - (0x80000u - kBorderSteps)) << 12;
+}
 // a value of 64 bits so that rounding it again to few bits gives what rounding once does
 OOS_DEV float round_to_odd(double v) {
   const float f = __double2float_rz(v);
@@ -55,8 +63,8 @@ static __device__ __noinline__ double2 turn64(unsigned long long rate, int pos) 
 }
 
 // T: elements of the rows.  A row's half is dealt in chunks of VEC to LANES lanes, NC each;
-// 32 / LANES rows at once.
-template <typename T, int VEC, int LANES, int NC>
+// 32 / LANES rows at once.  SEARCH: K is turned and not normed.
+template <typename T, int VEC, int LANES, int NC, bool SEARCH>
 __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Args a, const __grid_constant__ RopeTurns rope) {
   constexpr int ROWS = 32 / LANES, PASSES = kScaleBlock / ROWS;
   // of element m = (c LANES + sub) VEC + i of a half: at (c VEC + i) LANES + sub, so that a
@@ -129,8 +137,9 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
     __syncthreads();
   }
   if (h >= nkv) return;
+  uint32_t near = 0;   // passes with pairs next to a border
   if (side == 0) {
-    const T* gain = (const T*)a.gain;
+    const T* gain = SEARCH ? nullptr : (const T*)a.gain;
     float g[NC][2][VEC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -156,6 +165,7 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
         for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         f = rsqrtf(ss / (float)d + a.eps);
       }
+      uint32_t least = ~0u;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -166,15 +176,17 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
             lo_ = lo_ * f * g[c][0][i];
             hi_ = hi_ * f * g[c][1][i];
           }
-          if (a.positions && m < d2 && r >= lo && r < hi) {
+          if ((SEARCH || a.positions) && m < d2 && r >= lo && r < hi) {
             const float2 cs = s_turn[r][(c * VEC + i) * LANES + sub];
             const float turned = lo_ * cs.x - hi_ * cs.y;
             hi_ = hi_ * cs.x + lo_ * cs.y;
             lo_ = turned;
+            if (SEARCH) least = min(least, from_border(fmaxf(fabsf(lo_), fabsf(hi_))));
           }
           y[p][c][0][i] = lo_;
           y[p][c][1][i] = hi_;
         }
+      if (SEARCH) near |= (least <= 2 * kBorderSteps << 12 ? 1u : 0u) << p;
     }
   }
   float amax = 0.f;   // of what is finite in the block's rows; the others' are zeros
@@ -219,62 +231,6 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
     }
   }
   const float inv = pow2f(-e);
-  if (side == 0 && (a.gain || a.positions)) {
-    uint32_t near = 0;   // passes
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-      bool any = false;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) any = any || on_border(y[p][c][half][i] * inv);
-      near |= (any ? 1u : 0u) << p;
-    }
-    near = __reduce_or_sync(0xffffffffu, near);
-    if (near) {
-      const T* gain = (const T*)a.gain;
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p) {
-        const int r = p * ROWS + group;
-        if (!((near >> p) & 1)) continue;
-        const bool there = r >= lo && r < hi;
-        const T* row = (const T*)a.in[0] + (t0 + (there ? r : lo)) * a.stride[0] + (long long)h * d;
-        double f = 1.0;
-        if (gain) {
-          double ss = 0.0;
-          for (int k = sub; k < d; k += LANES) ss += (double)to_f32(row[k]) * (double)to_f32(row[k]);
-#pragma unroll
-          for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const double x = ss / d + (double)a.eps;   // a step of Newton's from fp32's root
-          f = (double)rsqrtf((float)x);
-          f *= 1.5 - 0.5 * x * f * f;
-        }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            const int m = (c * LANES + sub) * VEC + i;
-            if (!there || m >= d2 || !(on_border(y[p][c][0][i] * inv) || on_border(y[p][c][1][i] * inv))) continue;
-            double u = to_f32(row[m]), w = to_f32(row[d2 + m]);
-            if (gain) {
-              u *= f * (double)to_f32(gain[m]);
-              w *= f * (double)to_f32(gain[d2 + m]);
-            }
-            if (a.positions) {
-              const double2 cs = turn64(rope.f[m], a.positions[t0 + r]);
-              const double turned = u * cs.x - w * cs.y;
-              w = w * cs.x + u * cs.y;
-              u = turned;
-            }
-            // what fp32 passed stays NaN beside a partner that is computed again
-            if (!isnan(y[p][c][0][i])) y[p][c][0][i] = round_to_odd(u);
-            if (!isnan(y[p][c][1][i])) y[p][c][1][i] = round_to_odd(w);
-          }
-      }
-    }
-  }
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
     const int r = p * ROWS + group;
@@ -299,6 +255,27 @@ __global__ void __launch_bounds__(kApMaxHeads * 32, 2) k_append8(const Append8Ar
         }
       }
   }
+  if constexpr (SEARCH) {
+    // a lane's pairs of a row, a lane each, over the codes that are written
+    uint32_t who = __ballot_sync(0xffffffffu, near != 0);
+    if (who) __syncwarp();
+#pragma unroll 1
+    for (; who; who &= who - 1) {
+      const int from = __ffs(who) - 1, m = (lane / VEC * LANES + from % LANES) * VEC + lane % VEC;
+#pragma unroll 1
+      for (uint32_t passes = __shfl_sync(0xffffffffu, near, from); passes; passes &= passes - 1) {
+        const int r = (__ffs(passes) - 1) * ROWS + from / LANES;
+        if (lane >= NC * VEC || m >= d2) continue;
+        const T* row = (const T*)a.in[0] + (t0 + r) * a.stride[0] + (long long)h * d + m;
+        uint8_t* to = codes + (long long)r * nkv * d + m;
+        const double u = to_f32(row[0]), w = to_f32(row[d2]);
+        const double2 cs = turn64(rope.f[m], a.positions[t0 + r]);
+        // what fp32 passed stays NaN
+        if ((to[0] & 0x7f) != 0x7f) to[0] = (uint8_t)f32x2_e4m3(round_to_odd((u * cs.x - w * cs.y) * (double)inv), 0.f);
+        if ((to[d2] & 0x7f) != 0x7f) to[d2] = (uint8_t)f32x2_e4m3(round_to_odd((w * cs.x + u * cs.y) * (double)inv), 0.f);
+      }
+    }
+  }
   if (lane == 0 && (begun || e > old)) *scale = (uint8_t)(e + 127);
 }
 
@@ -307,7 +284,8 @@ static cudaError_t launch_append8_of(const Append8Args& a, const RopeTurns& rope
   const int heads = std::min(a.pages.p.nkv, kApMaxHeads);
   const long long blocks = 2ll * a.batch.n_seqs + a.batch.n_tokens / kScaleBlock;
   const dim3 grid((unsigned)blocks, 2u * (unsigned)((a.pages.p.nkv + heads - 1) / heads));
-  return launch(true, k_append8<T, VEC, LANES, NC>, grid, dim3(32 * heads), 0, st, a, rope);
+  return a.positions && !a.gain ? launch(true, k_append8<T, VEC, LANES, NC, true>, grid, dim3(32 * heads), 0, st, a, rope)
+                                : launch(true, k_append8<T, VEC, LANES, NC, false>, grid, dim3(32 * heads), 0, st, a, rope);
 }
 
 template <typename T>
