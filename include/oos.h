@@ -559,8 +559,7 @@ int oos_paged_append8(const oos_paged_cache8* cache, const oos_batch* batch, int
  *          below 2^-21 of the row's largest weight times scale to 2^-32 of that
  *   many   scores are of q with an error of at most 2^-17 of the largest; weights are
  *          rounded to bf16 (2^-8, a sixteenth of what a code is rounded by) for BF16, and
- *          for F16 as above, where a scale below 2^-60 counts as 2^-60 and its codes are
- *          rounded to binary16 in the unit of that
+ *          as above for F16
  * Where weights are bf16 a row is divided by their rounded sum.  Everything else is as
  * in oos_shared_prefix_attention, its status and refusals included. */
 size_t oos_shared_prefix_attention8_workspace_bytes(int32_t dtype, int32_t n_q_heads, int32_t prefix_len,

@@ -19,8 +19,9 @@
 //     the conversion of two at a time, and the scale 2^e is a factor of the weight,
 //     2^(score + e - m + 7) with m a maximum of score + e: what a row adds up is rounded to
 //     2^-11, below 2^-21 of its largest term (448 2^e times the weight) to 2^-32 of that.  The sum of the weights is
-//     taken of unrounded ones without the scales, which a weight's own has to leave some of in
-//     32 bits: an e below -60 counts as -60, and the codes are made smaller instead.
+//     taken of unrounded ones without the scales, which has all of them down to 2^-37 of the
+//     largest while every e is 48 at most, either way.  From the first tile with another e on it
+//     has exponentials of its own, with a maximum of the scores alone.
 //
 // 13 prompts of up to 300 tokens, 40 heads over 8, 1000 shared and up to 1800 own keys in
 // binary16: 200 us (tiles of 16 rows, before this kernel: 783); 16 trees of up to 64 nodes, 32
@@ -43,7 +44,7 @@ constexpr int kT8VStages = 2;
 constexpr int kT8Threads = 512;            // K; scores; P.V; -; V x 4; softmax x 8
 constexpr int kT8Soft0 = 8, kT8V0 = 4;
 constexpr int kT8Ordered = 64;             // sequences whose tiles are dealt by length
-constexpr int kT8LowExp = -60;             // V's exponents in binary16 weights
+constexpr int kT8NearExp = 48;             // V's exponents whose weights in binary16 give the sum, too
 constexpr int kT8RegsIo = 64, kT8RegsSoft = 192, kT8RegsLaunch = 128;
 static_assert(256 * kT8RegsIo + 256 * kT8RegsSoft <= kT8Threads * kT8RegsLaunch, "register split");
 // PARTS: of a query
@@ -65,13 +66,6 @@ OOS_DEV uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // bytes 0 and 2 (1 and 3) of a word of codes as bf16 of 2^-120 the value
 OOS_DEV uint32_t even_codes(uint32_t w) { return ((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u); }
 OOS_DEV uint32_t odd_codes(uint32_t w) { return (w & 0x80008000u) | ((w >> 4) & 0x07f007f0u); }
-OOS_DEV uint32_t mul_half2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// 2^e as binary16, e <= 0; 0 below 2^-24
-OOS_DEV uint32_t half_power(int e) { return e >= -14 ? (uint32_t)(min(e, 0) + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u; }
 
 // Instruction descriptor of tcgen05.mma.kind::f8f6f4 with e4m3 A and B (format 0 in both
 // fields), fp32 D, both K-major
@@ -158,8 +152,9 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
   uint64_t* qready = bar + 20;     // eight warps: queries in shared memory
   uint64_t* odone = bar + 21;      // both issuers: all products done
   uint64_t* sets_read = bar + 22;  // eight warps: ancestors in registers
-  // of a V stage, by the V warps: the power of K's scale and 2^-7, V's scale if the weights take
-  // it and the keys that are there, of each 16, and a byte of each warp: a v is NaN
+  // of a V stage, by the V warps: the power of K's scale and 2^-7, V's exponent if the weights take
+  // it and the keys that are there, of each 16, and a byte of each warp: a v is NaN (1), an
+  // exponent of the weights is not near 0 (2)
   float* s_kpow = reinterpret_cast<float*>(bar + 23);                // [2][8]
   float* s_vexp = s_kpow + 16;                                       // [2][8]
   uint16_t* s_valid = reinterpret_cast<uint16_t*>(s_vexp + 16);      // [2][8]
@@ -362,7 +357,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
       if (n >= kT8VStages &&
           !__all_sync(0xffffffffu, tl_wait(&vempty[st], (uint32_t)(n / kT8VStages - 1) & 1u, abort_flag, status)))
         break;
-      bool nan = false;
+      bool nan = false, far = false;
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
         const int from = 2 * (n & 15) + h, b = v + 4 * h;
@@ -371,11 +366,12 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
         const int left = n_own - (t0 + n) * kTlKeys - b * kScaleBlock;
         if (lane == 0) {
           s_kpow[8 * st + b] = pow2f(ek - 7);
-          if (F16) s_vexp[8 * st + b] = (float)max(ev, kT8LowExp);
+          if (F16) s_vexp[8 * st + b] = (float)ev;
           s_valid[8 * st + b] = (uint16_t)(there && left > 0 ? (1u << min(left, kScaleBlock)) - 1 : 0u);
         }
         const int e1 = min(ev, 7);
-        const uint32_t f1 = F16 ? half_power(ev - kT8LowExp) : (uint32_t)(120 + e1 + 127) << 7, f2 = (uint32_t)(ev - e1 + 127) << 7;
+        const uint32_t f1 = (uint32_t)(120 + e1 + 127) << 7, f2 = (uint32_t)(ev - e1 + 127) << 7;   // bf16's
+        far = far || abs(ev) > kT8NearExp;
         const unsigned char* in = raw + n % L::kRaw * kT8Codes + b * (kScaleBlock * kTlD) + lane * 16;
         const int c = lane & 7;
         unsigned char* out = sm + L::kOffV + st * kTlTile + (c >> 2) * kTlDBlock;
@@ -391,9 +387,9 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
             x[2 * j + 1] = F16 ? e4m3x2_half2((uint16_t)(w[j] >> 16)) : mul_bf16x2(odd_codes(w[j]), f1 | f1 << 16);
             top |= (w[j] & 0x7f7f7f7fu) + 0x01010101u;
           }
-          if (F16 ? ev < kT8LowExp : ev > 7) {
+          if (!F16 && ev > 7) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = F16 ? mul_half2(x[j], f1 | f1 << 16) : mul_bf16x2(x[j], f2 | f2 << 16);
+            for (int j = 0; j < 8; ++j) x[j] = mul_bf16x2(x[j], f2 | f2 << 16);
           }
           if (top & 0x80808080u) {
             nan = true;
@@ -414,7 +410,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
         }
       }
       nan = __any_sync(0xffffffffu, nan);
-      if (lane == 0) s_wild[4 * st + v] = nan;
+      if (lane == 0) s_wild[4 * st + v] = (nan ? 1 : 0) | (F16 && far ? 2 : 0);
       if ((n & 15) == 15) {
         at = at2;
         sk = sk2;
@@ -516,6 +512,8 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
     const uint32_t ts = tmem + lane_off + kTlTmS, tp = tmem + lane_off + kTlTmP + x * (kTlKeys / 2);
     const uint32_t to = tmem + lane_off + kTlTmO + x * kTlD;
     float m = -INFINITY, l = 0.f;
+    bool far = false;       // the sum of the weights is in 2^(ml - 7)
+    float ml = 0.f;
     for (int j = 0; j < mine; ++j) {
       if (!__all_sync(0xffffffffu, tl_wait(&sfull[x], (uint32_t)j & 1u, abort_flag, status))) break;
       tc_fence_after();
@@ -529,8 +527,6 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
       if (lane == 0) mbar_arrive(&sfree[x]);
       bool apart = false;
       uint32_t see[4];   // keys of the tile that the row sees
-      float scb[8];      // what a score of each 16 keys is multiplied by
-      float sve[8];      // and V's exponent, if the weights take it
       {
         const int vst = tile % kT8VStages, seen = t.first - i * kTlKeys;   // keys committed before the step
         // V is there, and with it the words on the keys
@@ -540,11 +536,6 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
         for (int k = 0; k < 4; ++k) {
           see[k] = reinterpret_cast<const uint32_t*>(s_valid)[4 * vst + k];
           there &= see[k];
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          scb[k] = fmaxf(sc * s_kpow[8 * vst + k], 0x1p-126f);   // not 0: -inf times it stays
-          sve[k] = F16 ? s_vexp[8 * vst + k] : 0.f;
         }
         const bool full = there == ~0u && (a.parent ? seen : seen + tok_lo + 1) >= kTlKeys;   // of the whole stream
         if (!full) {
@@ -564,16 +555,23 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
 #pragma unroll
           for (int k = 0; k < 128; ++k)
             if (!((see[k >> 5] >> (k & 31)) & 1)) sv[k] = -INFINITY;
-          apart = (long long)(i + 1) * kTlKeys > t.first && reinterpret_cast<const uint32_t*>(s_wild)[vst] != 0;
+          apart = (long long)(i + 1) * kTlKeys > t.first && (reinterpret_cast<const uint32_t*>(s_wild)[vst] & 0x01010101u) != 0;
+        }
+        if (F16 && !far && (reinterpret_cast<const uint32_t*>(s_wild)[vst] & 0x02020202u) != 0) {
+          far = true;
+          ml = m;
         }
       }
+      auto scb = [&](int k) { return fmaxf(sc * s_kpow[8 * (tile % kT8VStages) + k], 0x1p-126f); };   // not 0: -inf times it stays
+      // V's exponent, if the weights take it; read where it is used, for want of registers
+      auto v_exp = [&](int k) { return F16 ? s_vexp[8 * (tile % kT8VStages) + k] : 0.f; };
       float tmax = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         float mx[2] = {max_nan(sv[16 * k], sv[16 * k + 1]), max_nan(sv[16 * k + 2], sv[16 * k + 3])};
 #pragma unroll
         for (int i = 4; i < 16; i += 2) mx[(i >> 1) & 1] = max3_nan(mx[(i >> 1) & 1], sv[16 * k + i], sv[16 * k + i + 1]);
-        tmax = max_nan(tmax, fmaf(max_nan(mx[0], mx[1]), scb[k], sve[k]));
+        tmax = max_nan(tmax, fmaf(max_nan(mx[0], mx[1]), scb(k), v_exp(k)));
       }
       const bool move = !(tmax <= m + 8.f);   // a NaN moves it, and stays
       // the tile before has left this P and is in O
@@ -595,8 +593,20 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
             tmem_st16u(to + 32 * c + 16, reinterpret_cast<const uint32_t*>(ov + 16));
           }
         }
-        l *= f;
+        if (!F16 || !far) l *= f;
         if (move) m = tmax;
+      }
+      if (F16 && far) {
+        float smax = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 128; ++k) smax = max_nan(smax, sv[k] * scb(k >> 4));
+        if (!(smax <= ml + 8.f)) {
+          l *= ml == -INFINITY ? 0.f : exp2f(ml - smax);
+          ml = smax;
+        }
+        const float by = ml == -INFINITY ? 0.f : kHalfBias - ml;
+#pragma unroll
+        for (int k = 0; k < 128; ++k) l += ex2_approx(fmaf(sv[k], scb(k >> 4), by));
       }
       // weights 2^(s sc - m); without a finite score yet every score is -inf, and gives 0
       const float neg = m == -INFINITY ? 0.f : (F16 ? kHalfBias : 0.f) - m;
@@ -609,14 +619,14 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
-            const float f = scb[2 * c + (i >> 4)], by = neg + sve[2 * c + (i >> 4)];
+            const float f = scb(2 * c + (i >> 4)), by = neg + v_exp(2 * c + (i >> 4));
             float2 e = fma2(make_float2(sv[32 * c + i], sv[32 * c + i + 1]), make_float2(f, f), make_float2(by, by));
             e = make_float2(ex2_approx(e.x), ex2_approx(e.y));
             if constexpr (F16) {
               const __half2 v = __floats2half2_rn(e.x, e.y);
               pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
               sum = (i & 15) == 0 ? e : add2(sum, e);
-              if ((i & 15) == 14) l_new = fmaf(sum.x + sum.y, exp2i(-(int)sve[2 * c + (i >> 4)]), l_new);
+              if ((i & 15) == 14) l_new = fmaf(sum.x + sum.y, exp2i(-(int)v_exp(2 * c + (i >> 4))), l_new);
             } else {
               const __nv_bfloat162 v = __floats2bfloat162_rn(e.x, e.y);
               pk[i / 2] = *reinterpret_cast<const uint32_t*>(&v);
@@ -673,12 +683,18 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
           mbar_arrive(&pfull[2 * x + 1]);
         }
       }
-      l += F16 ? l_new : (ps[0].x + ps[0].y) + (ps[1].x + ps[1].y);
+      if (!F16) l_new = (ps[0].x + ps[0].y) + (ps[1].x + ps[1].y);
+      if (!F16 || !far) l += l_new;
     }
     // the ring and TMEM are free once all products are done (the issuer always says so)
     drain_wait(odone, 0);
     tc_fence_after();
     const bool have = mine > 0 && !*abort_flag;
+    float unit = 1.f;   // of O, in the sum's
+    if (F16 && far) {
+      unit = ml == -INFINITY ? 1.f : exp2f(m - ml);
+      m = ml;
+    }
     float* row = stage + (size_t)(x * kTlRows + lrow) * kPartLd;
 #pragma unroll 1
     for (int c = 0; c < 4; ++c) {
@@ -689,7 +705,7 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
       for (int i = 0; i < 32; i += 4)
         *reinterpret_cast<float4*>(row + 32 * c + i) =
             !have ? make_float4(0.f, 0.f, 0.f, 0.f)
-            : F16 ? make_float4(ov[i], ov[i + 1], ov[i + 2], ov[i + 3])
+            : F16 ? make_float4(ov[i] * unit, ov[i + 1] * unit, ov[i + 2] * unit, ov[i + 3] * unit)
                   : make_float4(ov[i], ov[i + 2], ov[i + 1], ov[i + 3]);   // V's order
     }
     *reinterpret_cast<float2*>(row + kTlD) = make_float2(have ? (F16 ? m - kHalfBias : m) : -INFINITY, have ? l : 0.f);

@@ -1,0 +1,72 @@
+"""GPU tests of the weights of attention over 8-bit pages: what few rows round them by, and their sum beside scales of V
+that lie far apart.  Against 64 bits (pages8_ref.py)."""
+
+import math
+
+import pytest
+import torch
+
+import batch_ref as R
+import pages8_ref as R8
+import test_gpu_pages8 as T
+from paper_2608_00814_gb300 import binding as B
+from test_gpu_batch_ops import BF16, F16, gen, randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _built():
+    from paper_2608_00814_gb300 import _build
+    _build.build()
+
+
+@pytest.mark.parametrize("dtype, kv", [(BF16, BF16), (BF16, F16), (F16, F16)])
+@pytest.mark.parametrize("counts, lens, nq, width", [
+    ([1, 1, 1, 1], [700, 90, 333, 16], 8, None),        # tiles of 8 rows, a block each
+    ([1, 1, 1, 1], [700, 90, 333, 16], 8, 70),          # equal shares
+    ([5, 2, 9, 1], [400, 90, 333, 200], 8, None),
+    ([5, 2, 9, 1], [400, 90, 333, 200], 8, 70),
+    ([100, 90], [300, 420], 2, 70),                     # 95 rows on average, few tiles: the same kernels
+    ([200], [450], 2, None),                            # and over a short table
+])
+def test_few_rows_round_own_weights_to_11_bits(dtype, kv, counts, lens, nq, width):
+    """Without a prefix every weight is binary16's, of bf16 queries too: half a step of 2^-11, where bf16 has 2^-8; and of q
+    2^-25 of a row's largest is left out."""
+    d = 128
+    step = R.Step(counts, lens, 16, seed=1, width=width)
+    q, _, _, cache = T.inputs8(step, 0, nq, 2, d, dtype, kv, seed=2)
+    out, st = T.attend8(step, q, None, None, 0, cache)
+    assert int(st) == 0
+    none = torch.zeros(0, 2, d, dtype=F16, device="cuda")
+    out64, mag, size, (left, _, term, v) = R8.attention(step, q, none, none, cache, 1 / math.sqrt(d))
+    left = min(left, left * 2.0 ** -8) if step.n * (nq // 2) > 64 * len(counts) else left
+    R8.check_attention(out, out64, mag, size, (left, R.U[F16], term, v), max(lens))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("high", [30, 110, 119])
+@pytest.mark.parametrize("low", [-20, -60, -117])
+@pytest.mark.parametrize("counts, lens, width", [([1, 2], [70, 300], None), ([1, 2], [70, 300], 80), ([90, 140], [400, 330], 80)])
+def test_weights_count_whatever_scale_their_v_has(dtype, high, low, counts, lens, width):
+    """Blocks of zeros under a large scale, and between them blocks whose scores are 2^10 of the others' and whose v is all
+    but zero: they weigh as much as their scores say, which the prefix's v shows.  Their own v is below 2^-11 of what is
+    added up, or lost beside the large scale: 2^-32 of that at most, as far as zeros count."""
+    d, nkv, nq, prefix = 128, 2, 4, 40
+    step = R.Step(counts, lens, 16, seed=3, width=width)
+    g = gen(4)
+    q = (1 + randn(g, step.rows, nq, d, std=0.05)).to(dtype)
+    pk, pv = torch.zeros(prefix, nkv, d, dtype=dtype, device="cuda"), randn(g, prefix, nkv, d, dtype=dtype)
+    k, v, ks, vs = T.pool(g, step.n_pages, 16, nkv, d)
+    ks.fill_(127)
+    odd = torch.arange(step.n_pages, device="cuda") % 2 == 1
+    k.copy_(torch.where(odd[:, None, None, None], 1.0, 0.0).expand(k.shape).to(k.dtype))
+    v.copy_(torch.where(odd[:, None, None, None], v.float(), 0.0).to(v.dtype))
+    vs.copy_((127 + torch.where(odd, low, high)).to(torch.uint8)[:, None, None].expand(vs.shape))
+    cache = B.PagedCache8(k, v, ks, vs)
+    scale = 10 * math.log(2) / d
+    out, st = T.attend8(step, q, pk, pv, prefix, cache, scale=scale)
+    assert int(st) == 0
+    ref, mag, size, (left, weights, _, _) = R8.attention(step, q, pk, pv, cache, scale)
+    own = 448 * 2.0 ** low      # of v: at most all of it is lost
+    R8.check_attention(out, ref, mag, size, (left, weights, own / (prefix + max(lens)), 0.0), prefix + max(lens))
