@@ -587,7 +587,8 @@ int oos_shared_prefix_attention8(int32_t dtype, int32_t n_q_heads, const void* q
  *                  the sequence's rows, strictly ascending (a path from the root down is)
  *   accepted_len   DEVICE int32[n_seqs]: 0 .. n_b, of a sequence with at most 128 rows
  *   out_seq_len    DEVICE int32[n_seqs]: first_b + accepted_len[b], the positions that
- *                  count from now on; overlaps no other argument
+ *                  count from now on; overlaps no other argument (OOS_EINVAL where it does
+ *                  batch's arrays, accepted, accepted_len or out_status)
  *   out_status     DEVICE int32[1], the caller's to clear: OOS_EBATCH when a sequence's
  *                  offsets, length, nodes or pages are out of range; all its positions then
  *                  stay as they are, and out_seq_len[b] is seq_len[b].

@@ -246,6 +246,16 @@ static void fill(const oos_paged_cache8* c, int n, LayerPtrs* p) {
   }
 }
 
+// The first block writes the new lengths while the others still read the call's arrays: n values
+// at p on any of them.
+static bool overlaps_batch(const oos_batch& b, const int32_t* accepted, const int32_t* accepted_len, const int32_t* status,
+                           const int32_t* p) {
+  const long long n = b.n_seqs;
+  auto on = [&](const int32_t* q, long long m) { return (uintptr_t)p < (uintptr_t)q + 4 * m && (uintptr_t)q < (uintptr_t)p + 4 * n; };
+  return on(b.q_start, n + 1) || on(b.seq_len, n) || on(b.block_table, n * b.max_pages) || on(accepted, b.n_tokens) ||
+         on(accepted_len, n) || on(status, 1);
+}
+
 template <typename C>
 static int compact(const C* layers, int n_layers, const oos_batch* batch, const int32_t* accepted,
                    const int32_t* accepted_len, int32_t* out_seq_len, int32_t* out_status, void* stream) {
@@ -256,7 +266,7 @@ static int compact(const C* layers, int n_layers, const oos_batch* batch, const 
   if (!layers_of(layers, n_layers, &l)) return OOS_EINVAL;
   if (!l.es || !head_dim_ok(l.d)) return OOS_EUNSUPPORTED;
   const long long row = (long long)l.nkv * l.d * l.es;
-  if (row > (1 << 24)) return OOS_EINVAL;
+  if (row > (1 << 24) || overlaps_batch(*batch, accepted, accepted_len, out_status, out_seq_len)) return OOS_EINVAL;
   CompactArgs a;
   memset(&a, 0, sizeof(a));
   a.batch = view_of(*batch);
