@@ -328,7 +328,7 @@ static int attend(int dtype, int n_q_heads, const void* q, int64_t q_stride, con
   cudaError_t e;
   if (p.tc) {
     a.p_splits = p.prefix.splits;
-    a.s_splits = p.few ? p.pages.splits : p.sequence.splits;
+    a.s_splits = p.few ? p.pages.splits : p.sequence.splits;   // 0 of few rows over 8-bit pages
     a.own_part = p.few ? p.pages.part : p.sequence.part;
     e = a.p_splits > 0 ? launch_prefix_tc(a, p.prefix, dtype, c.dtype, st) : cudaSuccess;
     if (e == cudaSuccess && p.stream) e = launch_stream8(a, p.shares, (uint8_t*)workspace + p.shares_off, dtype, st);
@@ -336,7 +336,7 @@ static int attend(int dtype, int n_q_heads, const void* q, int64_t q_stride, con
       e = !p.few ? (own8 ? launch_sequence8_tc(a, p.sequence, dtype, st) : launch_sequence_tc(a, p.sequence, dtype, c.dtype, st))
                  : own8 ? launch_pages8_tc(a, p.pages, dtype, st)
                         : launch_pages_tc(a, p.pages, dtype, c.dtype, st);
-    if (p.few && !own8) a.s_splits = p.pages.part;   // for the join
+    if (p.few) a.s_splits = p.pages.part;   // for the join
     if (e == cudaSuccess && (p.few ? p.pages.part : p.sequence.part || a.s_splits > 1)) {
       const dim3 grid((unsigned)(((long long)batch->n_tokens * n_q_heads + 7) / 8));
       e = dtype == OOS_DTYPE_BF16 ? launch(true, k_attn_join_parts<__nv_bfloat16>, grid, dim3(256), 0, st, a)

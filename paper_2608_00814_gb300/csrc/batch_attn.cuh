@@ -197,7 +197,7 @@ cudaError_t launch_prefix_tc(const BatchAttnArgs& a, const PrefixPlan& p, int dt
 // splits of launch_sequence_tc, or own_part, left as parts p_splits .. for k_attn_join_parts
 cudaError_t launch_sequence_tc(const BatchAttnArgs& a, const SequencePlan& p, int dtype, int kv_dtype, cudaStream_t st);
 cudaError_t launch_pages_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, int kv_dtype, cudaStream_t st);
-// the same over 8-bit pages, queries of dtype; several splits leave parts
+// the same over 8-bit pages, queries of dtype: a block for each tile, which joins its rows itself
 PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, int n_sms);
 cudaError_t launch_pages8_tc(const BatchAttnArgs& a, const PagesPlan& p, int dtype, cudaStream_t st);
 // the same, an equal share of all keys for every warp, and the join; n_seqs <= kStreamSeqs

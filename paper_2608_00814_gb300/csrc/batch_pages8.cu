@@ -142,7 +142,6 @@ PagesPlan plan_pages8_tc(long long rows, int n_seqs, int nkv, int n_sms) {
   const int per_sm = p8_blocks(rows <= 8ll * n_seqs ? 1 : 2);
   p.tile_rows = rows <= 8ll * n_seqs ? 8 : 16;
   p.tiles = (int)(n_seqs + rows / p.tile_rows);
-  p.splits = 1;
   const long long live = std::max((long long)n_seqs, (rows + p.tile_rows - 1) / p.tile_rows) * nkv;
   p.sms = (int)std::min<long long>(n_sms, (live + per_sm - 1) / per_sm);
   return p;
