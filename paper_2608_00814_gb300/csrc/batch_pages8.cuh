@@ -267,7 +267,7 @@ struct P8Rows {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[h][n][e] *= sc[n][e & 1] * pk;
+        for (int e = 0; e < 4; ++e) s[h][n][e] *= fminf(sc[n][e & 1] * pk, kMostFactor);
     }
     // keys that each of this thread's rows sees
     const int seen = t.first - key0;   // those before it are committed

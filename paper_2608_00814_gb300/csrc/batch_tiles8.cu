@@ -562,7 +562,8 @@ __global__ void __launch_bounds__(kT8Threads, 1) k_attn_tiles8(const __grid_cons
           ml = m;
         }
       }
-      auto scb = [&](int k) { return fmaxf(sc * s_kpow[8 * (tile % kT8VStages) + k], 0x1p-126f); };   // not 0: -inf times it stays
+      // a score's factor; not 0: -inf times it stays
+      auto scb = [&](int k) { return fminf(fmaxf(sc * s_kpow[8 * (tile % kT8VStages) + k], 0x1p-126f), kMostFactor); };
       // V's exponent, if the weights take it; read where it is used, for want of registers
       auto v_exp = [&](int k) { return F16 ? s_vexp[8 * (tile % kT8VStages) + k] : 0.f; };
       float tmax = -INFINITY;

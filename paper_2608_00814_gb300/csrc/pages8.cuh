@@ -24,6 +24,8 @@ inline Pages8View view_of(const oos_paged_cache8& c) {
 
 // exponent of a scale's byte
 OOS_DEV int scale_exp(int byte) { return max(kScaleLow, min(kScaleHigh, byte - 127)); }
+// what a score may be multiplied by: past fp32's largest number a score of 0 would be NaN
+constexpr float kMostFactor = 0x1.fffffep127f;
 OOS_DEV float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 
 // Exponent of the least scale that holds the magnitude: m 2^e <= 448 2^(e - 8) for m <= 1.75.

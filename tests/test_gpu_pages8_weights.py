@@ -70,3 +70,32 @@ def test_weights_count_whatever_scale_their_v_has(dtype, high, low, counts, lens
     ref, mag, size, (left, weights, _, _) = R8.attention(step, q, pk, pv, cache, scale)
     own = 448 * 2.0 ** low      # of v: at most all of it is lost
     R8.check_attention(out, ref, mag, size, (left, weights, own / (prefix + max(lens)), 0.0), prefix + max(lens))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("counts, lens, width", [([1, 2], [70, 300], None), ([1, 2], [70, 300], 80), ([90, 140], [400, 330], 80)])
+def test_factors_past_fp32(dtype, counts, lens, width):
+    """A key whose score is far below fp32's range beside keys of zeros, under the largest scale and with large queries, so
+    that what a product of codes is multiplied by is past fp32: the zeros' scores are 0 and weigh the same (1, exactly), the
+    other key nothing.  So out is v's mean: half a step of it, and of fp32 for each key of either sum."""
+    d, nkv, nq = 128, 2, 4
+    step = R.Step(counts, lens, 16, seed=3, width=width)
+    g = gen(5)
+    q = (256 * (1 + randn(g, step.rows, nq, d).abs().clamp(max=2))).to(dtype)
+    k, v, ks, vs = T.pool(g, step.n_pages, 16, nkv, d, lo=-8, hi=-4)
+    k.zero_()
+    ks.fill_(127 + 119)
+    for b in range(len(counts)):
+        for s in (3, lens[b] - counts[b] - 20):
+            page, at = step.where(b, s)
+            k[page, at] = -448.0
+    cache = B.PagedCache8(k, v, ks, vs)
+    scale = 512.0
+    out, st = T.attend8(step, q, None, None, 0, cache, scale=scale)
+    assert int(st) == 0
+    none = torch.zeros(0, nkv, d, dtype=dtype, device="cuda")
+    ref, mag, _, _ = R8.attention(step, q, none, none, cache, scale)
+    out = out[:step.n].double().cpu()
+    assert bool(torch.isfinite(out).all())
+    tol = R.U[dtype] * ref.abs() + (4 * max(lens) + 64) * R.F32 * mag + (2.0 ** -25 if dtype is F16 else 0)
+    assert bool(((out - ref).abs() <= tol).all()), float(((out - ref).abs() - tol).max())
