@@ -538,6 +538,8 @@ typedef struct {
  *     larger scale, the codes already there are rounded again to it; a smaller one is
  *     not taken.  So a position appended alone may be rounded up to once more for each
  *     octave that the scale grows by, each time by half a step of the new one.
+ * All rows of a step count, nodes of a tree that are then rejected among them: what they made
+ * a scale stays, also after oos_paged_compact8, and so does what codes were rounded by.
  * The scale is of the fp32 values after norm and rotation, which are then rounded once,
  * to the nearest even code: of two codes whose border lies within fp32's error of a value
  * (a few 2^-24 of its pair's length) it may take either.  Values that are not finite become

@@ -34,7 +34,8 @@ constexpr int kS8MaxPlaces = 256;    // of a tile, about: longer pieces otherwis
 constexpr int kS8JoinThreads = 128;
 // Units that a warp takes in a microsecond, by which the shares of blocks that start when the
 // prefix's are done are smaller (64 requests as above: 0 59 us, 0.25 to 0.45 55, 0.65 56; 200 of
-// up to 1500 keys 83, 84 to 86, 93)
+// up to 1500 keys 83, 84 to 86, 93; in tiles of 16 rows 64 trees of up to 4 nodes 0 78, 0.15 77,
+// 0.3 and 0.45 74, 200 of them over up to 1500 keys 116, 111, 105, 104)
 constexpr double kS8UnitsPerUs = 0.3;
 
 // Shares of `piece` units for the first `early` warps, of `late` less for the others
