@@ -99,3 +99,43 @@ def test_factors_past_fp32(dtype, counts, lens, width):
     assert bool(torch.isfinite(out).all())
     tol = R.U[dtype] * ref.abs() + (4 * max(lens) + 64) * R.F32 * mag + (2.0 ** -25 if dtype is F16 else 0)
     assert bool(((out - ref).abs() <= tol).all()), float(((out - ref).abs() - tol).max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("nan", [False, True])
+@pytest.mark.parametrize("counts, lens, nq, start", [
+    ([90, 128], [700, 300], 8, 256),       # two row tiles a block; from the third tile of keys on
+    ([128, 100], [128, 900], 2, 0),        # one, whose tiles of keys two streams take in turn
+    ([128, 120], [1000, 640], 2, 384),
+    ([110, 127], [5000, 4900], 2, 2300),   # several ranges of keys a sequence
+    ([128], [2600], 10, 2048),
+])
+def test_scales_far_from_those_before(dtype, tree, nan, counts, lens, nq, start):
+    """From some position on a third of V's blocks stand under scales of next to nothing and of the least there is, behind
+    tiles of ordinary ones; also with trees, and with a NaN among the step's own v, which reaches the rows that see it."""
+    d, nkv, prefix = 128, 2, 70
+    step = R.Step(counts, lens, 16, seed=6, width=330)
+    parent = [-1 if j == 0 else max(0, j - 1 - j % 3) for c in counts for j in range(c)] if tree else None
+    par = torch.tensor(parent, dtype=torch.int32, device="cuda") if tree else None
+    q, pk, pv, cache = T.inputs8(step, prefix, nq, nkv, d, dtype, dtype, seed=7, std=0.5)
+    for b, n in enumerate(lens):
+        for s in range(start // 16 * 16, n, 16):
+            if (s // 16) % 3:
+                page, at = step.where(b, s)
+                cache.v_scale[page, at // 16] = 127 - (117 if (s // 16) % 3 == 1 else 55)
+    ref = R8.attention(step, q, pk[:prefix], pv[:prefix], cache, 1 / math.sqrt(d), parent)
+    want = torch.zeros(step.n, nq, dtype=torch.bool)
+    if nan:
+        b, node = len(counts) - 1, 40
+        page, at = step.where(b, lens[b] - counts[b] + node)
+        cache.v.view(torch.uint8)[page, at, 1, 9] = R8.NAN_CODE
+        first = step.q_start[b]
+        seen = R.ancestors(parent[first:first + counts[b]])[:, node] if tree else torch.arange(counts[b]) >= node
+        want[first:first + counts[b], nq // 2:] = seen[:, None]
+    out, st = T.attend8(step, q, pk, pv, prefix, cache, par)
+    assert int(st) == 0
+    out = out[:step.n]
+    assert torch.equal(torch.isnan(out[..., 9]).cpu(), want) and int(torch.isnan(out).sum()) == int(want.sum())
+    out = torch.where(torch.isnan(out), ref[0].to(dtype).cuda(), out)
+    R8.check_attention(out, *ref, prefix + max(lens))
